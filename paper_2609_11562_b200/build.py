@@ -4,11 +4,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libentwine.so")
+INCLUDE = os.path.join(ROOT, "include")
 SOURCES = ["plan.cc", "entwine_kernels.cu"]
 
 
@@ -26,7 +28,7 @@ def _source_hash() -> str:
     """Hash of everything the library is built from (file times do not survive a copy of the tree)."""
     import hashlib
     h = hashlib.sha256()
-    deps = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC)) + [os.path.join(ROOT, "include", "entwine.h")]
+    deps = sorted(os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d))
     for d in deps:
         h.update(os.path.basename(d).encode())
         with open(d, "rb") as f:
@@ -45,17 +47,24 @@ def needs_build() -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
-    cmd = [_nvcc(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-shared", "-Xcompiler", "-fPIC", "-x", "cu",
-           "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    flags = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-Xcompiler", "-fPIC",
+             "-I", INCLUDE, "-I", CSRC]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += os.environ.get("ENTWINE_NVCC_FLAGS", "").split()
-    cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode != 0:
+        flags += ["-Xptxas", "-v"]
+    flags += os.environ.get("ENTWINE_NVCC_FLAGS", "").split()
+    with tempfile.TemporaryDirectory() as tmp:
+        # the sources side by side, then one link
+        objs = [os.path.join(tmp, src + ".o") for src in SOURCES]
+        cmds = [[_nvcc(), *flags, "-x", "cu", "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
+        cmds = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in cmds]
+        outs = [(p.communicate()[0], p.returncode) for p in cmds]
+        if all(rc == 0 for _, rc in outs):
+            res = subprocess.run([_nvcc(), *flags, "-shared", *objs, "-o", LIB], capture_output=True, text=True)
+            outs.append((res.stdout + res.stderr, res.returncode))
+    for text, rc in outs:
+        if verbose or rc != 0:
+            sys.stderr.write(text)
+    if any(rc != 0 for _, rc in outs):
         raise RuntimeError("nvcc failed building libentwine.so")
     with open(STAMP, "w") as f:
         f.write(_source_hash() + "\n")
