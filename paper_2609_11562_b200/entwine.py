@@ -1,9 +1,13 @@
-"""ctypes binding over the C-ABI library (include/entwine.h).
+"""ctypes binding over the C-ABI library (include/entwine.h, include/entwine_ops.h).
 
 Argument marshalling only: every step of the path runs in the CUDA library.  Importing this
 module fails loudly if libentwine.so has not been built (there is no fallback).
 Device-buffer arguments are torch CUDA tensors (bf16, contiguous) or raw integer addresses;
 `stream` is a torch.cuda.Stream, a raw handle or None (the current torch stream).
+
+The operators beside the fused call (quant_i8, moe_dispatch and the others at the end of this file) take
+torch CUDA tensors only: sizes, row distances and element types are read from them, and what does not fit
+together is refused with EntwineError(ERR_INVALID) before anything is launched.
 """
 from __future__ import annotations
 
@@ -11,6 +15,7 @@ import ctypes
 import os
 
 import numpy as np
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libentwine.so")
@@ -63,6 +68,18 @@ _lib.entwine_destroy.argtypes = [_vp]
 _lib.entwine_gemm_rs_static.argtypes = [_vp] * 7 + [ctypes.POINTER(_i64)]
 _lib.entwine_strerror.argtypes = [_int]
 _lib.entwine_strerror.restype = ctypes.c_char_p
+# every symbol include/entwine_ops.h declares, with its argument types
+_OP_ARGS = {
+    "entwine_quant_i8": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _vp],
+    "entwine_moe_dispatch": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp],
+    "entwine_moe_dispatch_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp],
+    "entwine_moe_combine": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp],
+    "entwine_moe_combine_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp],
+}
+OP_SYMBOLS = tuple(_OP_ARGS)
+for _name, _args in _OP_ARGS.items():
+    getattr(_lib, _name).argtypes = _args
+    getattr(_lib, _name).restype = _int
 for _name in SYMBOLS:
     if _name != "entwine_strerror":
         getattr(_lib, _name).restype = _int
@@ -93,7 +110,6 @@ def _ptr(t):
 
 def _stream(s):
     if s is None:
-        import torch
         return torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
@@ -244,3 +260,118 @@ class Plan:
             self.destroy()
         except Exception:
             pass
+
+
+# ------------------------------------------------------------------------------------------
+# operators beside the fused call (include/entwine_ops.h)
+# ------------------------------------------------------------------------------------------
+DTYPE_BF16, DTYPE_FP16, DTYPE_FP32, DTYPE_I8 = 0, 1, 2, 3
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16, torch.float32: DTYPE_FP32, torch.int8: DTYPE_I8}
+_FLOATING = (torch.bfloat16, torch.float16, torch.float32)
+
+
+def _refuse(what):
+    raise EntwineError(ERR_INVALID, what)
+
+
+def _need(ok, what):
+    if not ok:
+        _refuse(what)
+
+
+def _on_device(t, name):
+    if not isinstance(t, torch.Tensor) or t.get_device() < 0 or t.get_device() != torch.cuda.current_device():
+        _refuse(f"{name} must be a tensor on the current CUDA device")
+
+
+def _matrix(t, name, dtypes, shape=None):
+    """A matrix whose rows are contiguous: (rows, cols, distance between two rows)."""
+    _on_device(t, name)
+    if t.dtype not in dtypes or t.dim() != 2 or (shape is not None and t.shape != shape):
+        _refuse(f"{name} must be a matrix{'' if shape is None else f' {tuple(shape)}'} of {' or '.join(map(str, dtypes))}, "
+                f"not {tuple(t.shape)} of {t.dtype}")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
+        _refuse(f"{name} must have contiguous rows that do not overlap (strides {t.stride()})")
+    return rows, cols, max(ld, cols)
+
+
+def _dense(t, name, dtypes, shape):
+    """A contiguous tensor of this shape: its address."""
+    _on_device(t, name)
+    if t.dtype not in dtypes or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name} must be contiguous, {tuple(shape)} of {' or '.join(map(str, dtypes))}, "
+                f"not {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def quant_i8(x, q, scale, stream=None):
+    """Rows to int8 with a scale each: scale = amax / 127, q = rint(127 x / amax), ties to even.
+    x [M, K] bf16, fp16 or fp32; q [M, K] int8; scale [M] fp32."""
+    rows, cols, ldx = _matrix(x, "x", _FLOATING)
+    _, _, ldq = _matrix(q, "q", (torch.int8,), x.shape)
+    _check(_lib.entwine_quant_i8(x.data_ptr(), _DTYPES[x.dtype], rows, cols, ldx, q.data_ptr(), ldq,
+                                 _dense(scale, "scale", (torch.float32,), (rows,)), _stream(stream)), "entwine_quant_i8")
+
+
+def _routing(row_of):
+    _on_device(row_of, "row_of")
+    _need(row_of.dim() == 2, "row_of must be [T, k]")
+    return row_of.shape[0], row_of.shape[1], _dense(row_of, "row_of", (torch.int32,), row_of.shape)
+
+
+def moe_dispatch(x, ids, n_experts, rows, offsets, row_of, x_scale=None, row_scale=None, stream=None):
+    """Tokens sorted by expert.  x [T, H] bf16, fp16, fp32 or int8; ids [T, k] int32 or int64, an id outside
+    [0, n_experts) drops the assignment; rows [T*k, H]; offsets [n_experts+1] int32; row_of [T, k] int32 (-1:
+    dropped); x_scale [T] -> row_scale [T*k] fp32, both or neither.  Rows behind offsets[-1] are left as they were."""
+    T, H, ldx = _matrix(x, "x", tuple(_DTYPES))
+    _on_device(ids, "ids")
+    _need(ids.dim() == 2 and ids.shape[0] == T, "ids must be [T, k]")
+    k = ids.shape[1]
+    _, _, ldr = _matrix(rows, "rows", (x.dtype,), (T * k, H))
+    _need((x_scale is None) == (row_scale is None), "x_scale and row_scale go together")
+    if x_scale is not None:
+        x_scale, row_scale = (_dense(x_scale, "x_scale", (torch.float32,), (T,)),
+                              _dense(row_scale, "row_scale", (torch.float32,), (T * k,)))
+    _check(_lib.entwine_moe_dispatch(x.data_ptr(), _DTYPES[x.dtype], T, H, ldx, x_scale,
+                                     _dense(ids, "ids", (torch.int32, torch.int64), (T, k)), ids.dtype == torch.int64,
+                                     k, int(n_experts), rows.data_ptr(), ldr, row_scale,
+                                     _dense(offsets, "offsets", (torch.int32,), (int(n_experts) + 1,)),
+                                     _dense(row_of, "row_of", (torch.int32,), (T, k)), _stream(stream)),
+           "entwine_moe_dispatch")
+
+
+def moe_dispatch_bwd(d_rows, row_of, dx, stream=None):
+    """Gradient of moe_dispatch: dx[t] = sum_j d_rows[row_of[t, j]] in fp32, j ascending.  d_rows [n, H], dx [T, H]."""
+    n, H, ldr = _matrix(d_rows, "d_rows", _FLOATING)
+    T, k, at = _routing(row_of)
+    _, _, ldx = _matrix(dx, "dx", (d_rows.dtype,), (T, H))
+    _check(_lib.entwine_moe_dispatch_bwd(d_rows.data_ptr(), _DTYPES[d_rows.dtype], n, H, ldr, at, T, k, dx.data_ptr(),
+                                         ldx, _stream(stream)), "entwine_moe_dispatch_bwd")
+
+
+def moe_combine(y, weights, row_of, out, stream=None):
+    """out[t] = sum_j weights[t, j] y[row_of[t, j]] in fp32, j ascending.  y [n, H], out [T, H] of one type, weights
+    [T, k] fp32."""
+    n, H, ldy = _matrix(y, "y", _FLOATING)
+    T, k, at = _routing(row_of)
+    _, _, ldo = _matrix(out, "out", (y.dtype,), (T, H))
+    _check(_lib.entwine_moe_combine(y.data_ptr(), _DTYPES[y.dtype], n, H, ldy,
+                                    _dense(weights, "weights", (torch.float32,), (T, k)), at, T, k, out.data_ptr(),
+                                    ldo, _stream(stream)), "entwine_moe_combine")
+
+
+def moe_combine_bwd(dout, y, weights, row_of, dy, dw, stream=None):
+    """Gradients of moe_combine: dy[row_of[t, j]] = weights[t, j] dout[t], dw[t, j] = <dout[t], y[row_of[t, j]]>
+    (fp32; 0 where dropped).  Rows of dy that no assignment names are left as they were."""
+    T, H, ldo = _matrix(dout, "dout", _FLOATING)
+    _, k, at = _routing(row_of)
+    _need(row_of.shape[0] == T, "row_of must be [T, k]")
+    n, _, ldy = _matrix(y, "y", (dout.dtype,))
+    _need(y.shape[1] == H, "y must have rows as long as dout's")
+    _, _, lddy = _matrix(dy, "dy", (dout.dtype,), (n, H))
+    _check(_lib.entwine_moe_combine_bwd(dout.data_ptr(), _DTYPES[dout.dtype], T, H, ldo, y.data_ptr(), n, ldy,
+                                        _dense(weights, "weights", (torch.float32,), (T, k)), at, k, dy.data_ptr(),
+                                        lddy, _dense(dw, "dw", (torch.float32,), (T, k)), _stream(stream)),
+           "entwine_moe_combine_bwd")

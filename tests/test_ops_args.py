@@ -1,0 +1,152 @@
+"""CPU tests of the operators beside the fused call: every symbol of include/entwine_ops.h is exported and bound, and
+calls that cannot be right are refused before any CUDA call, by the C entry points and by the binding."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2609_11562_b200 import build as B
+
+B.build()
+from paper_2609_11562_b200 import entwine as E  # noqa: E402
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+L = E._lib
+P = 1 << 20  # an aligned address that is never followed: every call below is refused first
+
+
+def test_every_declared_operator_is_exported_and_bound():
+    header = open(os.path.join(ROOT, "include", "entwine_ops.h")).read()
+    declared = set(re.findall(r"^int (entwine_[a-z0-9_]+)\(", header, flags=re.M))
+    assert declared == set(E.OP_SYMBOLS) and declared
+    lib = ctypes.CDLL(E.LIB_PATH)
+    for name in declared:
+        assert hasattr(lib, name), name
+    for name, value in re.findall(r"(ENTWINE_(?:BF16|FP16|FP32|I8)) = (\d)", header):
+        assert getattr(E, name.replace("ENTWINE_", "DTYPE_")) == int(value)
+
+
+def _vary(good, bad):
+    """The good argument list with one argument replaced, for each (index, value) of bad."""
+    for i, v in bad:
+        args = list(good)
+        args[i] = v
+        yield i, v, args
+
+
+def _all_refused(fn, good, bad):
+    for i, v, args in _vary(good, bad):
+        assert fn(*args) == E.ERR_INVALID, (i, v)
+
+
+def test_quant_i8_refusals():
+    good = [P, E.DTYPE_BF16, 4, 64, 64, P, 64, P, None]
+    _all_refused(L.entwine_quant_i8, good, [
+        (0, None), (0, P + 1), (1, E.DTYPE_I8), (1, 9), (1, -1), (2, -1), (2, 1 << 31), (3, 0), (3, -4), (4, 63), (5, None),
+        (6, 63), (7, None), (7, P + 2)])
+    assert L.entwine_quant_i8(None, E.DTYPE_BF16, 0, 64, 64, None, 64, None, None) == E.OK  # nothing to do
+
+
+def test_moe_dispatch_refusals():
+    #       x, dtype, T, H, ldx, x_scale, ids, ids64, k, E, rows, ldr, row_scale, offsets, row_of, stream
+    good = [P, E.DTYPE_BF16, 4, 64, 64, P, P, 1, 2, 8, P, 64, P, P, P, None]
+    _all_refused(L.entwine_moe_dispatch, good, [
+        (0, None), (0, P + 1), (1, 7), (2, -1), (2, 1 << 31), (3, 0), (4, 63), (5, None), (5, P + 2), (6, None), (6, P + 4), (8, 0),
+        (8, -1), (8, 1 << 30), (9, 0), (9, 1025), (10, None), (11, 63), (12, None), (12, P + 1), (13, None), (13, P + 2),
+        (14, None), (14, P + 1)])
+
+
+def test_moe_return_refusals():
+    #       y, dtype, n_rows, H, ldy, row_of, T, k, dx, ldx, stream
+    good = [P, E.DTYPE_FP32, 8, 64, 64, P, 4, 2, P, 64, None]
+    _all_refused(L.entwine_moe_dispatch_bwd, good, [
+        (0, None), (0, P + 2), (1, E.DTYPE_I8), (2, -1), (3, 0), (4, 63), (5, None), (6, -1), (7, 0), (7, 1 << 30), (8, None), (9, 63)])
+    good = [P, E.DTYPE_FP32, 8, 64, 64, P, P, 4, 2, P, 64, None]
+    _all_refused(L.entwine_moe_combine, good, [
+        (0, None), (1, E.DTYPE_I8), (2, -1), (3, 0), (4, 63), (5, None), (5, P + 2), (6, None), (7, -1), (8, 0), (9, None), (10, 63)])
+    assert L.entwine_moe_combine(None, E.DTYPE_FP32, 0, 64, 64, None, None, 0, 2, None, 64, None) == E.OK
+    #       dout, dtype, T, H, ldo, y, n_rows, ldy, w, row_of, k, dy, lddy, dw, stream
+    good = [P, E.DTYPE_FP16, 4, 64, 64, P, 8, 64, P, P, 2, P, 64, P, None]
+    _all_refused(L.entwine_moe_combine_bwd, good, [
+        (0, None), (0, P + 1), (1, E.DTYPE_I8), (2, -1), (3, 0), (4, 63), (5, None), (6, -1), (7, 63), (8, None), (9, None),
+        (10, 0), (11, None), (12, 63), (13, None), (13, P + 2)])
+
+
+def test_binding_refuses_host_tensors():
+    x = torch.zeros(4, 8)
+    for call in (lambda: E.quant_i8(x, x, x), lambda: E.moe_dispatch(x, x, 4, x, x, x), lambda: E.moe_dispatch_bwd(x, x, x),
+                 lambda: E.moe_combine(x, x, x, x), lambda: E.moe_combine_bwd(x, x, x, x, x, x),
+                 lambda: E.quant_i8([[1.0]], x, x)):
+        with pytest.raises(E.EntwineError) as e:
+            call()
+        assert e.value.code == E.ERR_INVALID
+
+
+class _Tensor(torch.Tensor):
+    """A host tensor that says it lies on a device."""
+
+    @staticmethod
+    def on(t, device):
+        t = t.as_subclass(_Tensor)
+        t.place = device
+        return t
+
+    def get_device(self):
+        return self.place
+
+
+def test_binding_refuses_tensors_of_another_device(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    x, q, s = torch.zeros(4, 8), torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4)
+    for devices in ((1, 0, 0), (0, 1, 0), (0, 0, 1)):
+        args = [_Tensor.on(t, d) for t, d in zip((x, q, s), devices)]
+        with pytest.raises(E.EntwineError, match="current CUDA device"):
+            E.quant_i8(*args, stream=0)
+
+
+def test_binding_refuses_what_does_not_fit(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    calls = []
+    for name in E.OP_SYMBOLS:
+        if hasattr(L, name):
+            monkeypatch.setattr(L, name, lambda *a, name=name: calls.append(name) or E.OK)
+    on = lambda t: _Tensor.on(t, 0)  # noqa: E731
+    f = lambda *s: on(torch.zeros(*s))  # noqa: E731
+    i8, i32 = lambda *s: on(torch.zeros(*s, dtype=torch.int8)), lambda *s: on(torch.zeros(*s, dtype=torch.int32))  # noqa: E731
+    bad = [
+        lambda: E.quant_i8(f(4, 8), i8(4, 7), f(4), stream=0),
+        lambda: E.quant_i8(f(4, 8), f(4, 8), f(4), stream=0),
+        lambda: E.quant_i8(f(4, 8), i8(4, 8), f(5), stream=0),
+        lambda: E.quant_i8(f(4, 8, 2), i8(4, 8), f(4), stream=0),
+        lambda: E.quant_i8(on(torch.zeros(8, 4).t()), i8(4, 8), f(4), stream=0),
+        lambda: E.quant_i8(on(torch.zeros(1, 8).expand(4, 8)), i8(4, 8), f(4), stream=0),
+        lambda: E.quant_i8(on(torch.zeros(4, 8, dtype=torch.float64)), i8(4, 8), f(4), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), i32(5, 2), 3, f(8, 8), i32(4), i32(4, 2), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), f(4, 2), 3, f(8, 8), i32(4), i32(4, 2), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), i32(4, 2), 3, f(7, 8), i32(4), i32(4, 2), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), i32(4, 2), 3, i8(8, 8), i32(4), i32(4, 2), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), i32(4, 2), 3, f(8, 8), i32(3), i32(4, 2), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), i32(4, 2), 3, f(8, 8), i32(4), i32(2, 4), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), i32(4, 2), 3, f(8, 8), i32(4), i32(4, 2), x_scale=f(4), stream=0),
+        lambda: E.moe_dispatch(f(4, 8), i32(4, 2), 3, f(8, 8), i32(4), i32(4, 2), x_scale=f(4), row_scale=f(4), stream=0),
+        lambda: E.moe_dispatch_bwd(f(8, 8), i32(4, 2), f(4, 9), stream=0),
+        lambda: E.moe_dispatch_bwd(i8(8, 8), i32(4, 2), i8(4, 8), stream=0),
+        lambda: E.moe_dispatch_bwd(f(8, 8), i32(8), f(4, 8), stream=0),
+        lambda: E.moe_combine(f(8, 8), f(4, 3), i32(4, 2), f(4, 8), stream=0),
+        lambda: E.moe_combine(f(8, 8), i32(4, 2), i32(4, 2), f(4, 8), stream=0),
+        lambda: E.moe_combine(f(8, 8), f(4, 2), i32(4, 2), f(5, 8), stream=0),
+        lambda: E.moe_combine_bwd(f(4, 8), f(8, 9), f(4, 2), i32(4, 2), f(8, 9), f(4, 2), stream=0),
+        lambda: E.moe_combine_bwd(f(4, 8), f(8, 8), f(4, 2), i32(5, 2), f(8, 8), f(4, 2), stream=0),
+        lambda: E.moe_combine_bwd(f(4, 8), f(8, 8), f(4, 2), i32(4, 2), f(7, 8), f(4, 2), stream=0),
+        lambda: E.moe_combine_bwd(f(4, 8), f(8, 8), f(4, 2), i32(4, 2), f(8, 8), f(2, 4), stream=0),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(E.EntwineError) as e:
+            call()
+        assert e.value.code == E.ERR_INVALID, i
+    assert not calls  # nothing reached the library
+    E.quant_i8(on(torch.zeros(4, 16)[:, :8]), i8(4, 8), f(4), stream=0)
+    E.moe_dispatch(f(4, 8), i32(4, 2), 3, f(8, 8), i32(4), i32(4, 2), stream=0)
+    assert calls == ["entwine_quant_i8", "entwine_moe_dispatch"]
