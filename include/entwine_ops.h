@@ -40,6 +40,42 @@ int entwine_quant_i8(const void* x, int dtype, int64_t rows, int64_t cols, int64
                      float* scale, void* stream);
 
 /*
+ * entwine_gemm_i8 - the row-parallel layer's product in 8-bit integers, scaled per token and per output channel:
+ *   C[m][n] = scale_a[m] scale_b[n] sum_k A[m][k] B[n][k] + bias[n]
+ * The int32 sum is exact, the scaling is fp32, C is rounded once.
+ *   A [M, K] int8, B [N, K] int8 (K contiguous, as entwine.h's default layout): both 16-byte aligned with lda and
+ *   ldb multiples of 16 (K itself may be any length: what follows it in a row is not read into the sum)
+ *   scale_a [M], scale_b [N], bias [N] fp32; bias may be NULL
+ *   C [M, N], c_dtype ENTWINE_BF16, ENTWINE_FP16 or ENTWINE_FP32
+ * M = 0 is allowed and does nothing; N >= 1; 1 <= K <= 131071 (the largest sum fits int32).
+ * Errors: ENTWINE_ERR_INVALID, ENTWINE_ERR_CUDA.  Device-side waits are bounded: see entwine_ops_status.
+ */
+int entwine_gemm_i8(const void* A, int64_t lda, const float* scale_a, const void* B, int64_t ldb,
+                    const float* scale_b, const float* bias, void* C, int c_dtype, int64_t ldc, int64_t M, int64_t N,
+                    int64_t K, void* stream);
+
+/*
+ * entwine_gemm_i8_grouped - the same product with a weight matrix per expert, for rows sorted by expert: rows
+ * [offsets[g], offsets[g+1]) of A are multiplied with B[g] and scaled with scale_b[g] (and bias[g]).
+ *   offsets [G+1] int32, device memory, non-decreasing, 0 <= offsets[0], offsets[G] <= M (as entwine_moe_dispatch
+ *   writes them); a bound outside [0, M] is taken as the nearest inside, a decreasing pair as an empty expert
+ *   B [G][N][K], expert_stride elements from one expert's matrix to the next (a multiple of 16)
+ *   scale_b [G][N], bias [G][N] or NULL
+ * Rows of C that belong to no expert are left as they were.  1 <= G <= 1024, G * N < 2^31; the rest as above.
+ */
+int entwine_gemm_i8_grouped(const void* A, int64_t lda, const float* scale_a, const void* B, int64_t ldb,
+                            int64_t expert_stride, const float* scale_b, const float* bias, const int32_t* offsets,
+                            void* C, int c_dtype, int64_t ldc, int64_t M, int64_t N, int64_t K, int64_t G,
+                            void* stream);
+
+/*
+ * entwine_ops_status - synchronises `stream` and returns ENTWINE_ERR_TIMEOUT if a bounded device-side wait of a
+ * product on the current device has run out since the last such query (the call's C is then incomplete), else
+ * ENTWINE_OK.  Not allowed on a capturing stream (ENTWINE_ERR_INVALID).
+ */
+int entwine_ops_status(void* stream);
+
+/*
  * entwine_moe_dispatch - tokens sorted by expert.  ids [T][k] (int32, or int64 with ids64 != 0; contiguous) names
  * the k experts of each token, 0 <= id < E; any other value (-1, say) drops the assignment.  The assignments that
  * are left are ordered by expert, within an expert by t*k + j:

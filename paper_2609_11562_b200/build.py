@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libentwine.so")
 INCLUDE = os.path.join(ROOT, "include")
-SOURCES = ["plan.cc", "entwine_kernels.cu", "quant.cu", "moe.cu"]
+SOURCES = ["plan.cc", "entwine_kernels.cu", "quant.cu", "moe.cu", "gemm_i8.cu"]
 
 
 def _nvcc() -> str:

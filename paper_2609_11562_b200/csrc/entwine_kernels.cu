@@ -1864,23 +1864,6 @@ struct DeviceState {
   __nv_bfloat16 *sA = nullptr, *sB = nullptr, *sPeers = nullptr, *sOut = nullptr, *sSend = nullptr;
 };
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn get_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (fn) return fn;
-  void* p = nullptr;
-  cudaDriverEntryPointQueryResult qres;
-  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) != cudaSuccess ||
-      qres != cudaDriverEntryPointSuccess)
-    return nullptr;
-  fn = reinterpret_cast<EncodeTiledFn>(p);
-  return fn;
-}
-
 // 2-D map over a row-major bf16 matrix [rows, cols] with a (box_rows x box_cols) box;
 // out-of-range elements read as zero (K tails).  `swizzle128` selects the 128-byte swizzle
 // (box_cols must then be 64 elements = 128 bytes).

@@ -71,6 +71,9 @@ _lib.entwine_strerror.restype = ctypes.c_char_p
 # every symbol include/entwine_ops.h declares, with its argument types
 _OP_ARGS = {
     "entwine_quant_i8": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _vp],
+    "entwine_gemm_i8": [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _int, _i64, _i64, _i64, _i64, _vp],
+    "entwine_gemm_i8_grouped": [_vp, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _int, _i64, _i64, _i64, _i64, _i64, _vp],
+    "entwine_ops_status": [_vp],
     "entwine_moe_dispatch": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp],
     "entwine_moe_dispatch_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp],
     "entwine_moe_combine": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp],
@@ -313,6 +316,45 @@ def quant_i8(x, q, scale, stream=None):
     _, _, ldq = _matrix(q, "q", (torch.int8,), x.shape)
     _check(_lib.entwine_quant_i8(x.data_ptr(), _DTYPES[x.dtype], rows, cols, ldx, q.data_ptr(), ldq,
                                  _dense(scale, "scale", (torch.float32,), (rows,)), _stream(stream)), "entwine_quant_i8")
+
+
+def _bias(bias, shape):
+    return None if bias is None else _dense(bias, "bias", (torch.float32,), shape)
+
+
+def gemm_i8(a, scale_a, b, scale_b, out, bias=None, stream=None):
+    """out[m, n] = scale_a[m] scale_b[n] sum_k a[m, k] b[n, k] (+ bias[n]).  a [M, K], b [N, K] int8 with rows on 16-byte
+    boundaries; scale_a [M], scale_b [N], bias [N] fp32; out [M, N] bf16, fp16 or fp32."""
+    M, K, lda = _matrix(a, "a", (torch.int8,))
+    N, Kb, ldb = _matrix(b, "b", (torch.int8,))
+    _need(K == Kb, "a and b must have rows of one length")
+    _, _, ldc = _matrix(out, "out", _FLOATING, (M, N))
+    _check(_lib.entwine_gemm_i8(a.data_ptr(), lda, _dense(scale_a, "scale_a", (torch.float32,), (M,)), b.data_ptr(), ldb,
+                                _dense(scale_b, "scale_b", (torch.float32,), (N,)), _bias(bias, (N,)), out.data_ptr(),
+                                _DTYPES[out.dtype], ldc, M, N, K, _stream(stream)), "entwine_gemm_i8")
+
+
+def gemm_i8_grouped(a, scale_a, b, scale_b, offsets, out, bias=None, stream=None):
+    """Rows [offsets[g], offsets[g+1]) of a times expert g's matrix: b [G, N, K] int8, scale_b and bias [G, N] fp32,
+    offsets [G+1] int32 on the device; the rest as gemm_i8.  Rows of no expert are left as they were."""
+    M, K, lda = _matrix(a, "a", (torch.int8,))
+    _on_device(b, "b")
+    _need(b.dtype == torch.int8 and b.dim() == 3 and b.shape[2] == K and min(b.shape) > 0, "b must be [G, N, K] int8")
+    G, N, _ = b.shape
+    step, ldb, one = b.stride()
+    _need((one == 1 or K == 1) and (N == 1 or ldb >= K) and (G == 1 or step >= (N - 1) * ldb + K),
+          "b must have contiguous rows and matrices that do not overlap")
+    _, _, ldc = _matrix(out, "out", _FLOATING, (M, N))
+    _check(_lib.entwine_gemm_i8_grouped(a.data_ptr(), lda, _dense(scale_a, "scale_a", (torch.float32,), (M,)),
+                                        b.data_ptr(), max(ldb, K), step, _dense(scale_b, "scale_b", (torch.float32,), (G, N)),
+                                        _bias(bias, (G, N)), _dense(offsets, "offsets", (torch.int32,), (G + 1,)),
+                                        out.data_ptr(), _DTYPES[out.dtype], ldc, M, N, K, G, _stream(stream)),
+           "entwine_gemm_i8_grouped")
+
+
+def ops_status(stream=None):
+    """Synchronises the stream; raises EntwineError(ERR_TIMEOUT) if a product's bounded device-side wait has run out."""
+    _check(_lib.entwine_ops_status(_stream(stream)), "entwine_ops_status")
 
 
 def _routing(row_of):

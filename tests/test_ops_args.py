@@ -49,6 +49,21 @@ def test_quant_i8_refusals():
     assert L.entwine_quant_i8(None, E.DTYPE_BF16, 0, 64, 64, None, 64, None, None) == E.OK  # nothing to do
 
 
+def test_gemm_i8_refusals():
+    #       A, lda, scale_a, B, ldb, scale_b, bias, C, c_dtype, ldc, M, N, K, stream
+    good = [P, 64, P, P, 64, P, P, P, E.DTYPE_BF16, 32, 4, 32, 64, None]
+    _all_refused(L.entwine_gemm_i8, good, [
+        (0, None), (0, P + 8), (1, 63), (1, 72), (1, 48), (2, None), (2, P + 1), (3, None), (3, P + 4), (4, 72), (5, None),
+        (6, P + 2), (7, None), (7, P + 1), (8, E.DTYPE_I8), (8, 5), (9, 31), (10, -1), (10, 1 << 31), (11, 0), (11, 1 << 31),
+        (12, 0), (12, 65), (12, 131072)])
+    assert L.entwine_gemm_i8(None, 64, None, None, 64, None, None, None, 0, 32, 0, 32, 64, None) == E.OK
+    #       A, lda, scale_a, B, ldb, expert_stride, scale_b, bias, offsets, C, c_dtype, ldc, M, N, K, G, stream
+    good = [P, 64, P, P, 64, 2048, P, P, P, P, E.DTYPE_FP32, 32, 4, 32, 64, 4, None]
+    _all_refused(L.entwine_gemm_i8_grouped, good, [
+        (0, None), (1, 56), (3, P + 8), (4, 65), (5, 2040), (5, 1024), (6, None), (7, P + 1), (8, None), (8, P + 2), (9, P + 2), (10, 3),
+        (11, 16), (12, -4), (13, 0), (14, 80), (15, 0), (15, 1025), (13, 1 << 30)])
+
+
 def test_moe_dispatch_refusals():
     #       x, dtype, T, H, ldx, x_scale, ids, ids64, k, E, rows, ldr, row_scale, offsets, row_of, stream
     good = [P, E.DTYPE_BF16, 4, 64, 64, P, P, 1, 2, 8, P, 64, P, P, P, None]
@@ -141,6 +156,19 @@ def test_binding_refuses_what_does_not_fit(monkeypatch):
         lambda: E.moe_combine_bwd(f(4, 8), f(8, 8), f(4, 2), i32(5, 2), f(8, 8), f(4, 2), stream=0),
         lambda: E.moe_combine_bwd(f(4, 8), f(8, 8), f(4, 2), i32(4, 2), f(7, 8), f(4, 2), stream=0),
         lambda: E.moe_combine_bwd(f(4, 8), f(8, 8), f(4, 2), i32(4, 2), f(8, 8), f(2, 4), stream=0),
+        lambda: E.gemm_i8(i8(4, 16), f(4), i8(6, 32), f(6), f(4, 6), stream=0),
+        lambda: E.gemm_i8(i8(4, 16), f(4), i8(6, 16), f(6), f(4, 5), stream=0),
+        lambda: E.gemm_i8(i8(4, 16), f(4), i8(6, 16), f(6), i8(4, 6), stream=0),
+        lambda: E.gemm_i8(i8(4, 16), f(3), i8(6, 16), f(6), f(4, 6), stream=0),
+        lambda: E.gemm_i8(i8(4, 16), f(4), i8(6, 16), f(4), f(4, 6), stream=0),
+        lambda: E.gemm_i8(i8(4, 16), f(4), i8(6, 16), f(6), f(4, 6), bias=f(4), stream=0),
+        lambda: E.gemm_i8(f(4, 16), f(4), i8(6, 16), f(6), f(4, 6), stream=0),
+        lambda: E.gemm_i8(on(i8(16, 4).t()), f(4), i8(6, 16), f(6), f(4, 6), stream=0),
+        lambda: E.gemm_i8_grouped(i8(4, 16), f(4), i8(6, 16), f(6), i32(3), f(4, 6), stream=0),
+        lambda: E.gemm_i8_grouped(i8(4, 16), f(4), i8(2, 6, 16), f(2, 6), i32(2), f(4, 6), stream=0),
+        lambda: E.gemm_i8_grouped(i8(4, 16), f(4), i8(2, 6, 16), f(6, 2), i32(3), f(4, 6), stream=0),
+        lambda: E.gemm_i8_grouped(i8(4, 16), f(4), i8(2, 6, 32), f(2, 6), i32(3), f(4, 6), stream=0),
+        lambda: E.gemm_i8_grouped(i8(4, 16), f(4), on(torch.zeros(1, 6, 16, dtype=torch.int8).expand(2, 6, 16)), f(2, 6), i32(3), f(4, 6), stream=0),
     ]
     for i, call in enumerate(bad):
         with pytest.raises(E.EntwineError) as e:
