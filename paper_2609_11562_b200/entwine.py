@@ -113,7 +113,8 @@ def _ptr(t):
 
 def _stream(s):
     if s is None:
-        return torch.cuda.current_stream().cuda_stream
+        # the handle alone: building a Stream object takes 3 us, as long as a short kernel
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -273,82 +274,105 @@ _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16, torch.float32:
 _FLOATING = (torch.bfloat16, torch.float16, torch.float32)
 
 
+_I8, _I32, _FP32, _IDS = (torch.int8,), (torch.int32,), (torch.float32,), (torch.int32, torch.int64)
+_ANY = tuple(_DTYPES)
+
+
 def _refuse(what):
     raise EntwineError(ERR_INVALID, what)
 
 
-def _need(ok, what):
-    if not ok:
-        _refuse(what)
-
-
-def _on_device(t, name):
-    if not isinstance(t, torch.Tensor) or t.get_device() < 0 or t.get_device() != torch.cuda.current_device():
+def _device(t, name):
+    """The current device, on which this first argument has to lie; the others are compared with it."""
+    dev = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if dev < 0 or dev != torch.cuda.current_device():
         _refuse(f"{name} must be a tensor on the current CUDA device")
+    return dev
 
 
-def _matrix(t, name, dtypes, shape=None):
-    """A matrix whose rows are contiguous: (rows, cols, distance between two rows)."""
-    _on_device(t, name)
-    if t.dtype not in dtypes or t.dim() != 2 or (shape is not None and t.shape != shape):
-        _refuse(f"{name} must be a matrix{'' if shape is None else f' {tuple(shape)}'} of {' or '.join(map(str, dtypes))}, "
-                f"not {tuple(t.shape)} of {t.dtype}")
-    rows, cols = t.shape
-    ld, step = t.stride()
-    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
-        _refuse(f"{name} must have contiguous rows that do not overlap (strides {t.stride()})")
-    return rows, cols, max(ld, cols)
+def _wrong(t, name, dtypes, dev, what):
+    """Refuses an argument, saying what is wrong with it."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        _refuse(f"{name} must be a tensor on the current CUDA device")
+    if t.dtype not in dtypes:
+        _refuse(f"{name} must be of {' or '.join(map(str, dtypes))}, not {t.dtype}")
+    _refuse(f"{name} must be {what}, not {tuple(t.shape)} with strides {t.stride()}")
 
 
-def _dense(t, name, dtypes, shape):
+# (A short kernel takes as long as these checks: they read each property once and leave the wording to _wrong.)
+def _matrix(t, name, dtypes, dev):
+    """A matrix whose rows are contiguous and do not overlap: (rows, cols, distance between two rows)."""
+    try:
+        if t.get_device() == dev and t.dtype in dtypes:
+            rows, cols = t.shape
+            ld, step = t.stride()
+            if (step == 1 or cols <= 1) and (ld >= cols or rows <= 1):
+                return rows, cols, ld if ld > cols else cols
+    except (AttributeError, ValueError):
+        pass
+    _wrong(t, name, dtypes, dev, "a matrix of contiguous rows that do not overlap")
+
+
+def _result(t, name, dtypes, dev, rows, cols):
+    """The same for a matrix of known size: the distance between two rows."""
+    r, c, ld = _matrix(t, name, dtypes, dev)
+    if r != rows or c != cols:
+        _wrong(t, name, dtypes, dev, f"{(rows, cols)}")
+    return ld
+
+
+def _dense(t, name, dtypes, dev, *shape):
     """A contiguous tensor of this shape: its address."""
-    _on_device(t, name)
-    if t.dtype not in dtypes or t.shape != shape or not t.is_contiguous():
-        _refuse(f"{name} must be contiguous, {tuple(shape)} of {' or '.join(map(str, dtypes))}, "
-                f"not {tuple(t.shape)} of {t.dtype}")
-    return t.data_ptr()
+    try:
+        if t.get_device() == dev and t.dtype in dtypes and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _wrong(t, name, dtypes, dev, f"contiguous and {shape}")
 
 
 def quant_i8(x, q, scale, stream=None):
     """Rows to int8 with a scale each: scale = amax / 127, q = rint(127 x / amax), ties to even.
     x [M, K] bf16, fp16 or fp32; q [M, K] int8; scale [M] fp32."""
-    rows, cols, ldx = _matrix(x, "x", _FLOATING)
-    _, _, ldq = _matrix(q, "q", (torch.int8,), x.shape)
+    dev = _device(x, "x")
+    rows, cols, ldx = _matrix(x, "x", _FLOATING, dev)
+    ldq = _result(q, "q", _I8, dev, rows, cols)
     _check(_lib.entwine_quant_i8(x.data_ptr(), _DTYPES[x.dtype], rows, cols, ldx, q.data_ptr(), ldq,
-                                 _dense(scale, "scale", (torch.float32,), (rows,)), _stream(stream)), "entwine_quant_i8")
-
-
-def _bias(bias, shape):
-    return None if bias is None else _dense(bias, "bias", (torch.float32,), shape)
+                                 _dense(scale, "scale", _FP32, dev, rows), _stream(stream)), "entwine_quant_i8")
 
 
 def gemm_i8(a, scale_a, b, scale_b, out, bias=None, stream=None):
     """out[m, n] = scale_a[m] scale_b[n] sum_k a[m, k] b[n, k] (+ bias[n]).  a [M, K], b [N, K] int8 with rows on 16-byte
     boundaries; scale_a [M], scale_b [N], bias [N] fp32; out [M, N] bf16, fp16 or fp32."""
-    M, K, lda = _matrix(a, "a", (torch.int8,))
-    N, Kb, ldb = _matrix(b, "b", (torch.int8,))
-    _need(K == Kb, "a and b must have rows of one length")
-    _, _, ldc = _matrix(out, "out", _FLOATING, (M, N))
-    _check(_lib.entwine_gemm_i8(a.data_ptr(), lda, _dense(scale_a, "scale_a", (torch.float32,), (M,)), b.data_ptr(), ldb,
-                                _dense(scale_b, "scale_b", (torch.float32,), (N,)), _bias(bias, (N,)), out.data_ptr(),
+    dev = _device(a, "a")
+    M, K, lda = _matrix(a, "a", _I8, dev)
+    N, Kb, ldb = _matrix(b, "b", _I8, dev)
+    if K != Kb:
+        _refuse("a and b must have rows of one length")
+    ldc = _result(out, "out", _FLOATING, dev, M, N)
+    _check(_lib.entwine_gemm_i8(a.data_ptr(), lda, _dense(scale_a, "scale_a", _FP32, dev, M), b.data_ptr(), ldb,
+                                _dense(scale_b, "scale_b", _FP32, dev, N),
+                                None if bias is None else _dense(bias, "bias", _FP32, dev, N), out.data_ptr(),
                                 _DTYPES[out.dtype], ldc, M, N, K, _stream(stream)), "entwine_gemm_i8")
 
 
 def gemm_i8_grouped(a, scale_a, b, scale_b, offsets, out, bias=None, stream=None):
     """Rows [offsets[g], offsets[g+1]) of a times expert g's matrix: b [G, N, K] int8, scale_b and bias [G, N] fp32,
     offsets [G+1] int32 on the device; the rest as gemm_i8.  Rows of no expert are left as they were."""
-    M, K, lda = _matrix(a, "a", (torch.int8,))
-    _on_device(b, "b")
-    _need(b.dtype == torch.int8 and b.dim() == 3 and b.shape[2] == K and min(b.shape) > 0, "b must be [G, N, K] int8")
+    dev = _device(a, "a")
+    M, K, lda = _matrix(a, "a", _I8, dev)
+    if not isinstance(b, torch.Tensor) or b.dim() != 3 or b.get_device() != dev or b.dtype != torch.int8 or b.shape[2] != K:
+        _wrong(b, "b", _I8, dev, f"[G, N, {K}]")
     G, N, _ = b.shape
     step, ldb, one = b.stride()
-    _need((one == 1 or K == 1) and (N == 1 or ldb >= K) and (G == 1 or step >= (N - 1) * ldb + K),
-          "b must have contiguous rows and matrices that do not overlap")
-    _, _, ldc = _matrix(out, "out", _FLOATING, (M, N))
-    _check(_lib.entwine_gemm_i8_grouped(a.data_ptr(), lda, _dense(scale_a, "scale_a", (torch.float32,), (M,)),
-                                        b.data_ptr(), max(ldb, K), step, _dense(scale_b, "scale_b", (torch.float32,), (G, N)),
-                                        _bias(bias, (G, N)), _dense(offsets, "offsets", (torch.int32,), (G + 1,)),
-                                        out.data_ptr(), _DTYPES[out.dtype], ldc, M, N, K, G, _stream(stream)),
+    if (one != 1 and K > 1) or (ldb < K and N > 1) or (step < (N - 1) * ldb + K and G > 1):
+        _wrong(b, "b", _I8, dev, "matrices of contiguous rows that do not overlap")
+    ldc = _result(out, "out", _FLOATING, dev, M, N)
+    _check(_lib.entwine_gemm_i8_grouped(a.data_ptr(), lda, _dense(scale_a, "scale_a", _FP32, dev, M), b.data_ptr(),
+                                        ldb if ldb > K else K, step, _dense(scale_b, "scale_b", _FP32, dev, G, N),
+                                        None if bias is None else _dense(bias, "bias", _FP32, dev, G, N),
+                                        _dense(offsets, "offsets", _I32, dev, G + 1), out.data_ptr(),
+                                        _DTYPES[out.dtype], ldc, M, N, K, G, _stream(stream)),
            "entwine_gemm_i8_grouped")
 
 
@@ -357,63 +381,63 @@ def ops_status(stream=None):
     _check(_lib.entwine_ops_status(_stream(stream)), "entwine_ops_status")
 
 
-def _routing(row_of):
-    _on_device(row_of, "row_of")
-    _need(row_of.dim() == 2, "row_of must be [T, k]")
-    return row_of.shape[0], row_of.shape[1], _dense(row_of, "row_of", (torch.int32,), row_of.shape)
+def _assignments(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        _refuse(f"{name} must be a tensor [T, k]")
+    return t.shape
 
 
 def moe_dispatch(x, ids, n_experts, rows, offsets, row_of, x_scale=None, row_scale=None, stream=None):
     """Tokens sorted by expert.  x [T, H] bf16, fp16, fp32 or int8; ids [T, k] int32 or int64, an id outside
     [0, n_experts) drops the assignment; rows [T*k, H]; offsets [n_experts+1] int32; row_of [T, k] int32 (-1:
     dropped); x_scale [T] -> row_scale [T*k] fp32, both or neither.  Rows behind offsets[-1] are left as they were."""
-    T, H, ldx = _matrix(x, "x", tuple(_DTYPES))
-    _on_device(ids, "ids")
-    _need(ids.dim() == 2 and ids.shape[0] == T, "ids must be [T, k]")
-    k = ids.shape[1]
-    _, _, ldr = _matrix(rows, "rows", (x.dtype,), (T * k, H))
-    _need((x_scale is None) == (row_scale is None), "x_scale and row_scale go together")
-    if x_scale is not None:
-        x_scale, row_scale = (_dense(x_scale, "x_scale", (torch.float32,), (T,)),
-                              _dense(row_scale, "row_scale", (torch.float32,), (T * k,)))
+    dev = _device(x, "x")
+    T, H, ldx = _matrix(x, "x", _ANY, dev)
+    _, k = _assignments(ids, "ids")
+    ldr = _result(rows, "rows", (x.dtype,), dev, T * k, H)
+    if x_scale is not None or row_scale is not None:
+        x_scale, row_scale = _dense(x_scale, "x_scale", _FP32, dev, T), _dense(row_scale, "row_scale", _FP32, dev, T * k)
     _check(_lib.entwine_moe_dispatch(x.data_ptr(), _DTYPES[x.dtype], T, H, ldx, x_scale,
-                                     _dense(ids, "ids", (torch.int32, torch.int64), (T, k)), ids.dtype == torch.int64,
-                                     k, int(n_experts), rows.data_ptr(), ldr, row_scale,
-                                     _dense(offsets, "offsets", (torch.int32,), (int(n_experts) + 1,)),
-                                     _dense(row_of, "row_of", (torch.int32,), (T, k)), _stream(stream)),
-           "entwine_moe_dispatch")
+                                     _dense(ids, "ids", _IDS, dev, T, k), ids.dtype == torch.int64, k, n_experts,
+                                     rows.data_ptr(), ldr, row_scale,
+                                     _dense(offsets, "offsets", _I32, dev, n_experts + 1),
+                                     _dense(row_of, "row_of", _I32, dev, T, k), _stream(stream)), "entwine_moe_dispatch")
 
 
 def moe_dispatch_bwd(d_rows, row_of, dx, stream=None):
     """Gradient of moe_dispatch: dx[t] = sum_j d_rows[row_of[t, j]] in fp32, j ascending.  d_rows [n, H], dx [T, H]."""
-    n, H, ldr = _matrix(d_rows, "d_rows", _FLOATING)
-    T, k, at = _routing(row_of)
-    _, _, ldx = _matrix(dx, "dx", (d_rows.dtype,), (T, H))
-    _check(_lib.entwine_moe_dispatch_bwd(d_rows.data_ptr(), _DTYPES[d_rows.dtype], n, H, ldr, at, T, k, dx.data_ptr(),
-                                         ldx, _stream(stream)), "entwine_moe_dispatch_bwd")
+    dev = _device(d_rows, "d_rows")
+    n, H, ldr = _matrix(d_rows, "d_rows", _FLOATING, dev)
+    T, k = _assignments(row_of, "row_of")
+    ldx = _result(dx, "dx", (d_rows.dtype,), dev, T, H)
+    _check(_lib.entwine_moe_dispatch_bwd(d_rows.data_ptr(), _DTYPES[d_rows.dtype], n, H, ldr,
+                                         _dense(row_of, "row_of", _I32, dev, T, k), T, k, dx.data_ptr(), ldx,
+                                         _stream(stream)), "entwine_moe_dispatch_bwd")
 
 
 def moe_combine(y, weights, row_of, out, stream=None):
     """out[t] = sum_j weights[t, j] y[row_of[t, j]] in fp32, j ascending.  y [n, H], out [T, H] of one type, weights
     [T, k] fp32."""
-    n, H, ldy = _matrix(y, "y", _FLOATING)
-    T, k, at = _routing(row_of)
-    _, _, ldo = _matrix(out, "out", (y.dtype,), (T, H))
-    _check(_lib.entwine_moe_combine(y.data_ptr(), _DTYPES[y.dtype], n, H, ldy,
-                                    _dense(weights, "weights", (torch.float32,), (T, k)), at, T, k, out.data_ptr(),
-                                    ldo, _stream(stream)), "entwine_moe_combine")
+    dev = _device(y, "y")
+    n, H, ldy = _matrix(y, "y", _FLOATING, dev)
+    T, k = _assignments(row_of, "row_of")
+    ldo = _result(out, "out", (y.dtype,), dev, T, H)
+    _check(_lib.entwine_moe_combine(y.data_ptr(), _DTYPES[y.dtype], n, H, ldy, _dense(weights, "weights", _FP32, dev, T, k),
+                                    _dense(row_of, "row_of", _I32, dev, T, k), T, k, out.data_ptr(), ldo,
+                                    _stream(stream)), "entwine_moe_combine")
 
 
 def moe_combine_bwd(dout, y, weights, row_of, dy, dw, stream=None):
     """Gradients of moe_combine: dy[row_of[t, j]] = weights[t, j] dout[t], dw[t, j] = <dout[t], y[row_of[t, j]]>
     (fp32; 0 where dropped).  Rows of dy that no assignment names are left as they were."""
-    T, H, ldo = _matrix(dout, "dout", _FLOATING)
-    _, k, at = _routing(row_of)
-    _need(row_of.shape[0] == T, "row_of must be [T, k]")
-    n, _, ldy = _matrix(y, "y", (dout.dtype,))
-    _need(y.shape[1] == H, "y must have rows as long as dout's")
-    _, _, lddy = _matrix(dy, "dy", (dout.dtype,), (n, H))
+    dev = _device(dout, "dout")
+    T, H, ldo = _matrix(dout, "dout", _FLOATING, dev)
+    _, k = _assignments(row_of, "row_of")
+    n, Hy, ldy = _matrix(y, "y", (dout.dtype,), dev)
+    if Hy != H:
+        _refuse("y must have rows as long as dout's")
+    lddy = _result(dy, "dy", (dout.dtype,), dev, n, H)
     _check(_lib.entwine_moe_combine_bwd(dout.data_ptr(), _DTYPES[dout.dtype], T, H, ldo, y.data_ptr(), n, ldy,
-                                        _dense(weights, "weights", (torch.float32,), (T, k)), at, k, dy.data_ptr(),
-                                        lddy, _dense(dw, "dw", (torch.float32,), (T, k)), _stream(stream)),
-           "entwine_moe_combine_bwd")
+                                        _dense(weights, "weights", _FP32, dev, T, k),
+                                        _dense(row_of, "row_of", _I32, dev, T, k), k, dy.data_ptr(), lddy,
+                                        _dense(dw, "dw", _FP32, dev, T, k), _stream(stream)), "entwine_moe_combine_bwd")
