@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "ops_common.cuh"
+#include "sm100.cuh"
 
 namespace entwine {
 namespace {
@@ -9,128 +10,280 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortCtas = 8;      // CTAs of the sort: one cluster
+constexpr int kIdsAhead = 8;      // loads of assignments in flight per lane
 constexpr int kMaxExperts = 1024;
+constexpr int kChunk = 8;         // assignments of a token placed and written together
+// Assignments of a token read together by the sums.  Four loads of 16 bytes per thread at four or five CTAs per SM
+// reach 94-100 % of the copy rate; eight cost the registers of half of the CTAs (8192 tokens of 4096 bf16, eight
+// experts each: forward 94 us with four, 116 with eight; backward 175, 344).
+constexpr int kReads = 4;
 constexpr int64_t kMaxGrid = 2147483647;
+// up to this many assignments every token's CTA ranks its own ones against all others
+constexpr int64_t kSmallRouting = 2048;
+constexpr int64_t kFewTokens = 1024;  // below this a token's row is spread over several CTAs
 
-// Expert of assignment i, or E where it is dropped.
+// Expert of an assignment, or E where it is dropped.
 template <typename Id>
-__device__ __forceinline__ int expert_of(const Id* ids, int64_t i, int E) {
-  const Id e = ids[i];
+__device__ __forceinline__ int expert_of(Id e, int E) {
   return e >= 0 && e < Id(E) ? int(e) : E;
 }
 
-// Stable counting sort of n assignments by expert, one CTA.  Every warp owns a run of consecutive assignments and a
-// row of counts; the counts become start positions by a scan over warps and experts; then each warp walks its run
-// again, 32 assignments at a time, ranking equal experts among its lanes by a vote.
+// Inclusive scan over the lanes of a warp.
+__device__ __forceinline__ int32_t warp_scan(int32_t v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int32_t u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+
+// Stable counting sort of n assignments by expert, one cluster of eight CTAs.  Every warp owns a run of consecutive
+// assignments and a row of counts in shared memory; the counts become start positions by a scan over a CTA's warps,
+// over the CTAs (whose totals are read through distributed shared memory) and over the experts; then each warp walks
+// its run again, 32 assignments at a time, ranking equal experts among its lanes by a vote.  Bound by the latency of
+// the two walks: the 131072 assignments of 16384 tokens are 16 steps of 32 for each of the 256 warps.
 template <typename Id>
 __global__ void __launch_bounds__(kSortThreads) moe_sort_kernel(const Id* ids, int64_t n, int E, int32_t* offsets,
                                                                 int32_t* row_of) {
-  extern __shared__ int32_t counts[];  // [kSortWarps][E]
+  extern __shared__ int32_t counts[];  // [kSortWarps][E], then the CTA's totals [E]
   __shared__ int32_t warp_total[kSortWarps];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int64_t run = (n + kSortThreads - 1) / kSortThreads * 32;
-  const int64_t first = min(int64_t(warp) * run, n), last = min(first + run, n);
+  const int cta = int(cluster_ctarank()), warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int64_t walkers = kSortCtas * kSortWarps;
+  const int64_t run = (n + walkers * 32 - 1) / (walkers * 32) * 32;
+  const int64_t first = min((int64_t(cta) * kSortWarps + warp) * run, n), last = min(first + run, n);
   int32_t* mine = counts + warp * E;
+  int32_t* totals = counts + kSortWarps * E;
   for (int i = threadIdx.x; i < kSortWarps * E; i += kSortThreads) counts[i] = 0;
   __syncthreads();
-  for (int64_t i0 = first; i0 < last; i0 += 32) {
-    const int64_t i = i0 + lane;
-    const int e = i < last ? expert_of(ids, i, E) : E;
-    const unsigned same = __match_any_sync(0xffffffffu, e);
-    if (e < E && lane == __ffs(same) - 1) mine[e] += __popc(same);
-    __syncwarp();
+  for (int64_t i0 = first; i0 < last; i0 += 32 * kIdsAhead) {
+    Id id[kIdsAhead];
+#pragma unroll
+    for (int u = 0; u < kIdsAhead; ++u) id[u] = i0 + 32 * u + lane < last ? ids[i0 + 32 * u + lane] : Id(-1);
+#pragma unroll
+    for (int u = 0; u < kIdsAhead; ++u) {
+      if (i0 + 32 * u >= last) break;
+      const int e = expert_of(id[u], E);
+      const unsigned same = __match_any_sync(0xffffffffu, e);
+      if (e < E && lane == __ffs(same) - 1) mine[e] += __popc(same);
+      __syncwarp();
+    }
   }
   __syncthreads();
   // thread e: the counts of expert e become the starts of the warps' runs inside its rows
   const int e = threadIdx.x;
   int32_t total = 0;
-  if (e < E)
+  if (e < E) {
     for (int w = 0; w < kSortWarps; ++w) {
       const int32_t c = counts[w * E + e];
       counts[w * E + e] = total;
       total += c;
     }
-  int32_t sum = total;  // inclusive scan over the experts
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int32_t v = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += v;
+    totals[e] = total;
   }
+  __syncwarp();
+  cluster_sync_all();
+  int32_t before = 0;  // of this expert, in the CTAs before this one
+  total = 0;
+  if (e < E) {
+    int32_t t[kSortCtas];
+#pragma unroll
+    for (int c = 0; c < kSortCtas; ++c) t[c] = ld_cluster(map_to_cta(smem_u32(totals + e), c));
+#pragma unroll
+    for (int c = 0; c < kSortCtas; ++c) {
+      if (c < cta) before += t[c];
+      total += t[c];
+    }
+  }
+  const int32_t sum = warp_scan(total, lane);
   if (lane == 31) warp_total[warp] = sum;
   __syncthreads();
-  int32_t before = 0;
-  for (int w = 0; w < warp; ++w) before += warp_total[w];
-  const int32_t start = before + sum - total;
+  int32_t start = sum - total;
+  for (int w = 0; w < warp; ++w) start += warp_total[w];
   if (e < E) {
-    offsets[e] = start;
-    if (e == E - 1) offsets[E] = start + total;
-    for (int w = 0; w < kSortWarps; ++w) counts[w * E + e] += start;
+    if (cta == 0) {
+      offsets[e] = start;
+      if (e == E - 1) offsets[E] = start + total;
+    }
+    for (int w = 0; w < kSortWarps; ++w) counts[w * E + e] += start + before;
   }
-  __syncthreads();
-  for (int64_t i0 = first; i0 < last; i0 += 32) {
-    const int64_t i = i0 + lane;
-    const int x = i < last ? expert_of(ids, i, E) : E;
-    const unsigned same = __match_any_sync(0xffffffffu, x);
-    const int32_t base = x < E ? mine[x] : 0;
-    __syncwarp();
-    if (x < E && lane == __ffs(same) - 1) mine[x] = base + __popc(same);
-    __syncwarp();
-    if (i < last) row_of[i] = x < E ? base + __popc(same & ((1u << lane) - 1)) : -1;
+  __syncwarp();
+  cluster_sync_all();  // (also: no CTA leaves while its totals are read)
+  for (int64_t i0 = first; i0 < last; i0 += 32 * kIdsAhead) {
+    Id id[kIdsAhead];
+#pragma unroll
+    for (int u = 0; u < kIdsAhead; ++u) id[u] = i0 + 32 * u + lane < last ? ids[i0 + 32 * u + lane] : Id(-1);
+#pragma unroll
+    for (int u = 0; u < kIdsAhead; ++u) {
+      const int64_t i = i0 + 32 * u + lane;
+      if (i0 + 32 * u >= last) break;
+      const int x = expert_of(id[u], E);
+      const unsigned same = __match_any_sync(0xffffffffu, x);
+      const int32_t base = x < E ? mine[x] : 0;
+      __syncwarp();
+      if (x < E && lane == __ffs(same) - 1) mine[x] = base + __popc(same);
+      __syncwarp();
+      if (i < last) row_of[i] = x < E ? base + __popc(same & ((1u << lane) - 1)) : -1;
+    }
   }
 }
 
-// One CTA per token: its row is read once and written to each of its places.
+// A token's row read once and written to each of its places, `to` in shared or global memory.
+template <typename T, int V>
+__device__ __forceinline__ void move_row(const T* src, int64_t H, const int32_t* to, int64_t k, T* rows, int64_t ldr) {
+  using P = Piece<T, V>;
+  const int64_t pieces = H / V;
+  for (int64_t j0 = 0; j0 < k; j0 += kChunk) {
+    int32_t r[kChunk];
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) r[j] = j0 + j < k ? to[j0 + j] : -1;
+    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
+      const P v = reinterpret_cast<const P*>(src)[i];
+#pragma unroll
+      for (int j = 0; j < kChunk; ++j)
+        if (r[j] >= 0) reinterpret_cast<P*>(rows + r[j] * ldr)[i] = v;
+    }
+    for (int64_t i = pieces * V + threadIdx.x; i < H; i += kThreads)
+#pragma unroll
+      for (int j = 0; j < kChunk; ++j)
+        if (r[j] >= 0) rows[r[j] * ldr + i] = src[i];
+  }
+}
+
+// One CTA per token, behind the sort.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) moe_move_kernel(const T* x, int64_t H, int64_t ldx, const float* x_scale,
                                                             const int32_t* row_of, int64_t k, T* rows, int64_t ldr,
                                                             float* row_scale) {
-  using P = Piece<T, V>;
-  const int64_t t = blockIdx.x, pieces = H / V;
-  const T* src = x + t * ldx;
+  const int64_t t = blockIdx.x;
   const int32_t* to = row_of + t * k;
-  for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
-    const P v = reinterpret_cast<const P*>(src)[i];
-    for (int64_t j = 0; j < k; ++j)
-      if (to[j] >= 0) reinterpret_cast<P*>(rows + to[j] * ldr)[i] = v;
-  }
-  for (int64_t i = pieces * V + threadIdx.x; i < H; i += kThreads) {
-    const T v = src[i];
-    for (int64_t j = 0; j < k; ++j)
-      if (to[j] >= 0) rows[to[j] * ldr + i] = v;
-  }
+  move_row<T, V>(x + t * ldx, H, to, k, rows, ldr);
   if (x_scale)
     for (int64_t j = threadIdx.x; j < k; j += kThreads)
       if (to[j] >= 0) row_scale[to[j]] = x_scale[t];
 }
 
-// One CTA per token: the weighted sum of its rows (w null: weights of one).
-template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) moe_combine_kernel(const T* y, int64_t n_rows, int64_t H, int64_t ldy,
-                                                               const float* w, const int32_t* row_of, int64_t k,
-                                                               T* out, int64_t ldo) {
+// Few assignments: sort and move in one launch, a CTA per token.  The row of an assignment is the number of
+// assignments to lower experts plus that of earlier ones to its own, counted over all n by the token's CTA; the last
+// CTA of the grid counts the experts' rows for the offsets.
+template <typename T, int V, typename Id>
+__global__ void __launch_bounds__(kThreads) moe_dispatch_small_kernel(const T* x, int64_t T_, int64_t H, int64_t ldx,
+                                                                      const float* x_scale, const Id* ids, int k, int E,
+                                                                      T* rows, int64_t ldr, float* row_scale,
+                                                                      int32_t* offsets, int32_t* row_of) {
+  __shared__ int32_t all[kSmallRouting];
+  __shared__ int32_t table[kMaxExperts];  // the last CTA: rows of each expert; the others: rows of the assignments
+  const int n = int(T_) * k, lane = threadIdx.x % 32, t = blockIdx.x;
+  for (int i = threadIdx.x; i < n; i += kThreads) all[i] = expert_of(ids[i], E);
+  if (t == T_) {
+    __shared__ int32_t warp_total[kThreads / 32];
+    constexpr int kEach = kMaxExperts / kThreads;
+    for (int e = threadIdx.x; e < kMaxExperts; e += kThreads) table[e] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads)
+      if (all[i] < E) atomicAdd(&table[all[i]], 1);  // counts: no order to depend on
+    __syncthreads();
+    int32_t c[kEach], total = 0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) total += c[u] = table[threadIdx.x * kEach + u];
+    const int32_t sum = warp_scan(total, lane);
+    if (lane == 31) warp_total[threadIdx.x / 32] = sum;
+    __syncthreads();
+    int32_t start = sum - total;
+    for (int w = 0; w < int(threadIdx.x) / 32; ++w) start += warp_total[w];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int e = threadIdx.x * kEach + u;
+      if (e <= E) offsets[e] = start;
+      start += c[u];
+    }
+    if (E == kMaxExperts && threadIdx.x == kThreads - 1) offsets[E] = start;
+    return;
+  }
+  __shared__ int32_t part[kThreads / 32][kChunk];
+  __syncthreads();
+  for (int j0 = 0; j0 < k; j0 += kChunk) {
+    int32_t e[kChunk], count[kChunk];
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) {
+      e[j] = j0 + j < k ? all[t * k + j0 + j] : E;
+      count[j] = 0;
+    }
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const int32_t o = all[i];
+#pragma unroll
+      for (int j = 0; j < kChunk; ++j) count[j] += o < e[j] + (i < t * k + j0 + j ? 1 : 0) ? 1 : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) {
+      const int32_t c = __reduce_add_sync(0xffffffffu, count[j]);
+      if (lane == j) part[threadIdx.x / 32][j] = c;
+    }
+    __syncthreads();
+    if (threadIdx.x < kChunk && j0 + int(threadIdx.x) < k) {
+      const int j = j0 + threadIdx.x;
+      int32_t r = 0;
+#pragma unroll
+      for (int w = 0; w < kThreads / 32; ++w) r += part[w][threadIdx.x];
+      if (all[t * k + j] >= E) r = -1;
+      row_of[int64_t(t) * k + j] = r;
+      part[0][threadIdx.x] = r;
+      if (r >= 0 && x_scale) row_scale[r] = x_scale[t];
+    }
+    __syncthreads();
+    move_row<T, V>(x + t * ldx, H, part[0], min(k - j0, kChunk), rows, ldr);
+    __syncthreads();
+  }
+}
+
+// The weighted sum of a token's rows (w null: weights of one).  Bound by reading the rows: J assignments of U pieces
+// of the token are in flight together, and a row is spread over several CTAs where there are few tokens.
+template <typename T, int V, int J, int U>
+__global__ void __launch_bounds__(kThreads, 5) moe_combine_kernel(const T* y, int64_t n_rows, int64_t H, int64_t ldy,
+                                                                   const float* w, const int32_t* row_of, int64_t k,
+                                                                   T* out, int64_t ldo) {
   using P = Piece<T, V>;
-  const int64_t t = blockIdx.x, pieces = H / V;
+  const int64_t t = blockIdx.x, pieces = H / V, step = int64_t(gridDim.y) * blockDim.x;
   const int32_t* at = row_of + t * k;
   const float* wt = w ? w + t * k : nullptr;
   T* dst = out + t * ldo;
-  for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
-    float acc[V];
+  const int64_t first = int64_t(blockIdx.y) * blockDim.x + threadIdx.x;
+  for (int64_t i0 = first; i0 < pieces; i0 += U * step) {
+    float acc[U][V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-    for (int64_t j = 0; j < k; ++j) {
-      const int64_t r = at[j];
-      if (r < 0 || r >= n_rows) continue;
-      const P v = reinterpret_cast<const P*>(y + r * ldy)[i];
-      const float f = wt ? wt[j] : 1.0f;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] = fmaf(f, Elem<T>::up(v.e[e]), acc[e]);
+      for (int e = 0; e < V; ++e) acc[u][e] = 0.0f;
+    for (int64_t j0 = 0; j0 < k; j0 += J) {
+      P v[J][U];
+      float f[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int64_t r = j0 + j < k ? at[j0 + j] : -1;
+        const bool there = r >= 0 && r < n_rows;
+        f[j] = !there ? 0.0f : wt ? wt[j0 + j] : 1.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t i = i0 + u * step;
+          v[j][u] = load_if<T, V>(y + r * ldy + i * V, there && i < pieces);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float ye[V];
+          unpack<T, V>(v[j][u], ye);
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[u][e] = fmaf(f[j], ye[e], acc[u][e]);
+        }
     }
-    P o;
 #pragma unroll
-    for (int e = 0; e < V; ++e) o.e[e] = Elem<T>::down(acc[e]);
-    reinterpret_cast<P*>(dst)[i] = o;
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * step < pieces) reinterpret_cast<P*>(dst)[i0 + u * step] = pack<T, V>(acc[u]);
   }
-  for (int64_t i = pieces * V + threadIdx.x; i < H; i += kThreads) {
+  for (int64_t i = pieces * V + first; i < H; i += step) {
     float acc = 0.0f;
     for (int64_t j = 0; j < k; ++j) {
       const int64_t r = at[j];
@@ -140,49 +293,67 @@ __global__ void __launch_bounds__(kThreads) moe_combine_kernel(const T* y, int64
   }
 }
 
-// One CTA per token: dy of its rows, and the dot products that are the gradients of its weights.
+// One CTA per token: dy of its rows, and the dot products that are the gradients of its weights.  Bound by reading
+// y and writing dy; up to four assignments are handled in one walk over the token's gradient.
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) moe_combine_bwd_kernel(const T* dout, int64_t H, int64_t ldo, const T* y,
+__global__ void __launch_bounds__(kThreads, 4) moe_combine_bwd_kernel(const T* dout, int64_t H, int64_t ldo, const T* y,
                                                                    int64_t n_rows, int64_t ldy, const float* w,
                                                                    const int32_t* row_of, int64_t k, T* dy,
                                                                    int64_t lddy, float* dw) {
   using P = Piece<T, V>;
-  __shared__ float part[kThreads / 32];
+  __shared__ float part[kThreads / 32][kReads];
   const int64_t t = blockIdx.x, pieces = H / V;
   const T* g = dout + t * ldo;
-  for (int64_t j = 0; j < k; ++j) {
-    const int64_t r = row_of[t * k + j];
-    if (r < 0 || r >= n_rows) {
-      if (threadIdx.x == 0) dw[t * k + j] = 0.0f;
-      continue;
-    }
-    const float f = w[t * k + j];
-    const T* yr = y + r * ldy;
-    T* dr = dy + r * lddy;
-    float dot = 0.0f;
-    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
-      const P a = reinterpret_cast<const P*>(g)[i], b = reinterpret_cast<const P*>(yr)[i];
-      P o;
+  for (int64_t j0 = 0; j0 < k; j0 += kReads) {
+    int32_t r[kReads];
+    float f[kReads], dot[kReads];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float ge = Elem<T>::up(a.e[e]);
-        dot = fmaf(ge, Elem<T>::up(b.e[e]), dot);
-        o.e[e] = Elem<T>::down(f * ge);
+    for (int j = 0; j < kReads; ++j) {
+      r[j] = j0 + j < k ? row_of[t * k + j0 + j] : -1;
+      if (r[j] >= n_rows) r[j] = -1;
+      f[j] = r[j] >= 0 ? w[t * k + j0 + j] : 0.0f;
+      dot[j] = 0.0f;
+    }
+    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
+      const P a = reinterpret_cast<const P*>(g)[i];
+      P b[kReads];
+#pragma unroll
+      for (int j = 0; j < kReads; ++j) b[j] = r[j] >= 0 ? reinterpret_cast<const P*>(y + r[j] * ldy)[i] : P{};
+      float ge[V];
+      unpack<T, V>(a, ge);
+#pragma unroll
+      for (int j = 0; j < kReads; ++j) {
+        if (r[j] < 0) continue;
+        float ye[V], d[V];
+        unpack<T, V>(b[j], ye);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dot[j] = fmaf(ge[e], ye[e], dot[j]);
+          d[e] = f[j] * ge[e];
+        }
+        reinterpret_cast<P*>(dy + r[j] * lddy)[i] = pack<T, V>(d);
       }
-      reinterpret_cast<P*>(dr)[i] = o;
     }
     for (int64_t i = pieces * V + threadIdx.x; i < H; i += kThreads) {
       const float ge = Elem<T>::up(g[i]);
-      dot = fmaf(ge, Elem<T>::up(yr[i]), dot);
-      dr[i] = Elem<T>::down(f * ge);
+#pragma unroll
+      for (int j = 0; j < kReads; ++j) {
+        if (r[j] < 0) continue;
+        dot[j] = fmaf(ge, Elem<T>::up(y[r[j] * ldy + i]), dot[j]);
+        dy[r[j] * lddy + i] = Elem<T>::down(f[j] * ge);
+      }
     }
-    dot = warp_sum(dot);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = dot;
+#pragma unroll
+    for (int j = 0; j < kReads; ++j) {
+      const float d = warp_sum(dot[j]);
+      if (threadIdx.x % 32 == j) part[threadIdx.x / 32][j] = d;
+    }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      float s = part[0];
-      for (int i = 1; i < kThreads / 32; ++i) s += part[i];
-      dw[t * k + j] = s;
+    if (threadIdx.x < kReads && j0 + threadIdx.x < k) {
+      float s = part[0][threadIdx.x];
+#pragma unroll
+      for (int i = 1; i < kThreads / 32; ++i) s += part[i][threadIdx.x];
+      dw[t * k + j0 + threadIdx.x] = s;
     }
     __syncthreads();
   }
@@ -190,33 +361,63 @@ __global__ void __launch_bounds__(kThreads) moe_combine_bwd_kernel(const T* dout
 
 template <typename Id>
 int sort(const void* ids, int64_t n, int E, int32_t* offsets, int32_t* row_of, cudaStream_t stream) {
-  const int smem = kSortWarps * E * 4;
   cudaError_t e = cudaFuncSetAttribute(moe_sort_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       kSortWarps * kMaxExperts * 4);
-  if (e == cudaSuccess)
-    moe_sort_kernel<Id><<<1, kSortThreads, smem, stream>>>(static_cast<const Id*>(ids), n, E, offsets, row_of);
-  return launched(e);
+                                       (kSortWarps + 1) * kMaxExperts * 4);
+  if (e != cudaSuccess) return launched(e);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kSortCtas);
+  cfg.blockDim = dim3(kSortThreads);
+  cfg.dynamicSmemBytes = size_t(kSortWarps + 1) * E * 4;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {kSortCtas, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return launched(cudaLaunchKernelEx(&cfg, moe_sort_kernel<Id>, static_cast<const Id*>(ids), n, E, offsets, row_of));
+}
+
+template <typename T, typename Id>
+int dispatch(const void* x, int64_t T_, int64_t H, int64_t ldx, const float* x_scale, const void* ids, int64_t k, int E,
+             void* rows, int64_t ldr, float* row_scale, int32_t* offsets, int32_t* row_of, cudaStream_t stream) {
+  constexpr int V = 16 / sizeof(T);
+  const bool vec = aligned_rows(x, ldx, sizeof(T)) && aligned_rows(rows, ldr, sizeof(T));
+  const T* xt = static_cast<const T*>(x);
+  T* rt = static_cast<T*>(rows);
+  if (T_ * k <= kSmallRouting) {
+    auto kernel = vec ? moe_dispatch_small_kernel<T, V, Id> : moe_dispatch_small_kernel<T, 1, Id>;
+    kernel<<<unsigned(T_ + 1), kThreads, 0, stream>>>(xt, T_, H, ldx, x_scale, static_cast<const Id*>(ids), int(k), E,
+                                                      rt, ldr, row_scale, offsets, row_of);
+    return launched(cudaSuccess);
+  }
+  const int rc = sort<Id>(ids, T_ * k, E, offsets, row_of, stream);
+  if (rc != ENTWINE_OK) return rc;
+  auto kernel = vec ? moe_move_kernel<T, V> : moe_move_kernel<T, 1>;
+  kernel<<<unsigned(T_), kThreads, 0, stream>>>(xt, H, ldx, x_scale, row_of, k, rt, ldr, row_scale);
+  return launched(cudaSuccess);
 }
 
 template <typename T>
-int move(const void* x, int64_t T_, int64_t H, int64_t ldx, const float* x_scale, const int32_t* row_of, int64_t k,
-         void* rows, int64_t ldr, float* row_scale, cudaStream_t stream) {
-  constexpr int V = 16 / sizeof(T);
-  auto kernel = aligned_rows(x, ldx, sizeof(T)) && aligned_rows(rows, ldr, sizeof(T)) ? moe_move_kernel<T, V>
-                                                                                       : moe_move_kernel<T, 1>;
-  kernel<<<unsigned(T_), kThreads, 0, stream>>>(static_cast<const T*>(x), H, ldx, x_scale, row_of, k,
-                                                static_cast<T*>(rows), ldr, row_scale);
-  return launched(cudaSuccess);
+int dispatch_ids(const void* x, int64_t T_, int64_t H, int64_t ldx, const float* x_scale, const void* ids, int ids64,
+                 int64_t k, int E, void* rows, int64_t ldr, float* row_scale, int32_t* offsets, int32_t* row_of,
+                 cudaStream_t s) {
+  return ids64 ? dispatch<T, int64_t>(x, T_, H, ldx, x_scale, ids, k, E, rows, ldr, row_scale, offsets, row_of, s)
+               : dispatch<T, int32_t>(x, T_, H, ldx, x_scale, ids, k, E, rows, ldr, row_scale, offsets, row_of, s);
 }
 
 template <typename T>
 int combine(const void* y, int64_t n_rows, int64_t H, int64_t ldy, const float* w, const int32_t* row_of, int64_t T_,
             int64_t k, void* out, int64_t ldo, cudaStream_t stream) {
   constexpr int V = 16 / sizeof(T);
-  auto kernel = aligned_rows(y, ldy, sizeof(T)) && aligned_rows(out, ldo, sizeof(T)) ? moe_combine_kernel<T, V>
-                                                                                      : moe_combine_kernel<T, 1>;
-  kernel<<<unsigned(T_), kThreads, 0, stream>>>(static_cast<const T*>(y), n_rows, H, ldy, w, row_of, k,
-                                                static_cast<T*>(out), ldo);
+  const bool vec = aligned_rows(y, ldy, sizeof(T)) && aligned_rows(out, ldo, sizeof(T));
+  auto kernel = !vec ? moe_combine_kernel<T, 1, kReads, 1>
+                : k <= kReads / 2 ? moe_combine_kernel<T, V, kReads / 2, 2> : moe_combine_kernel<T, V, kReads, 1>;
+  // one piece per thread until the tokens alone fill the GPU
+  const int64_t pieces = vec ? (H + V - 1) / V : H;
+  const int threads = pieces <= 128 || T_ < kFewTokens ? 128 : kThreads;
+  const int64_t parts = T_ < kFewTokens ? std::min<int64_t>((pieces + threads - 1) / threads, 64) : 1;
+  kernel<<<dim3(unsigned(T_), unsigned(parts)), threads, 0, stream>>>(static_cast<const T*>(y), n_rows, H, ldy, w,
+                                                                      row_of, k, static_cast<T*>(out), ldo);
   return launched(cudaSuccess);
 }
 
@@ -272,13 +473,13 @@ int entwine_moe_dispatch(const void* x, int dtype, int64_t T, int64_t H, int64_t
                 bad_pointer(row_of, 4) || (x_scale && (bad_pointer(x_scale, 4) || bad_pointer(row_scale, 4)))))
     return ENTWINE_ERR_INVALID;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  int rc = ids64 ? sort<int64_t>(ids, T * k, int(E), offsets, row_of, s)
-                 : sort<int32_t>(ids, T * k, int(E), offsets, row_of, s);
-  if (rc != ENTWINE_OK || T == 0) return rc;
   switch (size) {  // rows are moved as they are: only the size of an element counts
-    case 1: return move<uint8_t>(x, T, H, ldx, x_scale, row_of, k, rows, ldr, row_scale, s);
-    case 2: return move<uint16_t>(x, T, H, ldx, x_scale, row_of, k, rows, ldr, row_scale, s);
-    default: return move<uint32_t>(x, T, H, ldx, x_scale, row_of, k, rows, ldr, row_scale, s);
+    case 1:
+      return dispatch_ids<uint8_t>(x, T, H, ldx, x_scale, ids, ids64, k, int(E), rows, ldr, row_scale, offsets, row_of, s);
+    case 2:
+      return dispatch_ids<uint16_t>(x, T, H, ldx, x_scale, ids, ids64, k, int(E), rows, ldr, row_scale, offsets, row_of, s);
+    default:
+      return dispatch_ids<uint32_t>(x, T, H, ldx, x_scale, ids, ids64, k, int(E), rows, ldr, row_scale, offsets, row_of, s);
   }
 }
 

@@ -5,7 +5,10 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
+#include <cstring>
+#include <type_traits>
 
 #include "entwine_ops.h"
 
@@ -36,6 +39,77 @@ struct alignas(sizeof(T) * V) Piece {
   T e[V];
 };
 
+// The elements of a piece in fp32.  16-bit ones are taken from the 32-bit words that hold two of them: element by
+// element the compiler spends three instructions on each.
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const Piece<T, V>& v, float (&f)[V]) {
+  if constexpr (sizeof(T) == 2 && V >= 2) {
+    uint32_t w[V / 2];
+    memcpy(w, &v, sizeof(v));
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      } else {
+        __half2 h;
+        memcpy(&h, &w[i], 4);
+        const float2 d = __half22float2(h);
+        f[2 * i] = d.x;
+        f[2 * i + 1] = d.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = Elem<T>::up(v.e[e]);
+  }
+}
+
+// fp32 values rounded to a piece, two at a time.
+template <typename T, int V>
+__device__ __forceinline__ Piece<T, V> pack(const float (&f)[V]) {
+  Piece<T, V> o;
+  if constexpr (sizeof(T) == 2 && V >= 2) {
+    uint32_t w[V / 2];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        memcpy(&w[i], &h, 4);
+      } else {
+        const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+        memcpy(&w[i], &h, 4);
+      }
+    }
+    memcpy(&o, w, sizeof(o));
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) o.e[e] = Elem<T>::down(f[e]);
+  }
+  return o;
+}
+
+// A piece that is read once, zeros where `there` is false.  As an instruction of its own, in order with its
+// neighbours, so that a batch of them is in flight together whatever the compiler makes of the code around it.
+template <typename T, int V>
+__device__ __forceinline__ Piece<T, V> load_if(const T* p, bool there) {
+  if constexpr (sizeof(T) * V == 16) {
+    uint4 w;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+        "@p ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "=&r"(w.x), "=&r"(w.y), "=&r"(w.z), "=&r"(w.w)
+        : "l"(p), "r"(int(there)));
+    Piece<T, V> v;
+    memcpy(&v, &w, 16);
+    return v;
+  } else {
+    return there ? *reinterpret_cast<const Piece<T, V>*>(p) : Piece<T, V>{};
+  }
+}
+
 inline bool aligned_rows(const void* p, int64_t ld, int64_t elem_bytes, int64_t bytes = 16) {
   return reinterpret_cast<uintptr_t>(p) % uintptr_t(bytes) == 0 && (ld * elem_bytes) % bytes == 0;
 }
@@ -50,6 +124,19 @@ inline int launched(cudaError_t e) {
   if (e == cudaSuccess) return ENTWINE_OK;
   cudaGetLastError();
   return ENTWINE_ERR_CUDA;
+}
+
+// SMs of the current device (148 where that cannot be told).
+inline int sm_count() {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
