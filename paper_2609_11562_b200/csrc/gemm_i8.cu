@@ -5,7 +5,12 @@
 // its columns tokens (rows of A).  With few tokens the instruction is as narrow as their number (16 at least), so
 // that a decoding step pays for reading B and nothing else; and a warp's lanes, consecutive channels, store
 // consecutive elements of a row of C.
+#include <algorithm>
 #include <cstring>
+
+#ifndef PAIRMIN
+#define PAIRMIN 256
+#endif
 
 #include "ops_common.cuh"
 #include "sm100.cuh"
@@ -28,6 +33,13 @@ struct Maps {
   CUtensorMap b;  // channels [G][N][K]
 };
 
+// (a pair tile: 256 channels, up to 256 tokens)
+constexpr int kPairThreads = 320;    // TMA warp, MMA warp, eight epilogue warps
+constexpr int kPairChannels = 256;
+constexpr int kPairTokens = 256;
+constexpr int kPairStageBytes = 32768;
+constexpr int kBand = 16;            // token tiles that share a walk over the channels: their rows stay in L2
+
 struct Params {
   const float* scale_a;
   const float* scale_b;
@@ -37,6 +49,7 @@ struct Params {
   int64_t ldc;
   int M, N, K, G;
   int token_tiles;         // an upper bound with experts
+  int tile_rows;           // most tokens of a pair tile, a multiple of 32
 };
 
 // Bounded wait for a phase of a barrier.
@@ -194,6 +207,270 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
   if (warp == 1) tmem_dealloc(tmem, T::kTmemCols);
 }
 
+// ------------------------------------------------------------------------------------------
+// many tokens: CTA pairs, persistent
+// ------------------------------------------------------------------------------------------
+// Two CTAs of a cluster compute 256 channels x up to 256 tokens (tcgen05 cta_group::2: 128 channels each, each loading
+// half of the tokens), so that an SM takes in 64 bytes per cycle at the full MMA rate instead of 96.  A tile is as
+// wide as its tokens, in steps of 32: an expert's last rows cost what they are.  Two accumulators in TMEM: the
+// epilogue of a tile runs beside the products of the next.
+struct PairTile {
+  int g, m0, rows, n0;
+};
+
+template <typename Out>
+struct PairCfg {
+  static constexpr int kStages = sizeof(Out) == 4 ? 5 : 6;
+  static constexpr int kStagingBytes = 32 * 32 * sizeof(Out);  // of a warp: 32 tokens x 32 channels
+  static constexpr int kSmem = kStages * kPairStageBytes + 8 * kStagingBytes + 1024;
+};
+
+// Tile t of the walk.  first[g]: token tiles of the experts before g.  An expert's tiles are as equal as steps of 32
+// rows allow; bands of kBand of them walk over the channels together.
+__device__ __forceinline__ PairTile pair_tile(const Params& P, const int* first, const int* start, int channel_tiles,
+                                              int t) {
+  const int u = t / channel_tiles;
+  int g = 0;
+  for (int step = 512; step > 0; step >>= 1)  // the last expert whose tiles start at or before u
+    if (g + step < P.G && first[g + step] <= u) g += step;
+  const int tiles = first[g + 1] - first[g];
+  int local = t - first[g] * channel_tiles;
+  const int band = local / (kBand * channel_tiles);
+  local -= band * kBand * channel_tiles;
+  const int in_band = min(kBand, tiles - band * kBand);
+  const int m = band * kBand + local % in_band;
+  const int total = start[2 * g + 1] - start[2 * g];
+  const int height = ((total + tiles - 1) / tiles + 31) / 32 * 32;
+  PairTile r;
+  r.g = g;
+  r.m0 = start[2 * g] + m * height;
+  r.rows = min(height, start[2 * g + 1] - r.m0);
+  r.n0 = local / in_band * kPairChannels;
+  return r;
+}
+
+template <typename Out>
+__global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __grid_constant__ Maps maps,
+                                                                       const __grid_constant__ Params P) {
+  using C = PairCfg<Out>;
+  constexpr int S = C::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[2 * S + 5];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int first[kMaxGroups + 1], start[2 * kMaxGroups];
+  __shared__ __align__(16) float token_scale[8][32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int rank = int(cluster_ctarank());
+  const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * S, tfull = full + 16 * S, tempty = tfull + 16,
+                 drain = tempty + 16;
+
+  // token tiles of each expert, then their running sum
+  for (int g = threadIdx.x; g < P.G; g += kPairThreads) {
+    int lo = 0, hi = P.M;
+    if (P.offsets) {
+      lo = min(max(P.offsets[g], 0), P.M);
+      hi = min(max(P.offsets[g + 1], lo), P.M);
+    }
+    start[2 * g] = lo;
+    start[2 * g + 1] = hi;
+    first[g + 1] = (hi - lo + P.tile_rows - 1) / P.tile_rows;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(tfull + 8 * a, 1);
+      mbar_init(tempty + 8 * a, 16);
+    }
+    mbar_init(drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    first[0] = 0;
+  }
+  if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    int before = 0;
+    for (int g0 = 0; g0 < P.G; g0 += 32) {
+      int sum = g0 + lane < P.G ? first[g0 + lane + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += v;
+      }
+      sum += before;
+      if (g0 + lane < P.G) first[g0 + lane + 1] = sum;
+      before = __shfl_sync(0xffffffffu, sum, 31);
+    }
+  }
+  __syncthreads();
+  cluster_sync_all();  // both CTAs' barriers exist before either signals
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const int channel_tiles = (P.N + kPairChannels - 1) / kPairChannels;
+  const int total = first[P.G] * channel_tiles, pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2;
+  const int blocks = (P.K + kKBytes - 1) / kKBytes;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint32_t bytes = kChannels * kKBytes + P.tile_rows / 2 * kKBytes;  // that each CTA brings
+      int stage = 0;
+      uint32_t phase = 0;
+      long long issued = 0;
+      bool ok = true;
+      for (int t = pair; ok && t < total; t += pairs) {
+        const PairTile w = pair_tile(P, first, start, channel_tiles, t);
+        const int half = (w.rows + 31) / 32 * 16;
+        for (int b = 0; b < blocks; ++b) {
+          if (!(ok = wait_bar(empty + 8 * stage, phase ^ 1))) break;
+          const uint32_t at = ring + stage * kPairStageBytes, bar = map_to_cta(full + 8 * stage, 0);
+          if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * bytes);
+          tma_load_3d_pair(at, &maps.b, b * kKBytes, w.n0 + rank * kChannels, w.g, bar);
+          tma_load_2d_pair(at + kChannels * kKBytes, &maps.a, b * kKBytes, w.m0 + rank * half, bar);
+          ++issued;
+          if (++stage == S) stage = 0, phase ^= 1;
+        }
+      }
+      // after a wait that ran out: copies still under way end before the CTA does
+      for (int i = 0; !ok && rank == 0 && i < S && i < issued; ++i) {
+        if (--stage < 0) stage = S - 1, phase ^= 1;
+        if (!wait_bar(full + 8 * stage, phase)) break;
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int t = pair; ok && t < total; t += pairs) {
+        const PairTile w = pair_tile(P, first, start, channel_tiles, t);
+        const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (uint32_t((w.rows + 31) / 32 * 4) << 17) |
+                               (uint32_t(kPairChannels >> 4) << 24);
+        if (!(ok = wait_bar(tempty + 8 * acc, acc_phase ^ 1))) break;
+        tc_fence_after();
+        const uint32_t d = tmem + acc * kPairTokens;
+        for (int b = 0; b < blocks; ++b) {
+          if (!(ok = wait_bar(full + 8 * stage, phase))) break;
+          tc_fence_after();
+          const uint32_t at = ring + stage * kPairStageBytes;
+          const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
+#pragma unroll
+          for (int k = 0; k < kKBytes / 32; ++k) umma_i8_pair(d, da + 2 * k, db + 2 * k, idesc, b > 0 || k > 0);
+          tc_commit_pair(empty + 8 * stage);
+          if (++stage == S) stage = 0, phase ^= 1;
+        }
+        if (ok) tc_commit_pair(tfull + 8 * acc);
+        if ((acc ^= 1) == 0) acc_phase ^= 1;
+      }
+      if (!ok) {  // products under way end before the TMEM is given back
+        tc_commit_pair(drain);
+        wait_bar(drain, 0);
+      }
+    }
+  } else {
+    // Epilogue: a warp owns 32 channels (its lane quarter of the accumulator), a lane one of them; groups of four
+    // warps take turns at the 32-token chunks of a tile.  Values go through the warp's own staging, so that 16-byte
+    // stores carry 32 channels of eight (fp32: four) tokens at a time.
+    const int q = warp & 3, group = (warp - 2) / 4;
+    Out* const staging = reinterpret_cast<Out*>(smem_raw + (ring - smem_u32(smem_raw)) + S * kPairStageBytes +
+                                                (warp - 2) * C::kStagingBytes);
+    float* const sa = token_scale[warp - 2];
+    constexpr int kVec = 16 / sizeof(Out), kLanesPerRow = 32 / kVec, kRowsPerStore = 32 / kLanesPerRow;
+    const bool vec = reinterpret_cast<uintptr_t>(P.c) % 16 == 0 && P.ldc * sizeof(Out) % 16 == 0;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int t = pair; t < total; t += pairs) {
+      const PairTile w = pair_tile(P, first, start, channel_tiles, t);
+      const int n0 = w.n0 + rank * kChannels + q * 32, n = n0 + lane;
+      const float sb = n < P.N ? P.scale_b[int64_t(w.g) * P.N + n] : 0.0f;
+      const float add = n < P.N && P.bias ? P.bias[int64_t(w.g) * P.N + n] : 0.0f;
+      const bool ok = __all_sync(0xffffffffu, wait_bar(tfull + 8 * acc, acc_phase));
+      if (!ok) break;
+      tc_fence_after();
+      const int chunks = (w.rows + 31) / 32;
+      for (int c = group; c < chunks; c += 2) {
+        uint32_t v[32];
+        tmem_ld32(tmem + (uint32_t(q) << 21) + acc * kPairTokens + c * 32, v);
+        sa[lane] = c * 32 + lane < w.rows ? P.scale_a[w.m0 + c * 32 + lane] : 0.0f;
+        tmem_ld_wait();
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          const float4 s4 = *reinterpret_cast<const float4*>(sa + j);
+          staging[(j + 0) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 0])) * s4.x, sb, add));
+          staging[(j + 1) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 1])) * s4.y, sb, add));
+          staging[(j + 2) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 2])) * s4.z, sb, add));
+          staging[(j + 3) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 3])) * s4.w, sb, add));
+        }
+        __syncwarp();
+        const int rows = min(32, w.rows - c * 32);
+        Out* const out = static_cast<Out*>(P.c) + int64_t(w.m0 + c * 32) * P.ldc + n0;
+        if (vec && n0 + 32 <= P.N) {
+          const int r0 = lane / kLanesPerRow, x = lane % kLanesPerRow * kVec;
+#pragma unroll
+          for (int i = 0; i < 32 / kRowsPerStore; ++i) {
+            const int r = i * kRowsPerStore + r0;
+            if (r < rows) *reinterpret_cast<uint4*>(out + r * P.ldc + x) = *reinterpret_cast<const uint4*>(staging + r * 32 + x);
+          }
+        } else if (n < P.N) {
+          for (int r = 0; r < rows; ++r) out[r * P.ldc + lane] = staging[r * 32 + lane];
+        }
+        __syncwarp();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty + 8 * acc, 0));
+      if ((acc ^= 1) == 0) acc_phase ^= 1;
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // neither CTA signals the other's barriers any more
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+template <typename Out>
+int run_pairs(const Maps& maps, Params P, cudaStream_t stream) {
+  using C = PairCfg<Out>;
+  const int64_t token_tiles = P.offsets ? P.M / P.tile_rows + P.G : (P.M + P.tile_rows - 1) / P.tile_rows;
+  const int64_t tiles = token_tiles * ((P.N + kPairChannels - 1) / kPairChannels);
+  if (tiles > kMaxExtent) return ENTWINE_ERR_INVALID;
+  auto kernel = gemm_i8_pair_kernel<Out>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  if (e != cudaSuccess) return launched(e);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(std::min<int64_t>(2 * tiles, sm_count() / 2 * 2)));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {2, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return launched(cudaLaunchKernelEx(&cfg, kernel, maps, P));
+}
+
+// The height of the pair tiles: as many waves of the pairs as there are, each as long as its tiles are high (and a
+// part that does not depend on it).
+int pair_rows(const Params& P) {
+  if (P.G > 1) return kPairTokens;
+  const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels, pairs = sm_count() / 2;
+  int best = kPairTokens;
+  int64_t least = 0;
+  for (int rows = kPairTokens; rows >= 96; rows -= 32) {
+    const int64_t token_tiles = (P.M + rows - 1) / rows, waves = (token_tiles * channel_tiles + pairs - 1) / pairs;
+    const int64_t cost = waves * (rows + 32);
+    if (least == 0 || cost < least) least = cost, best = rows;
+  }
+  return best;
+}
+
 template <int TOKENS, typename Out>
 int run(const Maps& maps, Params P, cudaStream_t stream) {
   using T = Tile<TOKENS>;
@@ -232,8 +509,15 @@ bool make_maps(Maps* maps, const void* A, int64_t lda, const void* B, int64_t ld
 template <typename Out>
 int run_as(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t expert_stride, const Params& P,
            cudaStream_t stream) {
-  // the narrowest tile that holds an expert's average rows
-  const int rows = (P.M + P.G - 1) / P.G;
+  const int rows = (P.M + P.G - 1) / P.G;  // of an average expert
+  if (rows > PAIRMIN) {
+    Params Q = P;
+    Q.tile_rows = pair_rows(P);
+    Maps maps;
+    if (!make_maps(&maps, A, lda, B, ldb, expert_stride, Q, Q.tile_rows / 2)) return ENTWINE_ERR_CUDA;
+    return run_pairs<Out>(maps, Q, stream);
+  }
+  // the narrowest tile that holds them
   const int tokens = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   Maps maps;
   if (!make_maps(&maps, A, lda, B, ldb, expert_stride, P, tokens)) return ENTWINE_ERR_CUDA;
