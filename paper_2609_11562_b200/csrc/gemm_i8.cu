@@ -8,10 +8,6 @@
 #include <algorithm>
 #include <cstring>
 
-#ifndef PAIRMIN
-#define PAIRMIN 256
-#endif
-
 #include "ops_common.cuh"
 #include "sm100.cuh"
 
@@ -21,6 +17,7 @@ namespace {
 constexpr int kChannels = 128;       // channels of a tile
 constexpr int kKBytes = 128;         // elements of K per pipeline stage (one swizzled row)
 constexpr int kThreads = 128;
+constexpr int kMaxSplit = 8;
 constexpr int kMaxGroups = 1024;
 constexpr int64_t kMaxK = 131071;    // 128 * 128 * K < 2^31
 constexpr int64_t kMaxExtent = 2147483647;
@@ -49,6 +46,7 @@ struct Params {
   int64_t ldc;
   int M, N, K, G;
   int token_tiles;         // an upper bound with experts
+  int split;               // CTAs that share the length K of a tile
   int tile_rows;           // most tokens of a pair tile, a multiple of 32
 };
 
@@ -70,8 +68,8 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity) {
 template <int TOKENS>
 struct Tile {
   static constexpr int kStageBytes = (kChannels + TOKENS) * kKBytes;
-  // all of the shared memory for one CTA per SM with wide tiles, two CTAs per SM with narrow ones
-  static constexpr int kStages = TOKENS >= 256 ? 4 : TOKENS >= 128 ? 6 : TOKENS >= 64 ? 4 : TOKENS >= 32 ? 5 : 6;
+  // two CTAs per SM
+  static constexpr int kStages = TOKENS >= 128 ? 3 : TOKENS >= 64 ? 4 : TOKENS >= 32 ? 5 : 6;
   static constexpr int kSmem = kStages * kStageBytes + 1024;
   static constexpr int kTmemCols = TOKENS < 32 ? 32 : TOKENS;
 };
@@ -108,6 +106,9 @@ __device__ __forceinline__ void find_tile(const Params& P, int tile, int lane, i
   }
 }
 
+// One tile of 128 channels x TOKENS tokens per cluster of one to eight CTAs, which share the length K: each sums its
+// blocks of K, then the int32 partial sums (exact in any order) meet through distributed shared memory, each CTA
+// finishing its share of the tokens.  So a decoding step reads the weights with all SMs.
 template <int TOKENS, typename Out>
 __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant__ Maps maps,
                                                            const __grid_constant__ Params P) {
@@ -119,13 +120,33 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
   __shared__ int job[3];
   __shared__ float token_scale[TOKENS];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int n0 = int(blockIdx.x / P.token_tiles) * kChannels, tile = int(blockIdx.x % P.token_tiles);
+  const int rank = int(cluster_ctarank()), index = int(blockIdx.x) / P.split;
+  const int n0 = index / P.token_tiles * kChannels, tile = index % P.token_tiles;
   const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * S, done = full + 16 * S;
+  const int all = (P.K + kKBytes - 1) / kKBytes;  // blocks of K; this CTA's:
+  const int first = int(int64_t(all) * rank / P.split), blocks = int(int64_t(all) * (rank + 1) / P.split) - first;
 
+  int issued = 0;
+  bool ok = true;
+  int g = 0, m0 = tile * TOKENS, m_end = P.M;
+  auto load = [&]() {
+    const int s = issued % S;
+    const uint32_t at = ring + s * T::kStageBytes;
+    mbar_arrive_expect_tx(full + 8 * s, T::kStageBytes);
+    tma_load_3d(at, &maps.b, (first + issued) * kKBytes, n0, g, full + 8 * s);
+    tma_load_2d(at + kChannels * kKBytes, &maps.a, (first + issued) * kKBytes, m0, full + 8 * s);
+    ++issued;
+  };
   if (warp == 0) {
-    int g = 0, m0 = tile * TOKENS, m_end = P.M;
-    if (P.offsets) find_tile<TOKENS>(P, tile, lane, &g, &m0, &m_end);
+    if (lane == 0) {
+      tma_prefetch_map(&maps.a);
+      tma_prefetch_map(&maps.b);
+    }
+    if (P.offsets) {
+      g = -1;
+      find_tile<TOKENS>(P, tile, lane, &g, &m0, &m_end);
+    }
     if (lane == 0) {
       job[0] = g;
       job[1] = m0;
@@ -136,29 +157,36 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
       }
       mbar_init(done, 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      if (g >= 0)  // the first loads need nothing that the rest of the CTA prepares
+        while (issued < min(S, blocks)) load();
     }
   }
-  __syncthreads();
-  const int g = job[0], m0 = job[1], m_end = job[2];
-  if (g < 0) return;  // fewer tiles than the bound
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), T::kTmemCols);
-  for (int i = threadIdx.x; i < TOKENS; i += kThreads) token_scale[i] = m0 + i < m_end ? P.scale_a[m0 + i] : 0.0f;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  const int blocks = (P.K + kKBytes - 1) / kKBytes;
+  g = job[0];
+  m0 = job[1];
+  m_end = job[2];
+  if (g < 0) {  // fewer tiles than the bound
+    if (warp == 1) tmem_dealloc(tmem, T::kTmemCols);
+    return;
+  }
+  for (int i = threadIdx.x; i < TOKENS; i += kThreads) token_scale[i] = m0 + i < m_end ? P.scale_a[m0 + i] : 0.0f;
+  // this lane's four channels in the last step
+  const int n = n0 + 4 * lane;
+  float sb[4], add[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sb[i] = n + i < P.N ? P.scale_b[int64_t(g) * P.N + n + i] : 0.0f;
+    add[i] = n + i < P.N && P.bias ? P.bias[int64_t(g) * P.N + n + i] : 0.0f;
+  }
 
-  int issued = 0;
-  bool ok = true;
   if (threadIdx.x == 0) {
-    for (; issued < blocks; ++issued) {
-      const int s = issued % S;
-      if (issued >= S && !(ok = wait_bar(empty + 8 * s, (issued / S - 1) & 1))) break;
-      const uint32_t at = ring + s * T::kStageBytes;
-      mbar_arrive_expect_tx(full + 8 * s, T::kStageBytes);
-      tma_load_3d(at, &maps.b, issued * kKBytes, n0, g, full + 8 * s);
-      tma_load_2d(at + kChannels * kKBytes, &maps.a, issued * kKBytes, m0, full + 8 * s);
+    while (issued < blocks) {
+      if (!(ok = wait_bar(empty + 8 * (issued % S), (issued / S - 1) & 1))) break;
+      load();
     }
   } else if (threadIdx.x == 32) {
     // int32 accumulator, signed 8-bit operands, both K-major
@@ -180,28 +208,61 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
   ok = wait_bar(done, 0) && ok;
   tc_fence_after();
   ok = !__syncthreads_or(!ok);
-  if (ok) {
-    const int n = n0 + threadIdx.x;
-    const float sb = n < P.N ? P.scale_b[int64_t(g) * P.N + n] : 0.0f;
-    const float add = n < P.N && P.bias ? P.bias[int64_t(g) * P.N + n] : 0.0f;
-    Out* c = static_cast<Out*>(P.c) + int64_t(m0) * P.ldc + n;
-    constexpr int kCols = 16;
+  if (!ok && threadIdx.x == 0) {
+    // copies still under way end before the CTA does
+    for (int i = issued > S ? issued - S : 0; i < issued; ++i)
+      if (!wait_bar(full + 8 * (i % S), (i / S) & 1)) break;
+  }
+  // The partial sums go to shared memory, over the operands: [TOKENS][channels].
+  const int used = min(TOKENS, m_end - m0);
+  {
+    constexpr int kCols = TOKENS < 32 ? TOKENS : 32;
+    const uint32_t mine = ring + threadIdx.x * 4;
 #pragma unroll 1
-    for (int j0 = 0; j0 < TOKENS && m0 + j0 < m_end; j0 += kCols) {
+    for (int j0 = 0; j0 < used; j0 += kCols) {
       uint32_t v[kCols];
-      tmem_ld16(tmem + (uint32_t(warp) << 21) + j0, v);
-      tmem_ld_wait();
+      if constexpr (kCols == 16) tmem_ld16(tmem + (uint32_t(warp) << 21) + j0, v);
+      else tmem_ld32(tmem + (uint32_t(warp) << 21) + j0, v);
+      tmem_ld_wait(v);
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) {
-        // the sum is exact; its conversion, the two products and the last rounding are the only inexact steps
-        const float f = fmaf(__int2float_rn(int(v[j])) * token_scale[j0 + j], sb, add);
-        if (n < P.N && m0 + j0 + j < m_end) c[int64_t(j0 + j) * P.ldc] = Elem<Out>::down(f);
+      for (int j = 0; j < kCols; ++j)
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(mine + (j0 + j) * kChannels * 4), "r"(v[j]) : "memory");
+    }
+  }
+  if (P.split > 1) cluster_sync_all();
+  else __syncthreads();
+  // Every warp finishes tokens, four channels per lane: the sum is exact; its conversion, the two products and the
+  // last rounding are the only inexact steps.
+  if (ok) {
+    const bool vec = reinterpret_cast<uintptr_t>(P.c) % (4 * sizeof(Out)) == 0 && P.ldc % 4 == 0 && n + 4 <= P.N;
+    for (int j = rank + warp * P.split; j < used; j += P.split * (kThreads / 32)) {
+      const uint32_t at = ring + (j * kChannels + 4 * lane) * 4;
+      int4 part[kMaxSplit];
+#pragma unroll
+      for (int r = 0; r < kMaxSplit; ++r) part[r] = r < P.split ? ld_cluster_v4(map_to_cta(at, r)) : make_int4(0, 0, 0, 0);
+      int4 sum = part[0];
+#pragma unroll
+      for (int r = 1; r < kMaxSplit; ++r) {
+        sum.x += part[r].x;
+        sum.y += part[r].y;
+        sum.z += part[r].z;
+        sum.w += part[r].w;
+      }
+      const float f = token_scale[j];
+      const float o[4] = {fmaf(__int2float_rn(sum.x) * f, sb[0], add[0]), fmaf(__int2float_rn(sum.y) * f, sb[1], add[1]),
+                          fmaf(__int2float_rn(sum.z) * f, sb[2], add[2]), fmaf(__int2float_rn(sum.w) * f, sb[3], add[3])};
+      Out* const c = static_cast<Out*>(P.c) + int64_t(m0 + j) * P.ldc + n;
+      if (vec) {
+        *reinterpret_cast<Piece<Out, 4>*>(c) = pack<Out, 4>(o);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + i < P.N) c[i] = Elem<Out>::down(o[i]);
       }
     }
-  } else if (threadIdx.x == 0) {
-    // copies still under way end before the CTA does
-    for (int i = issued > S ? issued - S : 0; i < issued; ++i) wait_bar(full + 8 * (i % S), (i / S) & 1);
   }
+  __syncwarp();
+  if (P.split > 1) cluster_sync_all();  // no CTA leaves while its sums are read
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tmem, T::kTmemCols);
@@ -221,33 +282,43 @@ struct PairTile {
 template <typename Out>
 struct PairCfg {
   static constexpr int kStages = sizeof(Out) == 4 ? 5 : 6;
-  static constexpr int kStagingBytes = 32 * 32 * sizeof(Out);  // of a warp: 32 tokens x 32 channels
-  static constexpr int kSmem = kStages * kPairStageBytes + 8 * kStagingBytes + 1024;
+  static constexpr int kStagingBytes = 32 * kChannels * sizeof(Out);  // of a group of epilogue warps
+  static constexpr int kSmem = kStages * kPairStageBytes + 2 * kStagingBytes + 1024;
 };
 
-// Tile t of the walk.  first[g]: token tiles of the experts before g.  An expert's tiles are as equal as steps of 32
-// rows allow; bands of kBand of them walk over the channels together.
-__device__ __forceinline__ PairTile pair_tile(const Params& P, const int* first, const int* start, int channel_tiles,
-                                              int t) {
-  const int u = t / channel_tiles;
+// What the walk over the tiles needs of each expert.
+struct PairGroups {
+  int first[kMaxGroups + 1];  // token tiles of the experts before
+  int start[kMaxGroups];      // first row
+  int end[kMaxGroups];
+  int height[kMaxGroups];     // rows of a tile: an expert's tiles are as equal as steps of 32 rows allow
+};
+
+// The tiles of a pair, in order.  An expert's bands of kBand token tiles each walk over the channels together.
+struct PairWalk {
+  const PairGroups& G;
+  int channel_tiles;
   int g = 0;
-  for (int step = 512; step > 0; step >>= 1)  // the last expert whose tiles start at or before u
-    if (g + step < P.G && first[g + step] <= u) g += step;
-  const int tiles = first[g + 1] - first[g];
-  int local = t - first[g] * channel_tiles;
-  const int band = local / (kBand * channel_tiles);
-  local -= band * kBand * channel_tiles;
-  const int in_band = min(kBand, tiles - band * kBand);
-  const int m = band * kBand + local % in_band;
-  const int total = start[2 * g + 1] - start[2 * g];
-  const int height = ((total + tiles - 1) / tiles + 31) / 32 * 32;
-  PairTile r;
-  r.g = g;
-  r.m0 = start[2 * g] + m * height;
-  r.rows = min(height, start[2 * g + 1] - r.m0);
-  r.n0 = local / in_band * kPairChannels;
-  return r;
-}
+  __device__ __forceinline__ PairTile at(int t) {
+    while (G.first[g + 1] * channel_tiles <= t) ++g;
+    const int tiles = G.first[g + 1] - G.first[g];
+    int local = t - G.first[g] * channel_tiles, m = 0, in_band = tiles;
+    if (tiles > kBand) {
+      const int band = local / (kBand * channel_tiles);
+      local -= band * kBand * channel_tiles;
+      m = band * kBand;
+      in_band = min(kBand, tiles - m);
+    }
+    const int channel = int(unsigned(local) / unsigned(in_band));
+    m += local - channel * in_band;
+    PairTile r;
+    r.g = g;
+    r.m0 = G.start[g] + m * G.height[g];
+    r.rows = min(G.height[g], G.end[g] - r.m0);
+    r.n0 = channel * kPairChannels;
+    return r;
+  }
+};
 
 template <typename Out>
 __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __grid_constant__ Maps maps,
@@ -257,7 +328,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * S + 5];
   __shared__ uint32_t tmem_slot;
-  __shared__ int first[kMaxGroups + 1], start[2 * kMaxGroups];
+  __shared__ PairGroups groups;
   __shared__ __align__(16) float token_scale[8][32];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int rank = int(cluster_ctarank());
@@ -265,18 +336,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
   const uint32_t full = smem_u32(bars), empty = full + 8 * S, tfull = full + 16 * S, tempty = tfull + 16,
                  drain = tempty + 16;
 
-  // token tiles of each expert, then their running sum
-  for (int g = threadIdx.x; g < P.G; g += kPairThreads) {
-    int lo = 0, hi = P.M;
-    if (P.offsets) {
-      lo = min(max(P.offsets[g], 0), P.M);
-      hi = min(max(P.offsets[g + 1], lo), P.M);
-    }
-    start[2 * g] = lo;
-    start[2 * g + 1] = hi;
-    first[g + 1] = (hi - lo + P.tile_rows - 1) / P.tile_rows;
-  }
   if (threadIdx.x == 0) {
+    tma_prefetch_map(&maps.a);
+    tma_prefetch_map(&maps.b);
     for (int s = 0; s < S; ++s) {
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
@@ -287,32 +349,48 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
     }
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    first[0] = 0;
+    groups.first[0] = 0;
   }
   if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 0) {
-    int before = 0;
-    for (int g0 = 0; g0 < P.G; g0 += 32) {
-      int sum = g0 + lane < P.G ? first[g0 + lane + 1] : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += v;
-      }
-      sum += before;
-      if (g0 + lane < P.G) first[g0 + lane + 1] = sum;
-      before = __shfl_sync(0xffffffffu, sum, 31);
+  // token tiles of each expert, then their running sum
+  for (int g = threadIdx.x; g < P.G; g += kPairThreads) {
+    int lo = 0, hi = P.M;
+    if (P.offsets) {
+      lo = min(max(P.offsets[g], 0), P.M);
+      hi = min(max(P.offsets[g + 1], lo), P.M);
     }
+    const int tiles = (hi - lo + P.tile_rows - 1) / P.tile_rows;
+    groups.start[g] = lo;
+    groups.end[g] = hi;
+    groups.height[g] = tiles > 0 ? ((hi - lo + tiles - 1) / tiles + 31) / 32 * 32 : 0;
+    groups.first[g + 1] = tiles;
   }
-  __syncthreads();
-  cluster_sync_all();  // both CTAs' barriers exist before either signals
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync_all();  // (of this CTA's threads, too) both CTAs' barriers exist before either signals
   tc_fence_after();
+  if (P.G > 1) {
+    if (warp == 0) {
+      int before = 0;
+      for (int g0 = 0; g0 < P.G; g0 += 32) {
+        int sum = g0 + lane < P.G ? groups.first[g0 + lane + 1] : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += v;
+        }
+        sum += before;
+        if (g0 + lane < P.G) groups.first[g0 + lane + 1] = sum;
+        before = __shfl_sync(0xffffffffu, sum, 31);
+      }
+    }
+    __syncthreads();
+  }
   const uint32_t tmem = tmem_slot;
   const int channel_tiles = (P.N + kPairChannels - 1) / kPairChannels;
-  const int total = first[P.G] * channel_tiles, pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2;
+  const int total = groups.first[P.G] * channel_tiles, pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2;
   const int blocks = (P.K + kKBytes - 1) / kKBytes;
+  PairWalk walk{groups, channel_tiles};
 
   if (warp == 0) {
     if (lane == 0) {
@@ -322,7 +400,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
       long long issued = 0;
       bool ok = true;
       for (int t = pair; ok && t < total; t += pairs) {
-        const PairTile w = pair_tile(P, first, start, channel_tiles, t);
+        const PairTile w = walk.at(t);
         const int half = (w.rows + 31) / 32 * 16;
         for (int b = 0; b < blocks; ++b) {
           if (!(ok = wait_bar(empty + 8 * stage, phase ^ 1))) break;
@@ -345,9 +423,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
-      for (int t = pair; ok && t < total; t += pairs) {
-        const PairTile w = pair_tile(P, first, start, channel_tiles, t);
-        const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (uint32_t((w.rows + 31) / 32 * 4) << 17) |
+      int rows = pair < total ? walk.at(pair).rows : 0, next_rows = 0;
+      for (int t = pair; ok && t < total; t += pairs, rows = next_rows) {
+        const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (uint32_t((rows + 31) / 32 * 4) << 17) |
                                (uint32_t(kPairChannels >> 4) << 24);
         if (!(ok = wait_bar(tempty + 8 * acc, acc_phase ^ 1))) break;
         tc_fence_after();
@@ -361,6 +439,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
           for (int k = 0; k < kKBytes / 32; ++k) umma_i8_pair(d, da + 2 * k, db + 2 * k, idesc, b > 0 || k > 0);
           tc_commit_pair(empty + 8 * stage);
           if (++stage == S) stage = 0, phase ^= 1;
+          if (b == 0 && t + pairs < total) next_rows = walk.at(t + pairs).rows;  // (while these products run)
         }
         if (ok) tc_commit_pair(tfull + 8 * acc);
         if ((acc ^= 1) == 0) acc_phase ^= 1;
@@ -372,57 +451,89 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
     }
   } else {
     // Epilogue: a warp owns 32 channels (its lane quarter of the accumulator), a lane one of them; groups of four
-    // warps take turns at the 32-token chunks of a tile.  Values go through the warp's own staging, so that 16-byte
-    // stores carry 32 channels of eight (fp32: four) tokens at a time.
+    // warps take turns at the 32-token chunks of a tile.  Values go through the group's staging, [32 tokens][128
+    // channels], so that whole lines of C are stored: with 64 bytes of a row per store (a warp's own channels) the
+    // requests to L2 were the limit, 6400-7600 cycles a tile.  The scales of a tile are read before its sums are waited
+    // for, a chunk's sums while the chunk before is worked on.
     const int q = warp & 3, group = (warp - 2) / 4;
+    constexpr int kTurns = kPairTokens / 64;  // chunks of a tile that a group takes
     Out* const staging = reinterpret_cast<Out*>(smem_raw + (ring - smem_u32(smem_raw)) + S * kPairStageBytes +
-                                                (warp - 2) * C::kStagingBytes);
+                                                group * C::kStagingBytes);
     float* const sa = token_scale[warp - 2];
-    constexpr int kVec = 16 / sizeof(Out), kLanesPerRow = 32 / kVec, kRowsPerStore = 32 / kLanesPerRow;
+    constexpr int kVec = 16 / sizeof(Out), kLanesPerRow = kChannels / kVec, kRowsPerStore = 32 / kLanesPerRow;
     const bool vec = reinterpret_cast<uintptr_t>(P.c) % 16 == 0 && P.ldc * sizeof(Out) % 16 == 0;
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int t = pair; t < total; t += pairs) {
-      const PairTile w = pair_tile(P, first, start, channel_tiles, t);
-      const int n0 = w.n0 + rank * kChannels + q * 32, n = n0 + lane;
+      const PairTile w = walk.at(t);
+      const int n0 = w.n0 + rank * kChannels, n = n0 + q * 32 + lane;
       const float sb = n < P.N ? P.scale_b[int64_t(w.g) * P.N + n] : 0.0f;
       const float add = n < P.N && P.bias ? P.bias[int64_t(w.g) * P.N + n] : 0.0f;
-      const bool ok = __all_sync(0xffffffffu, wait_bar(tfull + 8 * acc, acc_phase));
-      if (!ok) break;
+      float scales[kTurns];
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int r = (group + 2 * i) * 32 + lane;
+        scales[i] = r < w.rows ? P.scale_a[w.m0 + r] : 0.0f;
+      }
+      if (!named_bar_and(1 + group, 128, wait_bar(tfull + 8 * acc, acc_phase))) break;  // the group leaves together
       tc_fence_after();
       const int chunks = (w.rows + 31) / 32;
-      for (int c = group; c < chunks; c += 2) {
-        uint32_t v[32];
-        tmem_ld32(tmem + (uint32_t(q) << 21) + acc * kPairTokens + c * 32, v);
-        sa[lane] = c * 32 + lane < w.rows ? P.scale_a[w.m0 + c * 32 + lane] : 0.0f;
-        tmem_ld_wait();
+      const uint32_t sums = tmem + (uint32_t(q) << 21) + acc * kPairTokens;
+      // The accumulator has been read (its loads have completed).  Nothing else is handed over, so the arrival need
+      // not wait for this warp's stores to C: with release semantics it did, 1 us a tile.
+      auto release = [&]() {
+        tc_fence_before();
         __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(tempty + 8 * acc, 0));
+      };
+      auto finish = [&](const uint32_t (&v)[32], float scale, int c) {
+        sa[lane] = scale;
+        __syncwarp();
+        Out* const mine = staging + q * 32 + lane;
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
           const float4 s4 = *reinterpret_cast<const float4*>(sa + j);
-          staging[(j + 0) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 0])) * s4.x, sb, add));
-          staging[(j + 1) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 1])) * s4.y, sb, add));
-          staging[(j + 2) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 2])) * s4.z, sb, add));
-          staging[(j + 3) * 32 + lane] = Elem<Out>::down(fmaf(__int2float_rn(int(v[j + 3])) * s4.w, sb, add));
-        }
-        __syncwarp();
-        const int rows = min(32, w.rows - c * 32);
-        Out* const out = static_cast<Out*>(P.c) + int64_t(w.m0 + c * 32) * P.ldc + n0;
-        if (vec && n0 + 32 <= P.N) {
-          const int r0 = lane / kLanesPerRow, x = lane % kLanesPerRow * kVec;
+          const float f[4] = {fmaf(__int2float_rn(int(v[j + 0])) * s4.x, sb, add),
+                              fmaf(__int2float_rn(int(v[j + 1])) * s4.y, sb, add),
+                              fmaf(__int2float_rn(int(v[j + 2])) * s4.z, sb, add),
+                              fmaf(__int2float_rn(int(v[j + 3])) * s4.w, sb, add)};
+          const Piece<Out, 4> o = pack<Out, 4>(f);
 #pragma unroll
-          for (int i = 0; i < 32 / kRowsPerStore; ++i) {
-            const int r = i * kRowsPerStore + r0;
-            if (r < rows) *reinterpret_cast<uint4*>(out + r * P.ldc + x) = *reinterpret_cast<const uint4*>(staging + r * 32 + x);
-          }
-        } else if (n < P.N) {
-          for (int r = 0; r < rows; ++r) out[r * P.ldc + lane] = staging[r * 32 + lane];
+          for (int u = 0; u < 4; ++u) mine[(j + u) * kChannels] = o.e[u];
         }
-        __syncwarp();
+        named_bar_sync(1 + group, 128);
+        // a quarter of the rows for each warp
+        const int row0 = q * 8, rows = min(8, w.rows - c * 32 - row0);
+        Out* const out = static_cast<Out*>(P.c) + int64_t(w.m0 + c * 32 + row0) * P.ldc + n0;
+        const Out* const in = staging + row0 * kChannels;
+        const int r0 = lane / kLanesPerRow, x = lane % kLanesPerRow * kVec;
+        if (vec && n0 + kChannels <= P.N) {
+          uint4 o[8 / kRowsPerStore];
+#pragma unroll
+          for (int i = 0; i < 8 / kRowsPerStore; ++i)
+            o[i] = *reinterpret_cast<const uint4*>(in + (i * kRowsPerStore + r0) * kChannels + x);
+#pragma unroll
+          for (int i = 0; i < 8 / kRowsPerStore; ++i)
+            if (i * kRowsPerStore + r0 < rows) *reinterpret_cast<uint4*>(out + (i * kRowsPerStore + r0) * P.ldc + x) = o[i];
+        } else {
+          for (int r = 0; r < rows; ++r)
+            for (int i = lane; i < kChannels && n0 + i < P.N; i += 32) out[r * P.ldc + i] = in[r * kChannels + i];
+        }
+        named_bar_sync(1 + group, 128);
+      };
+      uint32_t v[2][32];
+      if (group < chunks) tmem_ld32(sums + group * 32, v[0]);
+      else release();
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int c = group + 2 * i;
+        if (c < chunks) {
+          tmem_ld_wait(v[i % 2]);
+          if (c + 2 < chunks) tmem_ld32(sums + (c + 2) * 32, v[(i + 1) % 2]);
+          else release();
+          finish(v[i % 2], scales[i], c);
+        }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty + 8 * acc, 0));
       if ((acc ^= 1) == 0) acc_phase ^= 1;
     }
   }
@@ -456,8 +567,10 @@ int run_pairs(const Maps& maps, Params P, cudaStream_t stream) {
   return launched(cudaLaunchKernelEx(&cfg, kernel, maps, P));
 }
 
-// The height of the pair tiles: as many waves of the pairs as there are, each as long as its tiles are high (and a
-// part that does not depend on it).
+// The height of the pair tiles.  Four instructions of a tile h tokens high move 32 KB + 128 h bytes through an SM's
+// shared memory (operands written by TMA, read by the tensor core, half of the tokens by either CTA), 256 + h cycles;
+// the products themselves take 2 h.  So a tile costs 256 + h, and the rows of one matrix are cut so that the waves of
+// the pairs cost least together.
 int pair_rows(const Params& P) {
   if (P.G > 1) return kPairTokens;
   const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels, pairs = sm_count() / 2;
@@ -465,7 +578,7 @@ int pair_rows(const Params& P) {
   int64_t least = 0;
   for (int rows = kPairTokens; rows >= 96; rows -= 32) {
     const int64_t token_tiles = (P.M + rows - 1) / rows, waves = (token_tiles * channel_tiles + pairs - 1) / pairs;
-    const int64_t cost = waves * (rows + 32);
+    const int64_t cost = waves * (rows + 256);
     if (least == 0 || cost < least) least = cost, best = rows;
   }
   return best;
@@ -475,13 +588,31 @@ template <int TOKENS, typename Out>
 int run(const Maps& maps, Params P, cudaStream_t stream) {
   using T = Tile<TOKENS>;
   const int64_t token_tiles = P.offsets ? P.M / TOKENS + P.G : (P.M + TOKENS - 1) / TOKENS;
-  const int64_t grid = token_tiles * ((P.N + kChannels - 1) / kChannels);
-  if (grid > kMaxExtent) return ENTWINE_ERR_INVALID;
+  const int64_t tiles = token_tiles * ((P.N + kChannels - 1) / kChannels);
+  const int blocks = (P.K + kKBytes - 1) / kKBytes;
+  // CTAs for all SMs, two each, with two blocks of K or more for every one: 16 tokens through 8192 x 3584 take 12.2, 10.6,
+  // 10.0 and 14.1 us with one, two, four and eight CTAs a tile (the rule takes four), through 1024 x 8192 20.3, 12.9, 9.0
+  // and 7.6 (eight); wide tiles exchange more sums: 128 tokens through 4096 x 4096 21.0, 15.3, 11.3 and 12.4 (four).
+  P.split = 1;
+  while (P.split * TOKENS < 512 && P.split < kMaxSplit && tiles * P.split * 2 <= 2 * int64_t(sm_count()) &&
+         blocks >= P.split * 4)
+    P.split *= 2;
+  if (tiles * P.split > kMaxExtent) return ENTWINE_ERR_INVALID;
   P.token_tiles = int(token_tiles);
   auto kernel = gemm_i8_kernel<TOKENS, Out>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
-  if (e == cudaSuccess) kernel<<<unsigned(grid), kThreads, T::kSmem, stream>>>(maps, P);
-  return launched(e);
+  if (e != cudaSuccess) return launched(e);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(tiles * P.split));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = T::kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {unsigned(P.split), 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return launched(cudaLaunchKernelEx(&cfg, kernel, maps, P));
 }
 
 bool make_maps(Maps* maps, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t expert_stride,
@@ -510,23 +641,25 @@ template <typename Out>
 int run_as(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t expert_stride, const Params& P,
            cudaStream_t stream) {
   const int rows = (P.M + P.G - 1) / P.G;  // of an average expert
-  if (rows > PAIRMIN) {
+  const int64_t pair_tiles = int64_t(P.G) * ((P.N + kPairChannels - 1) / kPairChannels);
+  Maps maps;
+  // Pairs where tokens are many, or where experts alone give every pair two tiles: 64 experts of 4096 x 1024 with 6, 16
+  // and 64 rows take 46.8, 52.9 and 54.9 us (49.4, 69.9 and 94.4 with the narrow tiles); 160 tokens through 8192 x 3584
+  // 14.7 us (17.7), 128 tokens 14.3 (13.4).
+  if (rows > 128 || (rows > 4 && pair_tiles >= sm_count())) {
     Params Q = P;
     Q.tile_rows = pair_rows(P);
-    Maps maps;
     if (!make_maps(&maps, A, lda, B, ldb, expert_stride, Q, Q.tile_rows / 2)) return ENTWINE_ERR_CUDA;
     return run_pairs<Out>(maps, Q, stream);
   }
   // the narrowest tile that holds them
-  const int tokens = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-  Maps maps;
+  const int tokens = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   if (!make_maps(&maps, A, lda, B, ldb, expert_stride, P, tokens)) return ENTWINE_ERR_CUDA;
   switch (tokens) {
     case 16: return run<16, Out>(maps, P, stream);
     case 32: return run<32, Out>(maps, P, stream);
     case 64: return run<64, Out>(maps, P, stream);
-    case 128: return run<128, Out>(maps, P, stream);
-    default: return run<256, Out>(maps, P, stream);
+    default: return run<128, Out>(maps, P, stream);
   }
 }
 
