@@ -1,15 +1,18 @@
-"""Builds the C-ABI library in-tree with nvcc for sm_100a: libentwine.so next to this file."""
+"""Builds the C-ABI library in-tree with nvcc for sm_100a (libentwine.so next to this file), and with the C compiler the
+extension module that marshals the operators' arguments (_opcalls.so)."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libentwine.so")
+OPCALLS = os.path.join(HERE, "_opcalls.so")
 INCLUDE = os.path.join(ROOT, "include")
 SOURCES = ["plan.cc", "entwine_kernels.cu", "quant.cu", "moe.cu", "gemm_i8.cu"]
 
@@ -38,7 +41,7 @@ def _source_hash() -> str:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(STAMP):
+    if not all(os.path.exists(f) for f in (LIB, OPCALLS, STAMP)):
         return True
     with open(STAMP) as f:
         return f.read().strip() != _source_hash()
@@ -56,6 +59,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
         # the sources side by side, then one link
         objs = [os.path.join(tmp, src + ".o") for src in SOURCES]
         cmds = [[_nvcc(), *flags, "-x", "cu", "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
+        cmds.append([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I",
+                     sysconfig.get_paths()["include"], os.path.join(CSRC, "opcalls.c"), "-o", OPCALLS])
         cmds = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in cmds]
         outs = [(p.communicate()[0], p.returncode) for p in cmds]
         if all(rc == 0 for _, rc in outs):
@@ -65,7 +70,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose or rc != 0:
             sys.stderr.write(text)
     if any(rc != 0 for _, rc in outs):
-        raise RuntimeError("nvcc failed building libentwine.so")
+        raise RuntimeError("building libentwine.so or _opcalls.so failed")
     with open(STAMP, "w") as f:
         f.write(_source_hash() + "\n")
     return LIB

@@ -7,7 +7,8 @@ Device-buffer arguments are torch CUDA tensors (bf16, contiguous) or raw integer
 
 The operators beside the fused call (quant_i8, moe_dispatch and the others at the end of this file) take
 torch CUDA tensors only: sizes, row distances and element types are read from them, and what does not fit
-together is refused with EntwineError(ERR_INVALID) before anything is launched.
+together is refused with EntwineError(ERR_INVALID) before anything is launched.  Their arguments are marshalled by an
+extension module (csrc/opcalls.c), because their smallest calls are as short as a ctypes call.
 """
 from __future__ import annotations
 
@@ -24,6 +25,10 @@ if not os.path.exists(LIB_PATH):
         f"{LIB_PATH} is missing: build it with `python -m paper_2609_11562_b200.build` "
         "(or __graft_entry__.build()); this package has no CPU fallback")
 _lib = ctypes.CDLL(LIB_PATH)
+try:
+    from . import _opcalls
+except ImportError as e:
+    raise ImportError("_opcalls.so is missing: build it with `python -m paper_2609_11562_b200.build`") from e
 
 ORDER_ROW_MAJOR, ORDER_INTERLEAVED, ORDER_M_MAJOR = 0, 1, 2
 OK, ERR_INVALID, ERR_RESOURCES, ERR_CUDA, ERR_TIMEOUT, ERR_INTERNAL = 0, -1, -2, -3, -4, -5
@@ -113,8 +118,7 @@ def _ptr(t):
 
 def _stream(s):
     if s is None:
-        # the handle alone: building a Stream object takes 3 us, as long as a short kernel
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -270,110 +274,35 @@ class Plan:
 # operators beside the fused call (include/entwine_ops.h)
 # ------------------------------------------------------------------------------------------
 DTYPE_BF16, DTYPE_FP16, DTYPE_FP32, DTYPE_I8 = 0, 1, 2, 3
-_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16, torch.float32: DTYPE_FP32, torch.int8: DTYPE_I8}
-_FLOATING = (torch.bfloat16, torch.float16, torch.float32)
 
 
-_I8, _I32, _FP32, _IDS = (torch.int8,), (torch.int32,), (torch.float32,), (torch.int32, torch.int64)
-_ANY = tuple(_DTYPES)
+def _bind_ops():
+    """Hands the marshalling module the library's entry points and what it asks torch for."""
+    addresses = {name: ctypes.cast(getattr(_lib, name), _vp).value for name in OP_SYMBOLS}
+    dtypes = (torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.int32, torch.int64)
+    # (the current stream's handle: building a Stream object takes 3 us, as long as a short kernel)
+    _opcalls.bind(addresses, dtypes, EntwineError, torch.cuda.current_device, torch._C._cuda_getCurrentRawStream)
 
 
-def _refuse(what):
-    raise EntwineError(ERR_INVALID, what)
-
-
-def _device(t, name):
-    """The current device, on which this first argument has to lie; the others are compared with it."""
-    dev = t.get_device() if isinstance(t, torch.Tensor) else -1
-    if dev < 0 or dev != torch.cuda.current_device():
-        _refuse(f"{name} must be a tensor on the current CUDA device")
-    return dev
-
-
-def _wrong(t, name, dtypes, dev, what):
-    """Refuses an argument, saying what is wrong with it."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
-        _refuse(f"{name} must be a tensor on the current CUDA device")
-    if t.dtype not in dtypes:
-        _refuse(f"{name} must be of {' or '.join(map(str, dtypes))}, not {t.dtype}")
-    _refuse(f"{name} must be {what}, not {tuple(t.shape)} with strides {t.stride()}")
-
-
-# (A short kernel takes as long as these checks: they read each property once and leave the wording to _wrong.)
-def _matrix(t, name, dtypes, dev):
-    """A matrix whose rows are contiguous and do not overlap: (rows, cols, distance between two rows)."""
-    try:
-        if t.get_device() == dev and t.dtype in dtypes:
-            rows, cols = t.shape
-            ld, step = t.stride()
-            if (step == 1 or cols <= 1) and (ld >= cols or rows <= 1):
-                return rows, cols, ld if ld > cols else cols
-    except (AttributeError, ValueError):
-        pass
-    _wrong(t, name, dtypes, dev, "a matrix of contiguous rows that do not overlap")
-
-
-def _result(t, name, dtypes, dev, rows, cols):
-    """The same for a matrix of known size: the distance between two rows."""
-    r, c, ld = _matrix(t, name, dtypes, dev)
-    if r != rows or c != cols:
-        _wrong(t, name, dtypes, dev, f"{(rows, cols)}")
-    return ld
-
-
-def _dense(t, name, dtypes, dev, *shape):
-    """A contiguous tensor of this shape: its address."""
-    try:
-        if t.get_device() == dev and t.dtype in dtypes and t.shape == shape and t.is_contiguous():
-            return t.data_ptr()
-    except AttributeError:
-        pass
-    _wrong(t, name, dtypes, dev, f"contiguous and {shape}")
+_bind_ops()
 
 
 def quant_i8(x, q, scale, stream=None):
     """Rows to int8 with a scale each: scale = amax / 127, q = rint(127 x / amax), ties to even.
     x [M, K] bf16, fp16 or fp32; q [M, K] int8; scale [M] fp32."""
-    dev = _device(x, "x")
-    rows, cols, ldx = _matrix(x, "x", _FLOATING, dev)
-    ldq = _result(q, "q", _I8, dev, rows, cols)
-    _check(_lib.entwine_quant_i8(x.data_ptr(), _DTYPES[x.dtype], rows, cols, ldx, q.data_ptr(), ldq,
-                                 _dense(scale, "scale", _FP32, dev, rows), _stream(stream)), "entwine_quant_i8")
+    _opcalls.quant_i8(x, q, scale, stream)
 
 
 def gemm_i8(a, scale_a, b, scale_b, out, bias=None, stream=None):
     """out[m, n] = scale_a[m] scale_b[n] sum_k a[m, k] b[n, k] (+ bias[n]).  a [M, K], b [N, K] int8 with rows on 16-byte
     boundaries; scale_a [M], scale_b [N], bias [N] fp32; out [M, N] bf16, fp16 or fp32."""
-    dev = _device(a, "a")
-    M, K, lda = _matrix(a, "a", _I8, dev)
-    N, Kb, ldb = _matrix(b, "b", _I8, dev)
-    if K != Kb:
-        _refuse("a and b must have rows of one length")
-    ldc = _result(out, "out", _FLOATING, dev, M, N)
-    _check(_lib.entwine_gemm_i8(a.data_ptr(), lda, _dense(scale_a, "scale_a", _FP32, dev, M), b.data_ptr(), ldb,
-                                _dense(scale_b, "scale_b", _FP32, dev, N),
-                                None if bias is None else _dense(bias, "bias", _FP32, dev, N), out.data_ptr(),
-                                _DTYPES[out.dtype], ldc, M, N, K, _stream(stream)), "entwine_gemm_i8")
+    _opcalls.gemm_i8(a, scale_a, b, scale_b, out, bias, stream)
 
 
 def gemm_i8_grouped(a, scale_a, b, scale_b, offsets, out, bias=None, stream=None):
     """Rows [offsets[g], offsets[g+1]) of a times expert g's matrix: b [G, N, K] int8, scale_b and bias [G, N] fp32,
     offsets [G+1] int32 on the device; the rest as gemm_i8.  Rows of no expert are left as they were."""
-    dev = _device(a, "a")
-    M, K, lda = _matrix(a, "a", _I8, dev)
-    if not isinstance(b, torch.Tensor) or b.dim() != 3 or b.get_device() != dev or b.dtype != torch.int8 or b.shape[2] != K:
-        _wrong(b, "b", _I8, dev, f"[G, N, {K}]")
-    G, N, _ = b.shape
-    step, ldb, one = b.stride()
-    if (one != 1 and K > 1) or (ldb < K and N > 1) or (step < (N - 1) * ldb + K and G > 1):
-        _wrong(b, "b", _I8, dev, "matrices of contiguous rows that do not overlap")
-    ldc = _result(out, "out", _FLOATING, dev, M, N)
-    _check(_lib.entwine_gemm_i8_grouped(a.data_ptr(), lda, _dense(scale_a, "scale_a", _FP32, dev, M), b.data_ptr(),
-                                        ldb if ldb > K else K, step, _dense(scale_b, "scale_b", _FP32, dev, G, N),
-                                        None if bias is None else _dense(bias, "bias", _FP32, dev, G, N),
-                                        _dense(offsets, "offsets", _I32, dev, G + 1), out.data_ptr(),
-                                        _DTYPES[out.dtype], ldc, M, N, K, G, _stream(stream)),
-           "entwine_gemm_i8_grouped")
+    _opcalls.gemm_i8_grouped(a, scale_a, b, scale_b, offsets, out, bias, stream)
 
 
 def ops_status(stream=None):
@@ -381,63 +310,25 @@ def ops_status(stream=None):
     _check(_lib.entwine_ops_status(_stream(stream)), "entwine_ops_status")
 
 
-def _assignments(t, name):
-    if not isinstance(t, torch.Tensor) or t.dim() != 2:
-        _refuse(f"{name} must be a tensor [T, k]")
-    return t.shape
-
-
 def moe_dispatch(x, ids, n_experts, rows, offsets, row_of, x_scale=None, row_scale=None, stream=None):
     """Tokens sorted by expert.  x [T, H] bf16, fp16, fp32 or int8; ids [T, k] int32 or int64, an id outside
     [0, n_experts) drops the assignment; rows [T*k, H]; offsets [n_experts+1] int32; row_of [T, k] int32 (-1:
     dropped); x_scale [T] -> row_scale [T*k] fp32, both or neither.  Rows behind offsets[-1] are left as they were."""
-    dev = _device(x, "x")
-    T, H, ldx = _matrix(x, "x", _ANY, dev)
-    _, k = _assignments(ids, "ids")
-    ldr = _result(rows, "rows", (x.dtype,), dev, T * k, H)
-    if x_scale is not None or row_scale is not None:
-        x_scale, row_scale = _dense(x_scale, "x_scale", _FP32, dev, T), _dense(row_scale, "row_scale", _FP32, dev, T * k)
-    _check(_lib.entwine_moe_dispatch(x.data_ptr(), _DTYPES[x.dtype], T, H, ldx, x_scale,
-                                     _dense(ids, "ids", _IDS, dev, T, k), ids.dtype == torch.int64, k, n_experts,
-                                     rows.data_ptr(), ldr, row_scale,
-                                     _dense(offsets, "offsets", _I32, dev, n_experts + 1),
-                                     _dense(row_of, "row_of", _I32, dev, T, k), _stream(stream)), "entwine_moe_dispatch")
+    _opcalls.moe_dispatch(x, ids, n_experts, rows, offsets, row_of, x_scale, row_scale, stream)
 
 
 def moe_dispatch_bwd(d_rows, row_of, dx, stream=None):
     """Gradient of moe_dispatch: dx[t] = sum_j d_rows[row_of[t, j]] in fp32, j ascending.  d_rows [n, H], dx [T, H]."""
-    dev = _device(d_rows, "d_rows")
-    n, H, ldr = _matrix(d_rows, "d_rows", _FLOATING, dev)
-    T, k = _assignments(row_of, "row_of")
-    ldx = _result(dx, "dx", (d_rows.dtype,), dev, T, H)
-    _check(_lib.entwine_moe_dispatch_bwd(d_rows.data_ptr(), _DTYPES[d_rows.dtype], n, H, ldr,
-                                         _dense(row_of, "row_of", _I32, dev, T, k), T, k, dx.data_ptr(), ldx,
-                                         _stream(stream)), "entwine_moe_dispatch_bwd")
+    _opcalls.moe_dispatch_bwd(d_rows, row_of, dx, stream)
 
 
 def moe_combine(y, weights, row_of, out, stream=None):
     """out[t] = sum_j weights[t, j] y[row_of[t, j]] in fp32, j ascending.  y [n, H], out [T, H] of one type, weights
     [T, k] fp32."""
-    dev = _device(y, "y")
-    n, H, ldy = _matrix(y, "y", _FLOATING, dev)
-    T, k = _assignments(row_of, "row_of")
-    ldo = _result(out, "out", (y.dtype,), dev, T, H)
-    _check(_lib.entwine_moe_combine(y.data_ptr(), _DTYPES[y.dtype], n, H, ldy, _dense(weights, "weights", _FP32, dev, T, k),
-                                    _dense(row_of, "row_of", _I32, dev, T, k), T, k, out.data_ptr(), ldo,
-                                    _stream(stream)), "entwine_moe_combine")
+    _opcalls.moe_combine(y, weights, row_of, out, stream)
 
 
 def moe_combine_bwd(dout, y, weights, row_of, dy, dw, stream=None):
     """Gradients of moe_combine: dy[row_of[t, j]] = weights[t, j] dout[t], dw[t, j] = <dout[t], y[row_of[t, j]]>
     (fp32; 0 where dropped).  Rows of dy that no assignment names are left as they were."""
-    dev = _device(dout, "dout")
-    T, H, ldo = _matrix(dout, "dout", _FLOATING, dev)
-    _, k = _assignments(row_of, "row_of")
-    n, Hy, ldy = _matrix(y, "y", (dout.dtype,), dev)
-    if Hy != H:
-        _refuse("y must have rows as long as dout's")
-    lddy = _result(dy, "dy", (dout.dtype,), dev, n, H)
-    _check(_lib.entwine_moe_combine_bwd(dout.data_ptr(), _DTYPES[dout.dtype], T, H, ldo, y.data_ptr(), n, ldy,
-                                        _dense(weights, "weights", _FP32, dev, T, k),
-                                        _dense(row_of, "row_of", _I32, dev, T, k), k, dy.data_ptr(), lddy,
-                                        _dense(dw, "dw", _FP32, dev, T, k), _stream(stream)), "entwine_moe_combine_bwd")
+    _opcalls.moe_combine_bwd(dout, y, weights, row_of, dy, dw, stream)

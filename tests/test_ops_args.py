@@ -112,21 +112,33 @@ class _Tensor(torch.Tensor):
         return self.place
 
 
-def test_binding_refuses_tensors_of_another_device(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+_I, _V = ctypes.c_int64, ctypes.c_void_p
+
+
+@pytest.fixture
+def recorded():
+    """The binding with the library replaced by functions that note their names, and device 0 as the current one."""
+    calls, keep, addresses = [], [], {}
+    for name in E.OP_SYMBOLS:
+        fn = ctypes.CFUNCTYPE(ctypes.c_int, *E._OP_ARGS[name])(lambda *a, name=name: calls.append((name, a)) or E.OK)
+        keep.append(fn)
+        addresses[name] = ctypes.cast(fn, _V).value
+    dtypes = (torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.int32, torch.int64)
+    E._opcalls.bind(addresses, dtypes, E.EntwineError, lambda: 0, lambda dev: 0)
+    yield calls
+    E._bind_ops()
+
+
+def test_binding_refuses_tensors_of_another_device(recorded):
     x, q, s = torch.zeros(4, 8), torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4)
     for devices in ((1, 0, 0), (0, 1, 0), (0, 0, 1)):
         args = [_Tensor.on(t, d) for t, d in zip((x, q, s), devices)]
         with pytest.raises(E.EntwineError, match="current CUDA device"):
             E.quant_i8(*args, stream=0)
+    assert not recorded
 
 
-def test_binding_refuses_what_does_not_fit(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    calls = []
-    for name in E.OP_SYMBOLS:
-        if hasattr(L, name):
-            monkeypatch.setattr(L, name, lambda *a, name=name: calls.append(name) or E.OK)
+def test_binding_refuses_what_does_not_fit(recorded):
     on = lambda t: _Tensor.on(t, 0)  # noqa: E731
     f = lambda *s: on(torch.zeros(*s))  # noqa: E731
     i8, i32 = lambda *s: on(torch.zeros(*s, dtype=torch.int8)), lambda *s: on(torch.zeros(*s, dtype=torch.int32))  # noqa: E731
@@ -174,7 +186,60 @@ def test_binding_refuses_what_does_not_fit(monkeypatch):
         with pytest.raises(E.EntwineError) as e:
             call()
         assert e.value.code == E.ERR_INVALID, i
-    assert not calls  # nothing reached the library
-    E.quant_i8(on(torch.zeros(4, 16)[:, :8]), i8(4, 8), f(4), stream=0)
-    E.moe_dispatch(f(4, 8), i32(4, 2), 3, f(8, 8), i32(4), i32(4, 2), stream=0)
-    assert calls == ["entwine_quant_i8", "entwine_moe_dispatch"]
+    assert not recorded  # nothing reached the library
+
+
+def test_binding_passes_what_fits(recorded):
+    on = lambda t: _Tensor.on(t, 0)  # noqa: E731
+    f = lambda *s: on(torch.zeros(*s))  # noqa: E731
+    i8, i32 = lambda *s: on(torch.zeros(*s, dtype=torch.int8)), lambda *s: on(torch.zeros(*s, dtype=torch.int32))  # noqa: E731
+    x, q, scale = on(torch.zeros(4, 16)[:, :8]), i8(4, 8), f(4)
+    E.quant_i8(x, q, scale, stream=7)
+    assert recorded.pop() == ("entwine_quant_i8", (x.data_ptr(), E.DTYPE_FP32, 4, 8, 16, q.data_ptr(), 8, scale.data_ptr(), 7))
+    E.quant_i8(x, q, scale)                             # the current stream, here the default one (a null handle)
+    assert recorded.pop()[1][-1] is None
+    a, b, sb, out, bias = i8(4, 16), on(torch.zeros(6, 48, dtype=torch.int8)[:, :16]), f(6), f(4, 6), f(6)
+    E.gemm_i8(a, scale, b, sb, out, bias=bias, stream=0)
+    assert recorded.pop() == ("entwine_gemm_i8", (a.data_ptr(), 16, scale.data_ptr(), b.data_ptr(), 48, sb.data_ptr(), bias.data_ptr(),
+                                                  out.data_ptr(), E.DTYPE_FP32, 6, 4, 6, 16, None))
+    e, se, off = on(torch.zeros(3, 6, 32, dtype=torch.int8)[:, :, :16]), f(3, 6), i32(4)
+    E.gemm_i8_grouped(a, scale, e, se, off, out, stream=0)
+    assert recorded.pop() == ("entwine_gemm_i8_grouped", (a.data_ptr(), 16, scale.data_ptr(), e.data_ptr(), 32, 192, se.data_ptr(), None,
+                                                          off.data_ptr(), out.data_ptr(), E.DTYPE_FP32, 6, 4, 6, 16, 3, None))
+    t, ids, rows, row_of = f(4, 8), on(torch.zeros(4, 2, dtype=torch.int64)), f(8, 8), i32(4, 2)
+    E.moe_dispatch(t, ids, 3, rows, off, row_of, stream=0)
+    assert recorded.pop() == ("entwine_moe_dispatch", (t.data_ptr(), E.DTYPE_FP32, 4, 8, 8, None, ids.data_ptr(), 1, 2, 3, rows.data_ptr(),
+                                                       8, None, off.data_ptr(), row_of.data_ptr(), None))
+    rs = f(8)
+    E.moe_dispatch(t, i32(4, 2), 3, rows, off, row_of, x_scale=scale, row_scale=rs, stream=0)
+    got = recorded.pop()[1]
+    assert (got[5], got[7], got[12]) == (scale.data_ptr(), 0, rs.data_ptr())
+    E.moe_dispatch_bwd(rows, row_of, t, stream=0)
+    assert recorded.pop() == ("entwine_moe_dispatch_bwd", (rows.data_ptr(), E.DTYPE_FP32, 8, 8, 8, row_of.data_ptr(), 4, 2, t.data_ptr(), 8, None))
+    w, dw = f(4, 2), f(4, 2)
+    E.moe_combine(rows, w, row_of, t, stream=0)
+    assert recorded.pop() == ("entwine_moe_combine", (rows.data_ptr(), E.DTYPE_FP32, 8, 8, 8, w.data_ptr(), row_of.data_ptr(), 4, 2, t.data_ptr(),
+                                                      8, None))
+    dy = f(8, 8)
+    E.moe_combine_bwd(t, rows, w, row_of, dy, dw, stream=0)
+    assert recorded.pop() == ("entwine_moe_combine_bwd", (t.data_ptr(), E.DTYPE_FP32, 4, 8, 8, rows.data_ptr(), 8, 8, w.data_ptr(), row_of.data_ptr(),
+                                                          2, dy.data_ptr(), 8, dw.data_ptr(), None))
+    assert not recorded
+
+
+def test_an_error_of_the_library_is_raised(recorded):
+    E._opcalls.bind({n: ctypes.cast(keep, _V).value for n, keep in _failing().items()},
+                    (torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.int32, torch.int64), E.EntwineError, lambda: 0, lambda dev: 0)
+    on = lambda t: _Tensor.on(t, 0)  # noqa: E731
+    with pytest.raises(E.EntwineError, match="entwine_quant_i8") as e:
+        E.quant_i8(on(torch.zeros(4, 8)), on(torch.zeros(4, 8, dtype=torch.int8)), on(torch.zeros(4)))
+    assert e.value.code == E.ERR_CUDA
+
+
+_kept = {}
+
+
+def _failing():
+    for name in E.OP_SYMBOLS:
+        _kept[name] = ctypes.CFUNCTYPE(ctypes.c_int, *E._OP_ARGS[name])(lambda *a: E.ERR_CUDA)
+    return _kept
