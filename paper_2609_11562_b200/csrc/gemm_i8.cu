@@ -52,13 +52,14 @@ struct Params {
 
 // Bounded wait for a phase of a barrier.
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const unsigned long long t0 = globaltimer_ns();
+  unsigned long long t0 = 0;
   for (;;) {
 #pragma unroll 1
-    for (int i = 0; i < 64; ++i)
+    for (int i = 0; i < 128; ++i)
       if (mbar_try_wait(bar, parity)) return true;
-    if (globaltimer_ns() - t0 > kWaitBudgetNs) {
+    const unsigned long long now = globaltimer_ns();
+    if (t0 == 0) t0 = now;
+    if (now - t0 > kWaitBudgetNs) {
       g_wait_failed = 1;
       return false;
     }
@@ -133,9 +134,12 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
   auto load = [&]() {
     const int s = issued % S;
     const uint32_t at = ring + s * T::kStageBytes;
-    mbar_arrive_expect_tx(full + 8 * s, T::kStageBytes);
-    tma_load_3d(at, &maps.b, (first + issued) * kKBytes, n0, g, full + 8 * s);
-    tma_load_2d(at + kChannels * kKBytes, &maps.a, (first + issued) * kKBytes, m0, full + 8 * s);
+    if (elect_one()) {
+      mbar_arrive_expect_tx(full + 8 * s, T::kStageBytes);
+      tma_load_3d(at, &maps.b, (first + issued) * kKBytes, n0, g, full + 8 * s);
+      tma_load_2d(at + kChannels * kKBytes, &maps.a, (first + issued) * kKBytes, m0, full + 8 * s);
+    }
+    __syncwarp();
     ++issued;
   };
   if (warp == 0) {
@@ -157,9 +161,10 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
       }
       mbar_init(done, 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      if (g >= 0)  // the first loads need nothing that the rest of the CTA prepares
-        while (issued < min(S, blocks)) load();
     }
+    __syncwarp();
+    if (g >= 0)  // the first loads need nothing that the rest of the CTA prepares
+      while (issued < min(S, blocks)) load();
   }
   if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), T::kTmemCols);
   tc_fence_before();
@@ -183,32 +188,35 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
     add[i] = n + i < P.N && P.bias ? P.bias[int64_t(g) * P.N + n + i] : 0.0f;
   }
 
-  if (threadIdx.x == 0) {
+  if (warp == 0) {
     while (issued < blocks) {
-      if (!(ok = wait_bar(empty + 8 * (issued % S), (issued / S - 1) & 1))) break;
+      if (!(ok = __all_sync(0xffffffffu, wait_bar(empty + 8 * (issued % S), (issued / S - 1) & 1)))) break;
       load();
     }
-  } else if (threadIdx.x == 32) {
+  } else if (warp == 1) {
     // int32 accumulator, signed 8-bit operands, both K-major
     constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (uint32_t(TOKENS >> 3) << 17) |
                                (uint32_t(kChannels >> 4) << 24);
     for (int i = 0; i < blocks; ++i) {
       const int s = i % S;
-      if (!(ok = wait_bar(full + 8 * s, (i / S) & 1))) break;
+      if (!(ok = __all_sync(0xffffffffu, wait_bar(full + 8 * s, (i / S) & 1)))) break;
       tc_fence_after();
       const uint32_t at = ring + s * T::kStageBytes;
       const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
+      if (elect_one()) {
 #pragma unroll
-      for (int k = 0; k < kKBytes / 32; ++k) umma_i8(tmem, da + 2 * k, db + 2 * k, idesc, i > 0 || k > 0);
-      tc_commit(empty + 8 * s);
+        for (int k = 0; k < kKBytes / 32; ++k) umma_i8(tmem, da + 2 * k, db + 2 * k, idesc, i > 0 || k > 0);
+        tc_commit(empty + 8 * s);
+      }
+      __syncwarp();
     }
-    tc_commit(done);
+    if (elect_one()) tc_commit(done);
   }
   __syncwarp();
   ok = wait_bar(done, 0) && ok;
   tc_fence_after();
   ok = !__syncthreads_or(!ok);
-  if (!ok && threadIdx.x == 0) {
+  if (!ok && warp == 0) {
     // copies still under way end before the CTA does
     for (int i = issued > S ? issued - S : 0; i < issued; ++i)
       if (!wait_bar(full + 8 * (i % S), (i / S) & 1)) break;
@@ -393,33 +401,33 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
   PairWalk walk{groups, channel_tiles};
 
   if (warp == 0) {
-    if (lane == 0) {
-      const uint32_t bytes = kChannels * kKBytes + P.tile_rows / 2 * kKBytes;  // that each CTA brings
-      int stage = 0;
-      uint32_t phase = 0;
-      long long issued = 0;
-      bool ok = true;
-      for (int t = pair; ok && t < total; t += pairs) {
-        const PairTile w = walk.at(t);
-        const int half = (w.rows + 31) / 32 * 16;
-        for (int b = 0; b < blocks; ++b) {
-          if (!(ok = wait_bar(empty + 8 * stage, phase ^ 1))) break;
-          const uint32_t at = ring + stage * kPairStageBytes, bar = map_to_cta(full + 8 * stage, 0);
+    const uint32_t bytes = kChannels * kKBytes + P.tile_rows / 2 * kKBytes;  // that each CTA brings
+    int stage = 0, in_flight = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int t = pair; ok && t < total; t += pairs) {
+      const PairTile w = walk.at(t);
+      const int n0 = w.n0 + rank * kChannels, m0 = w.m0 + rank * ((w.rows + 31) / 32 * 16);
+      for (int b = 0; b < blocks; ++b) {
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(empty + 8 * stage, phase ^ 1)))) break;
+        const uint32_t at = ring + stage * kPairStageBytes, bar = map_to_cta(full + 8 * stage, 0);
+        if (elect_one()) {
           if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * bytes);
-          tma_load_3d_pair(at, &maps.b, b * kKBytes, w.n0 + rank * kChannels, w.g, bar);
-          tma_load_2d_pair(at + kChannels * kKBytes, &maps.a, b * kKBytes, w.m0 + rank * half, bar);
-          ++issued;
-          if (++stage == S) stage = 0, phase ^= 1;
+          tma_load_3d_pair(at, &maps.b, b * kKBytes, n0, w.g, bar);
+          tma_load_2d_pair(at + kChannels * kKBytes, &maps.a, b * kKBytes, m0, bar);
         }
-      }
-      // after a wait that ran out: copies still under way end before the CTA does
-      for (int i = 0; !ok && rank == 0 && i < S && i < issued; ++i) {
-        if (--stage < 0) stage = S - 1, phase ^= 1;
-        if (!wait_bar(full + 8 * stage, phase)) break;
+        __syncwarp();
+        if (in_flight < S) ++in_flight;
+        if (++stage == S) stage = 0, phase ^= 1;
       }
     }
+    // after a wait that ran out: copies still under way end before the CTA does
+    for (int i = 0; !ok && rank == 0 && i < in_flight; ++i) {
+      if (--stage < 0) stage = S - 1, phase ^= 1;
+      if (!wait_bar(full + 8 * stage, phase)) break;
+    }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
@@ -427,25 +435,29 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
       for (int t = pair; ok && t < total; t += pairs, rows = next_rows) {
         const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (uint32_t((rows + 31) / 32 * 4) << 17) |
                                (uint32_t(kPairChannels >> 4) << 24);
-        if (!(ok = wait_bar(tempty + 8 * acc, acc_phase ^ 1))) break;
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(tempty + 8 * acc, acc_phase ^ 1)))) break;
         tc_fence_after();
         const uint32_t d = tmem + acc * kPairTokens;
         for (int b = 0; b < blocks; ++b) {
-          if (!(ok = wait_bar(full + 8 * stage, phase))) break;
+          if (!(ok = __all_sync(0xffffffffu, wait_bar(full + 8 * stage, phase)))) break;
           tc_fence_after();
           const uint32_t at = ring + stage * kPairStageBytes;
           const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
+          if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < kKBytes / 32; ++k) umma_i8_pair(d, da + 2 * k, db + 2 * k, idesc, b > 0 || k > 0);
-          tc_commit_pair(empty + 8 * stage);
+            for (int k = 0; k < kKBytes / 32; ++k) umma_i8_pair(d, da + 2 * k, db + 2 * k, idesc, b > 0 || k > 0);
+            tc_commit_pair(empty + 8 * stage);
+            if (b == blocks - 1) tc_commit_pair(tfull + 8 * acc);
+          }
+          __syncwarp();
           if (++stage == S) stage = 0, phase ^= 1;
           if (b == 0 && t + pairs < total) next_rows = walk.at(t + pairs).rows;  // (while these products run)
         }
-        if (ok) tc_commit_pair(tfull + 8 * acc);
         if ((acc ^= 1) == 0) acc_phase ^= 1;
       }
       if (!ok) {  // products under way end before the TMEM is given back
-        tc_commit_pair(drain);
+        if (elect_one()) tc_commit_pair(drain);
+        __syncwarp();
         wait_bar(drain, 0);
       }
     }
