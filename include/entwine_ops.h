@@ -58,7 +58,8 @@ int entwine_gemm_i8(const void* A, int64_t lda, const float* scale_a, const void
  * entwine_gemm_i8_grouped - the same product with a weight matrix per expert, for rows sorted by expert: rows
  * [offsets[g], offsets[g+1]) of A are multiplied with B[g] and scaled with scale_b[g] (and bias[g]).
  *   offsets [G+1] int32, device memory, non-decreasing, 0 <= offsets[0], offsets[G] <= M (as entwine_moe_dispatch
- *   writes them); a bound outside [0, M] is taken as the nearest inside, a decreasing pair as an empty expert
+ *   writes them); bounds outside [0, M] are taken as the nearest inside, a decreasing pair as an empty expert
+ *   (with decreasing offsets it is not said which of the overlapping rows are computed; nothing else is touched)
  *   B [G][N][K], expert_stride elements from one expert's matrix to the next (a multiple of 16)
  *   scale_b [G][N], bias [G][N] or NULL
  * Rows of C that belong to no expert are left as they were.  1 <= G <= 1024, G * N < 2^31; the rest as above.

@@ -464,9 +464,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
   } else {
     // Epilogue: a warp owns 32 channels (its lane quarter of the accumulator), a lane one of them; groups of four
     // warps take turns at the 32-token chunks of a tile.  Values go through the group's staging, [32 tokens][128
-    // channels], so that whole lines of C are stored: with 64 bytes of a row per store (a warp's own channels) the
-    // requests to L2 were the limit, 6400-7600 cycles a tile.  The scales of a tile are read before its sums are waited
-    // for, a chunk's sums while the chunk before is worked on.
+    // channels], so that whole lines of C are stored.  The scales of a tile are read before its sums are waited for, a
+    // chunk's sums while the chunk before is worked on.  At short K this is what a tile waits for: 4096 x 5120 outputs
+    // of K = 512 take 23 us, 14 without it (twice the epilogue warps: 20, but 5 % more at K >= 1024).
     const int q = warp & 3, group = (warp - 2) / 4;
     constexpr int kTurns = kPairTokens / 64;  // chunks of a tile that a group takes
     Out* const staging = reinterpret_cast<Out*>(smem_raw + (ring - smem_u32(smem_raw)) + S * kPairStageBytes +
@@ -602,9 +602,9 @@ int run(const Maps& maps, Params P, cudaStream_t stream) {
   const int64_t token_tiles = P.offsets ? P.M / TOKENS + P.G : (P.M + TOKENS - 1) / TOKENS;
   const int64_t tiles = token_tiles * ((P.N + kChannels - 1) / kChannels);
   const int blocks = (P.K + kKBytes - 1) / kKBytes;
-  // CTAs for all SMs, two each, with two blocks of K or more for every one: 16 tokens through 8192 x 3584 take 12.2, 10.6,
-  // 10.0 and 14.1 us with one, two, four and eight CTAs a tile (the rule takes four), through 1024 x 8192 20.3, 12.9, 9.0
-  // and 7.6 (eight); wide tiles exchange more sums: 128 tokens through 4096 x 4096 21.0, 15.3, 11.3 and 12.4 (four).
+  // CTAs for all SMs, two each, with two blocks of K or more for every one: 16 tokens through 8192 x 3584 take 11.4,
+  // 10.3, 9.6 and 13.8 us with one, two, four and eight CTAs a tile (the rule takes four), through 1024 x 8192 17.7, 11.7,
+  // 8.3 and 7.3 (eight); wide tiles exchange more sums: 128 tokens through 4096 x 4096 20.5, 15.0, 11.3 and 12.2 (four).
   P.split = 1;
   while (P.split * TOKENS < 512 && P.split < kMaxSplit && tiles * P.split * 2 <= 2 * int64_t(sm_count()) &&
          blocks >= P.split * 4)
@@ -653,12 +653,13 @@ template <typename Out>
 int run_as(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t expert_stride, const Params& P,
            cudaStream_t stream) {
   const int rows = (P.M + P.G - 1) / P.G;  // of an average expert
-  const int64_t pair_tiles = int64_t(P.G) * ((P.N + kPairChannels - 1) / kPairChannels);
+  const int64_t pair_tiles = int64_t(std::min(P.G, P.M)) * ((P.N + kPairChannels - 1) / kPairChannels);
   Maps maps;
-  // Pairs where tokens are many, or where experts alone give every pair two tiles: 64 experts of 4096 x 1024 with 6, 16
-  // and 64 rows take 46.8, 52.9 and 54.9 us (49.4, 69.9 and 94.4 with the narrow tiles); 160 tokens through 8192 x 3584
-  // 14.7 us (17.7), 128 tokens 14.3 (13.4).
-  if (rows > 128 || (rows > 4 && pair_tiles >= sm_count())) {
+  // Pairs where experts alone give every pair two tiles (64 experts of 4096 x 1024 with 4, 6, 16 and 64 rows take 42.2,
+  // 43.6, 47.2 and 52.4 us on pairs, 43.5, 48.4, 67.5 and 90.6 on narrow tiles), and for more than 128 tokens where half
+  // of the pairs get one (160 tokens through 8192 x 3584: 13.1 and 16.2 us; 300 through 1024 x 4096, where they do not,
+  // 13.0 and 10.0).
+  if (rows > 128 ? (rows + 127) / 128 * pair_tiles >= sm_count() / 4 : pair_tiles >= sm_count()) {
     Params Q = P;
     Q.tile_rows = pair_rows(P);
     if (!make_maps(&maps, A, lda, B, ldb, expert_stride, Q, Q.tile_rows / 2)) return ENTWINE_ERR_CUDA;

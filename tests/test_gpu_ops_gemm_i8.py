@@ -52,7 +52,8 @@ def _dtype_id(v):
 
 SHAPES = [(1, 1, 1), (1, 128, 128), (1, 1000, 4096), (2, 7, 15), (15, 129, 16), (16, 8, 127), (17, 300, 129), (31, 128, 1021),
           (33, 513, 640), (64, 256, 256), (65, 100, 64), (100, 1000, 1000), (128, 384, 512), (129, 257, 2049), (200, 96, 96), (255, 640, 160),
-          (256, 512, 1024), (257, 1025, 520), (300, 64, 4096), (511, 130, 33), (1000, 777, 1021), (2049, 1024, 256), (64, 8192, 512)]
+          (256, 512, 1024), (257, 1025, 520), (300, 64, 4096), (511, 130, 33), (1000, 777, 1021), (2049, 1024, 256), (64, 8192, 512),
+          (300, 5000, 200), (129, 8197, 136), (1000, 3000, 1021), (4500, 700, 128), (260, 40000, 48)]
 
 
 @pytest.mark.parametrize("dtype", FLOATING, ids=_dtype_id)
@@ -81,15 +82,15 @@ def test_gemm_i8_pitches_and_exact_sums():
     assert torch.equal(out[:1].double(), a[:1].double() @ b.double().T)
 
 
-@pytest.mark.parametrize("M", [3, 300])
-def test_gemm_i8_largest_sum(M):
+@pytest.mark.parametrize("M,N", [(3, 5), (300, 5), (300, 5000)])
+def test_gemm_i8_largest_sum(M, N):
     """K at its limit and every product at its largest: 2147467264, one step below int32's end in fp32's eyes."""
     K = 131071
     for sign in (1, -1):
         a = torch.full((M, K + 1), -128, dtype=torch.int8, device="cuda")[:, :K]
-        b = torch.full((5, K + 1), -128 if sign > 0 else 127, dtype=torch.int8, device="cuda")[:, :K]
-        out = torch.empty(M, 5, device="cuda")
-        E.gemm_i8(a, torch.ones(M, device="cuda"), b, torch.ones(5, device="cuda"), out)
+        b = torch.full((N, K + 1), -128 if sign > 0 else 127, dtype=torch.int8, device="cuda")[:, :K]
+        out = torch.empty(M, N, device="cuda")
+        E.gemm_i8(a, torch.ones(M, device="cuda"), b, torch.ones(N, device="cuda"), out)
         want = np.float32(128 * 128 * K if sign > 0 else -128 * 127 * K)
         assert bool((out == float(want)).all())
 
@@ -109,7 +110,9 @@ def test_gemm_i8_scales_that_are_not_finite():
 
 # rows per expert: empty experts first, in the middle and last, one row, tile ends, everything in one
 GROUPS = [([0, 3, 0, 1, 16, 17, 0], 128, 128), ([5], 100, 64), ([0, 0, 40, 0], 257, 300), ([1] * 33, 130, 1021), ([64, 65, 63, 0, 128], 384, 512),
-          ([300, 1, 0, 255, 257], 200, 640), ([1000, 0, 0, 24], 129, 96), ([7] * 100 + [0] * 28, 256, 256), ([0, 0, 0], 64, 64), ([513, 700], 512, 160)]
+          ([300, 1, 0, 255, 257], 200, 640), ([1000, 0, 0, 24], 129, 96), ([7] * 100 + [0] * 28, 256, 256), ([0, 0, 0], 64, 64), ([513, 700], 512, 160),
+          ([0, 3, 0, 1, 16, 17, 0, 64, 65, 33, 31, 129, 0], 3333, 192), ([300, 1, 0, 255, 257, 513], 1800, 640), ([1] * 33, 1300, 1021),
+          ([0] * 500 + [40] + [0] * 400 + [1, 2], 1024, 80), ([5000, 0, 70], 2000, 112)]
 
 
 def _grouped(counts, N, K, dtype, bias, spare, seed=0, first=0, expert_pad=0):
@@ -150,10 +153,10 @@ def test_grouped_offsets_out_of_order_or_range_stay_inside():
     _check(out[30:], a[30:], sa[30:], b[3], sb[3], None)
 
 
-@pytest.mark.parametrize("M", [4, 600])
-def test_gemm_i8_repeats_bitwise_and_replays(M):
+@pytest.mark.parametrize("M,N", [(4, 1536), (600, 1536), (600, 2560)])
+def test_gemm_i8_repeats_bitwise_and_replays(M, N):
     """Same bits on every call, in a captured first call, and with two graphs on streams of their own at once."""
-    N, K = 1536, 1408
+    K = 1408
     a, b, sa, sb = _levels(M, K, 1), _levels(N, K, 2), _scales(M, 3), _scales(N, 4)
     out = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
     E.gemm_i8(a, sa, b, sb, out)
