@@ -280,8 +280,9 @@ def _bind_ops():
     """Hands the marshalling module the library's entry points and what it asks torch for."""
     addresses = {name: ctypes.cast(getattr(_lib, name), _vp).value for name in OP_SYMBOLS}
     dtypes = (torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.int32, torch.int64)
-    # (the current stream's handle: building a Stream object takes 3 us, as long as a short kernel)
-    _opcalls.bind(addresses, dtypes, EntwineError, torch.cuda.current_device, torch._C._cuda_getCurrentRawStream)
+    # the current stream's handle where torch gives it alone: building a Stream object takes 3 us, as long as a short kernel
+    stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    _opcalls.bind(addresses, dtypes, EntwineError, torch.cuda.current_device, stream)
 
 
 _bind_ops()

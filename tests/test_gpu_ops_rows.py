@@ -123,7 +123,7 @@ def test_quant_many_rows_and_none():
 
 # ---------------------------------------------------------------------------------------------- sort and return
 ROUTES = [(1, 1, 1, 1), (1, 8, 8, 64), (3, 2, 5, 7), (16, 8, 64, 256), (33, 4, 16, 72), (100, 1, 2, 40), (257, 8, 60, 136),
-          (1000, 6, 1024, 16), (4097, 2, 33, 24), (20000, 4, 128, 8)]
+          (1000, 6, 1024, 16), (4097, 2, 33, 24), (20000, 4, 128, 8), (40, 3, 1024, 16), (256, 8, 1023, 24), (2049, 1, 1, 16)]
 
 
 def _ids(T, k, n_experts, seed, drop=0.2):
