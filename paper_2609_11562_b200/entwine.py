@@ -8,7 +8,9 @@ Device-buffer arguments are torch CUDA tensors (bf16, contiguous) or raw integer
 The operators beside the fused call (quant_i8, moe_dispatch and the others at the end of this file) take
 torch CUDA tensors only: sizes, row distances and element types are read from them, and what does not fit
 together is refused with EntwineError(ERR_INVALID) before anything is launched.  Their arguments are marshalled by an
-extension module (csrc/opcalls.c), because their smallest calls are as short as a ctypes call.
+extension module (csrc/opcalls.c), because their smallest calls are as short as a ctypes call.  A call works on its
+tensors after it has returned: one that is freed before that, on another stream than its allocation's, needs
+Tensor.record_stream as with any kernel.
 """
 from __future__ import annotations
 
