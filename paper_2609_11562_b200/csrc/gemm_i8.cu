@@ -501,10 +501,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
       auto finish = [&](const uint32_t (&v)[32], float scale, int c) {
         sa[lane] = scale;
         __syncwarp();
+        float4 s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = reinterpret_cast<const float4*>(sa)[j];
         Out* const mine = staging + q * 32 + lane;
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
-          const float4 s4 = *reinterpret_cast<const float4*>(sa + j);
+          const float4 s4 = s[j / 4];
           const float f[4] = {fmaf(__int2float_rn(int(v[j + 0])) * s4.x, sb, add),
                               fmaf(__int2float_rn(int(v[j + 1])) * s4.y, sb, add),
                               fmaf(__int2float_rn(int(v[j + 2])) * s4.z, sb, add),
