@@ -44,6 +44,7 @@ struct Params {
   const int32_t* offsets;  // null: one matrix for all rows
   void* c;
   int64_t ldc;
+  int c_step;              // bytes, up to 16, on whose multiples all rows of C start
   int M, N, K, G;
   int token_tiles;         // an upper bound with experts
   int split;               // CTAs that share the length K of a tile
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
   // Every warp finishes tokens, four channels per lane: the sum is exact; its conversion, the two products and the
   // last rounding are the only inexact steps.
   if (ok) {
-    const bool vec = reinterpret_cast<uintptr_t>(P.c) % (4 * sizeof(Out)) == 0 && P.ldc % 4 == 0 && n + 4 <= P.N;
+    const bool vec = P.c_step >= int(4 * sizeof(Out)) && n + 4 <= P.N;
     for (int j = rank + warp * P.split; j < used; j += P.split * (kThreads / 32)) {
       const uint32_t at = ring + (j * kChannels + 4 * lane) * 4;
       int4 part[kMaxSplit];
@@ -293,6 +294,31 @@ struct PairCfg {
   static constexpr int kStagingBytes = 32 * kChannels * sizeof(Out);  // of a group of epilogue warps
   static constexpr int kSmem = kStages * kPairStageBytes + 2 * kStagingBytes + 1024;
 };
+
+// Eight rows of 128 staged elements to C by one warp, E elements at a time; `left` channels of the tile lie inside C.
+template <typename Out, int E>
+__device__ __forceinline__ void store_rows(const Out* in, Out* out, int64_t ldc, int rows, int left, int lane) {
+  using V = Piece<Out, E>;
+  constexpr int kPerRow = kChannels / E, kTurns = kPerRow / 4, kBatch = kTurns < 8 ? kTurns : 8;
+#pragma unroll 1
+  for (int t0 = 0; t0 < kTurns; t0 += kBatch) {
+    V v[kBatch];
+#pragma unroll
+    for (int t = 0; t < kBatch; ++t) v[t] = reinterpret_cast<const V*>(in)[(t0 + t) * 32 + lane];
+#pragma unroll
+    for (int t = 0; t < kBatch; ++t) {
+      const int i = (t0 + t) * 32 + lane, r = i / kPerRow, x = i % kPerRow * E;
+      if (r >= rows) continue;
+      if (x + E <= left) {
+        *reinterpret_cast<V*>(out + r * ldc + x) = v[t];
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (x + e < left) out[r * ldc + x + e] = v[t].e[e];
+      }
+    }
+  }
+}
 
 // What the walk over the tiles needs of each expert.
 struct PairGroups {
@@ -472,8 +498,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
     Out* const staging = reinterpret_cast<Out*>(smem_raw + (ring - smem_u32(smem_raw)) + S * kPairStageBytes +
                                                 group * C::kStagingBytes);
     float* const sa = token_scale[warp - 2];
-    constexpr int kVec = 16 / sizeof(Out), kLanesPerRow = kChannels / kVec, kRowsPerStore = 32 / kLanesPerRow;
-    const bool vec = reinterpret_cast<uintptr_t>(P.c) % 16 == 0 && P.ldc * sizeof(Out) % 16 == 0;
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int t = pair; t < total; t += pairs) {
@@ -518,22 +542,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
         }
         named_bar_sync(1 + group, 128);
         // a quarter of the rows for each warp
-        const int row0 = q * 8, rows = min(8, w.rows - c * 32 - row0);
+        const int row0 = q * 8, rows = min(8, w.rows - c * 32 - row0), left = min(kChannels, P.N - n0);
         Out* const out = static_cast<Out*>(P.c) + int64_t(w.m0 + c * 32 + row0) * P.ldc + n0;
         const Out* const in = staging + row0 * kChannels;
-        const int r0 = lane / kLanesPerRow, x = lane % kLanesPerRow * kVec;
-        if (vec && n0 + kChannels <= P.N) {
-          uint4 o[8 / kRowsPerStore];
-#pragma unroll
-          for (int i = 0; i < 8 / kRowsPerStore; ++i)
-            o[i] = *reinterpret_cast<const uint4*>(in + (i * kRowsPerStore + r0) * kChannels + x);
-#pragma unroll
-          for (int i = 0; i < 8 / kRowsPerStore; ++i)
-            if (i * kRowsPerStore + r0 < rows) *reinterpret_cast<uint4*>(out + (i * kRowsPerStore + r0) * P.ldc + x) = o[i];
-        } else {
-          for (int r = 0; r < rows; ++r)
-            for (int i = lane; i < kChannels && n0 + i < P.N; i += 32) out[r * P.ldc + i] = in[r * kChannels + i];
-        }
+        if (P.c_step >= 16) store_rows<Out, 16 / sizeof(Out)>(in, out, P.ldc, rows, left, lane);
+        else if (P.c_step == 8) store_rows<Out, 8 / sizeof(Out)>(in, out, P.ldc, rows, left, lane);
+        else if (P.c_step == 4) store_rows<Out, 4 / sizeof(Out)>(in, out, P.ldc, rows, left, lane);
+        else store_rows<Out, 1>(in, out, P.ldc, rows, left, lane);
         named_bar_sync(1 + group, 128);
       };
       uint32_t v[2][32];
@@ -704,6 +719,8 @@ int gemm(const void* A, int64_t lda, const float* scale_a, const void* B, int64_
   P.offsets = offsets;
   P.c = C;
   P.ldc = ldc;
+  const uint64_t starts = reinterpret_cast<uintptr_t>(C) | uint64_t(ldc) * (c_dtype == ENTWINE_FP32 ? 4 : 2);
+  P.c_step = int(std::min<uint64_t>(starts & (~starts + 1), 16));
   P.M = int(M);
   P.N = int(N);
   P.K = int(K);
