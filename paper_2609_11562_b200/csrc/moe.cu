@@ -135,25 +135,42 @@ __global__ void __launch_bounds__(kSortThreads) moe_sort_kernel(const Id* ids, i
   }
 }
 
-// A token's row read once (for each kChunk places) and written to its places, `to` in shared or global memory.
+// A token's row written to its places, `to` in shared or global memory: read once for each kChunk of them where all rows
+// start on 16-byte boundaries (V > 1), else put together anew for each place, whose pieces lie differently.
 template <typename T, int V>
-__device__ __forceinline__ void move_row(const T* src, int64_t H, const int32_t* to, int64_t k, T* rows, int64_t ldr) {
-  using P = typename std::conditional<V == 1, T, uint4>::type;  // (sixteen bytes moved as one thing)
-  const int64_t pieces = H / V;
-  for (int64_t j0 = 0; j0 < k; j0 += kChunk) {
-    int32_t r[kChunk];
+__device__ __forceinline__ void move_row(const T* src, int64_t H, const int32_t* to, int64_t k, T* rows, int64_t ldr,
+                                         const Span& inside) {
+  if constexpr (V > 1) {
+    const int64_t pieces = H / V;
+    for (int64_t j0 = 0; j0 < k; j0 += kChunk) {
+      int32_t r[kChunk];
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) r[j] = j0 + j < k ? to[j0 + j] : -1;
-    for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
-      const P v = reinterpret_cast<const P*>(src)[i];
+      for (int j = 0; j < kChunk; ++j) r[j] = j0 + j < k ? to[j0 + j] : -1;
+      for (int64_t i = threadIdx.x; i < pieces; i += kThreads) {
+        const uint4 v = reinterpret_cast<const uint4*>(src)[i];  // (moved as one thing, whatever the elements)
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j)
-        if (r[j] >= 0) reinterpret_cast<P*>(rows + r[j] * ldr)[i] = v;
+        for (int j = 0; j < kChunk; ++j)
+          if (r[j] >= 0) reinterpret_cast<uint4*>(rows + r[j] * ldr)[i] = v;
+      }
+      for (int64_t i = pieces * V + threadIdx.x; i < H; i += kThreads)
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j)
+          if (r[j] >= 0) rows[r[j] * ldr + i] = src[i];
     }
-    for (int64_t i = pieces * V + threadIdx.x; i < H; i += kThreads)
-#pragma unroll
-      for (int j = 0; j < kChunk; ++j)
-        if (r[j] >= 0) rows[r[j] * ldr + i] = src[i];
+  } else {
+    for (int64_t j = 0; j < k; ++j) {
+      if (to[j] < 0) continue;
+      T* const dst = rows + to[j] * ldr;
+      const Cut<T> cut(dst, H);
+      for (int64_t i = threadIdx.x; i < cut.pieces; i += kThreads) {
+        const int64_t e = cut.head + i * (16 / int64_t(sizeof(T)));
+        const Piece<T, 16 / sizeof(T)> v = load_anywhere(src + e, inside);
+        uint4 bits;
+        memcpy(&bits, &v, 16);
+        *reinterpret_cast<uint4*>(dst + e) = bits;
+      }
+      for (int64_t i = threadIdx.x; i < cut.ends; i += kThreads) dst[cut.end(i)] = src[cut.end(i)];
+    }
   }
 }
 
@@ -164,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) moe_move_kernel(const T* x, int64_t 
                                                             float* row_scale) {
   const int64_t t = blockIdx.x;
   const int32_t* to = row_of + t * k;
-  move_row<T, V>(x + t * ldx, H, to, k, rows, ldr);
+  move_row<T, V>(x + t * ldx, H, to, k, rows, ldr, span_of(x, gridDim.x, H, ldx));
   if (x_scale)
     for (int64_t j = threadIdx.x; j < k; j += kThreads)
       if (to[j] >= 0) row_scale[to[j]] = x_scale[t];
@@ -238,7 +255,7 @@ __global__ void __launch_bounds__(kThreads) moe_dispatch_small_kernel(const T* x
       if (r >= 0 && x_scale) row_scale[r] = x_scale[t];
     }
     __syncthreads();
-    move_row<T, V>(x + t * ldx, H, part[0], min(k - j0, kChunk), rows, ldr);
+    move_row<T, V>(x + t * ldx, H, part[0], min(k - j0, kChunk), rows, ldr, span_of(x, T_, H, ldx));
     __syncthreads();
   }
 }
@@ -296,6 +313,58 @@ __global__ void __launch_bounds__(kThreads, 5) moe_combine_kernel(const T* y, in
       if (r >= 0 && r < n_rows) acc = fmaf(wt ? wt[j] : 1.0f, Elem<T>::up(y[r * ldy + i]), acc);
     }
     dst[i] = Elem<T>::down(acc);
+  }
+}
+
+// The same for rows that start anywhere: a thread takes an aligned piece of the token and puts the pieces of its rows
+// together from the words around them (8192 tokens of 4095 bf16, eight experts each: ALIGN_FWD us; element by element 470).
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 4) moe_combine_anywhere_kernel(const T* y, int64_t n_rows, int64_t H,
+                                                                           int64_t ldy, const float* w,
+                                                                           const int32_t* row_of, int64_t k, T* out,
+                                                                           int64_t ldo) {
+  constexpr int V = 16 / sizeof(T);
+  using P = Piece<T, V>;
+  const int64_t t = blockIdx.x, step = int64_t(gridDim.y) * blockDim.x;
+  const int32_t* at = row_of + t * k;
+  const float* wt = w ? w + t * k : nullptr;
+  T* dst = out + t * ldo;
+  const Cut<T> cut(dst, H);
+  const Span inside = span_of(y, n_rows, H, ldy);
+  const int64_t first = int64_t(blockIdx.y) * blockDim.x + threadIdx.x;
+  for (int64_t i = first; i < cut.pieces; i += step) {
+    const int64_t x = cut.head + i * V;
+    float acc[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+    for (int64_t j0 = 0; j0 < k; j0 += kReads) {
+      P v[kReads];
+      float f[kReads];
+#pragma unroll
+      for (int j = 0; j < kReads; ++j) {
+        const int64_t r = j0 + j < k ? at[j0 + j] : -1;
+        const bool there = r >= 0 && r < n_rows;
+        f[j] = !there ? 0.0f : wt ? wt[j0 + j] : 1.0f;
+        v[j] = there ? load_anywhere(y + r * ldy + x, inside) : P{};
+      }
+#pragma unroll
+      for (int j = 0; j < kReads; ++j) {
+        float ye[V];
+        unpack<T, V>(v[j], ye);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = fmaf(f[j], ye[e], acc[e]);
+      }
+    }
+    *reinterpret_cast<P*>(dst + x) = pack<T, V>(acc);
+  }
+  for (int64_t i = first; i < cut.ends; i += step) {
+    const int64_t x = cut.end(i);
+    float acc = 0.0f;
+    for (int64_t j = 0; j < k; ++j) {
+      const int64_t r = at[j];
+      if (r >= 0 && r < n_rows) acc = fmaf(wt ? wt[j] : 1.0f, Elem<T>::up(y[r * ldy + x]), acc);
+    }
+    dst[x] = Elem<T>::down(acc);
   }
 }
 
@@ -365,6 +434,63 @@ __global__ void __launch_bounds__(kThreads, 4) moe_combine_bwd_kernel(const T* d
   }
 }
 
+// The same for rows that start anywhere, one row of dy after another in its own aligned pieces.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 4) moe_combine_bwd_anywhere_kernel(const T* dout, int64_t H, int64_t ldo,
+                                                                               const T* y, int64_t n_rows, int64_t ldy,
+                                                                               const float* w, const int32_t* row_of,
+                                                                               int64_t k, T* dy, int64_t lddy,
+                                                                               float* dw) {
+  constexpr int V = 16 / sizeof(T);
+  using P = Piece<T, V>;
+  __shared__ float part[2][kThreads / 32];
+  const int64_t t = blockIdx.x;
+  const T* g = dout + t * ldo;
+  const Span in_g = span_of(dout, gridDim.x, H, ldo), in_y = span_of(y, n_rows, H, ldy);
+  int turn = 0;
+  for (int64_t j = 0; j < k; ++j) {
+    const int64_t r = row_of[t * k + j];
+    if (r < 0 || r >= n_rows) {
+      if (threadIdx.x == 0) dw[t * k + j] = 0.0f;
+      continue;
+    }
+    const float f = w[t * k + j];
+    const T* yr = y + r * ldy;
+    T* dr = dy + r * lddy;
+    const Cut<T> cut(dr, H);
+    float dot = 0.0f;
+    for (int64_t i = threadIdx.x; i < cut.pieces; i += kThreads) {
+      const int64_t x = cut.head + i * V;
+      const P a = load_anywhere(g + x, in_g), b = load_anywhere(yr + x, in_y);
+      float ge[V], ye[V], d[V];
+      unpack<T, V>(a, ge);
+      unpack<T, V>(b, ye);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        dot = fmaf(ge[e], ye[e], dot);
+        d[e] = f * ge[e];
+      }
+      *reinterpret_cast<P*>(dr + x) = pack<T, V>(d);
+    }
+    for (int64_t i = threadIdx.x; i < cut.ends; i += kThreads) {
+      const int64_t x = cut.end(i);
+      const float ge = Elem<T>::up(g[x]);
+      dot = fmaf(ge, Elem<T>::up(yr[x]), dot);
+      dr[x] = Elem<T>::down(f * ge);
+    }
+    dot = warp_sum(dot);
+    if (threadIdx.x % 32 == 0) part[turn][threadIdx.x / 32] = dot;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      float s = part[turn][0];
+#pragma unroll
+      for (int i = 1; i < kThreads / 32; ++i) s += part[turn][i];
+      dw[t * k + j] = s;
+    }
+    turn ^= 1;
+  }
+}
+
 template <typename Id>
 int sort(const void* ids, int64_t n, int E, int32_t* offsets, int32_t* row_of, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(moe_sort_kernel<Id>, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -416,10 +542,10 @@ int combine(const void* y, int64_t n_rows, int64_t H, int64_t ldy, const float* 
             int64_t k, void* out, int64_t ldo, cudaStream_t stream) {
   constexpr int V = 16 / sizeof(T);
   const bool vec = aligned_rows(y, ldy, sizeof(T)) && aligned_rows(out, ldo, sizeof(T));
-  auto kernel = !vec ? moe_combine_kernel<T, 1, kReads, 1>
+  auto kernel = !vec ? moe_combine_anywhere_kernel<T>
                 : k <= kReads / 2 ? moe_combine_kernel<T, V, kReads / 2, 2> : moe_combine_kernel<T, V, kReads, 1>;
   // one piece per thread until the tokens alone fill the GPU
-  const int64_t pieces = vec ? (H + V - 1) / V : H;
+  const int64_t pieces = (H + V - 1) / V;
   const int threads = pieces <= 128 || T_ < kFewTokens ? 128 : kThreads;
   const int64_t parts = T_ < kFewTokens ? std::min<int64_t>((pieces + threads - 1) / threads, 64) : 1;
   kernel<<<dim3(unsigned(T_), unsigned(parts)), threads, 0, stream>>>(static_cast<const T*>(y), n_rows, H, ldy, w,
@@ -434,7 +560,7 @@ int combine_bwd(const void* dout, int64_t T_, int64_t H, int64_t ldo, const void
   constexpr int V = 16 / sizeof(T);
   const bool vec = aligned_rows(dout, ldo, sizeof(T)) && aligned_rows(y, ldy, sizeof(T)) &&
                    aligned_rows(dy, lddy, sizeof(T));
-  auto kernel = vec ? moe_combine_bwd_kernel<T, V> : moe_combine_bwd_kernel<T, 1>;
+  auto kernel = vec ? moe_combine_bwd_kernel<T, V> : moe_combine_bwd_anywhere_kernel<T>;
   kernel<<<unsigned(T_), kThreads, 0, stream>>>(static_cast<const T*>(dout), H, ldo, static_cast<const T*>(y), n_rows,
                                                 ldy, w, row_of, k, static_cast<T*>(dy), lddy, dw);
   return launched(cudaSuccess);

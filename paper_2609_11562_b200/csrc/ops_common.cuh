@@ -110,6 +110,58 @@ __device__ __forceinline__ Piece<T, V> load_if(const T* p, bool there) {
   }
 }
 
+// Memory that may be read: a matrix from its first element to its last.
+struct Span {
+  uintptr_t lo, hi;
+};
+template <typename T>
+__host__ __device__ __forceinline__ Span span_of(const T* p, int64_t rows, int64_t cols, int64_t ld) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  return {lo, rows > 0 ? lo + uintptr_t(((rows - 1) * ld + cols) * int64_t(sizeof(T))) : lo};
+}
+
+// Sixteen bytes of elements that start anywhere in a matrix: the two aligned words around them, put together by byte
+// shifts.  What lies around the elements is read only inside the matrix (another row, or the space between rows);
+// at its very ends the elements are read one by one.
+template <typename T>
+__device__ __forceinline__ Piece<T, 16 / sizeof(T)> load_anywhere(const T* p, const Span& inside) {
+  constexpr int V = 16 / sizeof(T);
+  Piece<T, V> v;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~uintptr_t(15);
+  const uint32_t shift = uint32_t(at & 15);
+  if (base < inside.lo || base + (shift ? 32 : 16) > inside.hi) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v.e[e] = p[e];
+    return v;
+  }
+  const uint4 a = *reinterpret_cast<const uint4*>(base);
+  const uint4 b = shift ? *reinterpret_cast<const uint4*>(base + 16) : a;
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = shift & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = shift & 4 ? w[i + 1] : w[i];
+  const uint4 o = make_uint4(__funnelshift_r(w[0], w[1], (shift & 3) * 8), __funnelshift_r(w[1], w[2], (shift & 3) * 8),
+                             __funnelshift_r(w[2], w[3], (shift & 3) * 8), __funnelshift_r(w[3], w[4], (shift & 3) * 8));
+  memcpy(&v, &o, 16);
+  return v;
+}
+
+// How a row that starts anywhere falls into aligned 16-byte pieces: `head` elements before the first of them, `pieces`
+// of them, and the rest of H elements behind.
+template <typename T>
+struct Cut {
+  int64_t head, pieces, ends;  // ends: elements outside the pieces
+  __device__ __forceinline__ Cut(const T* row, int64_t H) {
+    constexpr int V = 16 / sizeof(T);
+    head = min(int64_t((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(T)), H);
+    pieces = (H - head) / V;
+    ends = H - pieces * V;
+  }
+  // element number of the i-th one outside the pieces
+  __device__ __forceinline__ int64_t end(int64_t i) const { return i < head ? i : i + pieces * (16 / sizeof(T)); }
+};
+
 inline bool aligned_rows(const void* p, int64_t ld, int64_t elem_bytes, int64_t bytes = 16) {
   return reinterpret_cast<uintptr_t>(p) % uintptr_t(bytes) == 0 && (ld * elem_bytes) % bytes == 0;
 }
