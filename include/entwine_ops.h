@@ -11,7 +11,7 @@
  *
  * Matrices are row-major; ld* is the distance between two rows in elements, at least the row's length.  Element
  * pointers need the alignment of their element only, except where a function says more; rows that start on
- * 16-byte boundaries are moved in 16-byte pieces, others element by element.
+ * 16-byte boundaries are the fastest.
  */
 #ifndef ENTWINE_OPS_H_
 #define ENTWINE_OPS_H_

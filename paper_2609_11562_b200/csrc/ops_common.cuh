@@ -32,8 +32,7 @@ struct Elem<float> {
   static __device__ __forceinline__ float down(float v) { return v; }
 };
 
-// V consecutive elements moved as one access: 16 bytes, or a single element where a row does not start on a
-// 16-byte boundary.
+// V consecutive elements moved as one access.
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Piece {
   T e[V];
@@ -93,21 +92,18 @@ __device__ __forceinline__ Piece<T, V> pack(const float (&f)[V]) {
 // neighbours, so that a batch of them is in flight together whatever the compiler makes of the code around it.
 template <typename T, int V>
 __device__ __forceinline__ Piece<T, V> load_if(const T* p, bool there) {
-  if constexpr (sizeof(T) * V == 16) {
-    uint4 w;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %5, 0;\n\t"
-        "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
-        "@p ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
-        : "=&r"(w.x), "=&r"(w.y), "=&r"(w.z), "=&r"(w.w)
-        : "l"(p), "r"(int(there)));
-    Piece<T, V> v;
-    memcpy(&v, &w, 16);
-    return v;
-  } else {
-    return there ? *reinterpret_cast<const Piece<T, V>*>(p) : Piece<T, V>{};
-  }
+  static_assert(sizeof(T) * V == 16, "sixteen bytes");
+  uint4 w;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+      "@p ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=&r"(w.x), "=&r"(w.y), "=&r"(w.z), "=&r"(w.w)
+      : "l"(p), "r"(int(there)));
+  Piece<T, V> v;
+  memcpy(&v, &w, 16);
+  return v;
 }
 
 // Memory that may be read: a matrix from its first element to its last.
@@ -122,30 +118,67 @@ __host__ __device__ __forceinline__ Span span_of(const T* p, int64_t rows, int64
 
 // Sixteen bytes of elements that start anywhere in a matrix: the two aligned words around them, put together by byte
 // shifts.  What lies around the elements is read only inside the matrix (another row, or the space between rows);
-// at its very ends the elements are read one by one.
+// at its very ends, where alone() is true, the elements are read one by one.
 template <typename T>
-__device__ __forceinline__ Piece<T, 16 / sizeof(T)> load_anywhere(const T* p, const Span& inside) {
-  constexpr int V = 16 / sizeof(T);
-  Piece<T, V> v;
-  const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~uintptr_t(15);
-  const uint32_t shift = uint32_t(at & 15);
-  if (base < inside.lo || base + (shift ? 32 : 16) > inside.hi) {
+struct Anywhere {
+  static constexpr int V = 16 / sizeof(T);
+  uint4 a, b;
+  uint32_t shift;
+
+  static __device__ __forceinline__ bool alone(const T* p, const Span& inside) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~uintptr_t(15);
+    return base < inside.lo || base + (at == base ? 16 : 32) > inside.hi;
+  }
+  // Both words, zeros where `there` is false; instructions of their own, so that those of a batch are in flight together.
+  __device__ __forceinline__ void fetch(const T* p, bool there) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~uintptr_t(15);
+    shift = uint32_t(at & 15);
+    a = word(base, there);
+    b = word(base + 16, there && shift != 0);
+  }
+  __device__ __forceinline__ Piece<T, V> get() const {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = shift & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = shift & 4 ? w[i + 1] : w[i];
+    const uint32_t bits = (shift & 3) * 8;
+    const uint4 o = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
+                               __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+    Piece<T, V> v;
+    memcpy(&v, &o, 16);
+    return v;
+  }
+  static __device__ __forceinline__ Piece<T, V> one_by_one(const T* p) {
+    Piece<T, V> v;
 #pragma unroll
     for (int e = 0; e < V; ++e) v.e[e] = p[e];
     return v;
   }
-  const uint4 a = *reinterpret_cast<const uint4*>(base);
-  const uint4 b = shift ? *reinterpret_cast<const uint4*>(base + 16) : a;
-  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int i = 0; i < 6; ++i) w[i] = shift & 8 ? w[i + 2] : w[i];
-#pragma unroll
-  for (int i = 0; i < 5; ++i) w[i] = shift & 4 ? w[i + 1] : w[i];
-  const uint4 o = make_uint4(__funnelshift_r(w[0], w[1], (shift & 3) * 8), __funnelshift_r(w[1], w[2], (shift & 3) * 8),
-                             __funnelshift_r(w[2], w[3], (shift & 3) * 8), __funnelshift_r(w[3], w[4], (shift & 3) * 8));
-  memcpy(&v, &o, 16);
-  return v;
-}
+  // One piece by itself.
+  static __device__ __forceinline__ Piece<T, V> load(const T* p, const Span& inside) {
+    if (alone(p, inside)) return one_by_one(p);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), base = at & ~uintptr_t(15);
+    Anywhere<T> v;
+    v.shift = uint32_t(at & 15);
+    v.a = *reinterpret_cast<const uint4*>(base);
+    v.b = v.shift ? *reinterpret_cast<const uint4*>(base + 16) : v.a;
+    return v.get();
+  }
+
+ private:
+  static __device__ __forceinline__ uint4 word(uintptr_t at, bool there) {
+    uint4 w;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+        "@p ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "=&r"(w.x), "=&r"(w.y), "=&r"(w.z), "=&r"(w.w)
+        : "l"(at), "r"(int(there)));
+    return w;
+  }
+};
 
 // How a row that starts anywhere falls into aligned 16-byte pieces: `head` elements before the first of them, `pieces`
 // of them, and the rest of H elements behind.

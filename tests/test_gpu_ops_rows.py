@@ -360,3 +360,48 @@ def test_capture_replay_and_other_streams():
             side[0].synchronize()
             assert torch.equal(again, b["out"])
             _check_quant(b["out"].cpu(), b["q"], b["scale"])
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float32, torch.int8), ids=_name)
+@pytest.mark.parametrize("H", [1, 5, 15, 16, 17, 31, 33, 47, 100, 523])
+def test_rows_at_every_alignment(H, dtype):
+    """Matrices that start at every element behind a 16-byte boundary, with NaN (or other levels) around every row: what
+    is read beside a row is not used, what lies beside it is not written."""
+    T, k, n_experts = 9, 3, 4
+    ids = _ids(T, k, n_experts, H)
+    _, rr = _sort_ref(ids, n_experts)
+    row_of, fill = torch.from_numpy(rr).cuda(), float("nan") if dtype != torch.int8 else 99
+    size = torch.empty(0, dtype=dtype).element_size()
+    x, y = _rand((T, H), dtype, 1), _rand((T * k, H), dtype, 2)
+    w = torch.rand(T, k, generator=torch.Generator().manual_seed(4))
+    for shift in range(16 // size):
+        for pitch in (H, H + 1, H + 3):
+            rows = _laid_out(torch.full((T * k, H), 7, dtype=dtype), pitch, shift, fill=55)
+            E.moe_dispatch(_laid_out(x, pitch, 16 // size - 1 - shift, fill=fill), ids.cuda(), n_experts, rows,
+                           torch.empty(n_experts + 1, dtype=torch.int32, device="cuda"), torch.empty(T, k, dtype=torch.int32, device="cuda"))
+            want = torch.full((T * k, H), 7, dtype=dtype)
+            t, j = np.nonzero(rr >= 0)
+            want[torch.from_numpy(rr[t, j].astype(np.int64))] = x[torch.from_numpy(t)]
+            assert torch.equal(rows.cpu(), want)
+            beside = rows._base.clone()
+            beside[shift:].view(T * k, pitch)[:, :H] = 55
+            assert bool((beside == 55).all())
+            if dtype == torch.int8:
+                continue
+            yd, out = _laid_out(y, pitch, shift, fill=fill), _laid_out(torch.zeros(T, H, dtype=dtype), pitch, (shift + 1) % 4, fill=55)
+            E.moe_combine(yd, w.cuda(), row_of, out)
+            yt, there = _taken(y, torch.from_numpy(rr))
+            w64 = np.where(there, _f64(w), 0.0)
+            ref, mag = (yt * w64[..., None]).sum(1), (np.abs(yt) * w64[..., None]).sum(1)
+            assert (np.abs(_f64(out) - ref) <= (k + 1) * 2.0 ** -24 * mag * 1.01 + _half_step(dtype) * np.abs(ref) + TINY[dtype]).all()
+            g = _rand((T, H), dtype, 3)
+            dy, dw = _laid_out(torch.full((T * k, H), 9.0, dtype=dtype), pitch, shift, fill=55), torch.empty(T, k, device="cuda")
+            E.moe_combine_bwd(_laid_out(g, pitch, (shift + 2) % 4, fill=fill), yd, w.cuda(), row_of, dy, dw)
+            want = np.full((T * k, H), 9.0)
+            want[rr[there]] = (w64[..., None] * _f64(g)[:, None])[there]
+            assert (np.abs(_f64(dy) - want) <= (2.0 ** -24 + _half_step(dtype)) * 1.01 * np.abs(want) + TINY[dtype]).all()
+            dot, mag = np.einsum("th,tkh->tk", _f64(g), yt), np.einsum("th,tkh->tk", np.abs(_f64(g)), np.abs(yt))
+            assert (np.abs(_f64(dw) - dot) <= H * 2.0 ** -24 * mag * 1.01).all()
+            beside = dy._base.clone()
+            beside[shift:].view(T * k, pitch)[:, :H] = 55
+            assert bool((beside == 55).all())
