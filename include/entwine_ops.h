@@ -76,6 +76,16 @@ int entwine_gemm_i8_grouped(const void* A, int64_t lda, const float* scale_a, co
  */
 int entwine_ops_status(void* stream);
 
+/* Settings of the process for its later calls (a captured call keeps those that it was captured with). */
+enum {
+  ENTWINE_OPS_OPT_WAIT_BUDGET_NS = 1, /* budget of every device-side wait of the products (default 2e9, at least 1e6) */
+  ENTWINE_OPS_OPT_WITHHOLD_BLOCK = 2  /* host-side fault injection: the first tile of a product waits for its
+                                         value-th block of 128 elements of K (counted within the CTA's share of K),
+                                         which is not loaded; -1: none (default)                                       */
+};
+/* ENTWINE_ERR_INVALID for an unknown key or a value out of range. */
+int entwine_ops_set_option(int key, int64_t value);
+
 /*
  * entwine_moe_dispatch - tokens sorted by expert.  ids [T][k] (int32, or int64 with ids64 != 0; contiguous) names
  * the k experts of each token, 0 <= id < E; any other value (-1, say) drops the assignment.  The assignments that

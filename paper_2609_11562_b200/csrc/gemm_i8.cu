@@ -6,6 +6,7 @@
 // that a decoding step pays for reading B and nothing else; and a warp's lanes, consecutive channels, store
 // consecutive elements of a row of C.
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 
 #include "ops_common.cuh"
@@ -21,9 +22,11 @@ constexpr int kMaxSplit = 8;
 constexpr int kMaxGroups = 1024;
 constexpr int64_t kMaxK = 131071;    // 128 * 128 * K < 2^31
 constexpr int64_t kMaxExtent = 2147483647;
-constexpr unsigned long long kWaitBudgetNs = 2000000000ull;
 
 __device__ int g_wait_failed;        // set when a bounded wait ran out, read by entwine_ops_status
+
+// entwine_ops_set_option
+std::atomic<int64_t> g_wait_budget_ns{2000000000}, g_withhold{-1};
 
 struct Maps {
   CUtensorMap a;  // tokens [M][K]
@@ -49,10 +52,12 @@ struct Params {
   int token_tiles;         // an upper bound with experts
   int split;               // CTAs that share the length K of a tile
   int tile_rows;           // most tokens of a pair tile, a multiple of 32
+  int withhold;            // block of K that the first tile's first CTA or pair does not load; -1: none
+  unsigned long long wait_ns;  // budget of every wait
 };
 
 // Bounded wait for a phase of a barrier.
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool wait_bar(const Params& P, uint32_t bar, uint32_t parity) {
   unsigned long long t0 = 0;
   for (;;) {
 #pragma unroll 1
@@ -60,7 +65,7 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity) {
       if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long now = globaltimer_ns();
     if (t0 == 0) t0 = now;
-    if (now - t0 > kWaitBudgetNs) {
+    if (now - t0 > P.wait_ns) {
       g_wait_failed = 1;
       return false;
     }
@@ -132,10 +137,11 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
   int issued = 0;
   bool ok = true;
   int g = 0, m0 = tile * TOKENS, m_end = P.M;
+  const int withhold = blockIdx.x == 0 ? P.withhold : -1;
   auto load = [&]() {
     const int s = issued % S;
     const uint32_t at = ring + s * T::kStageBytes;
-    if (elect_one()) {
+    if (issued != withhold && elect_one()) {
       mbar_arrive_expect_tx(full + 8 * s, T::kStageBytes);
       tma_load_3d(at, &maps.b, (first + issued) * kKBytes, n0, g, full + 8 * s);
       tma_load_2d(at + kChannels * kKBytes, &maps.a, (first + issued) * kKBytes, m0, full + 8 * s);
@@ -191,7 +197,7 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
 
   if (warp == 0) {
     while (issued < blocks) {
-      if (!(ok = __all_sync(0xffffffffu, wait_bar(empty + 8 * (issued % S), (issued / S - 1) & 1)))) break;
+      if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * (issued % S), (issued / S - 1) & 1)))) break;
       load();
     }
   } else if (warp == 1) {
@@ -200,7 +206,7 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
                                (uint32_t(kChannels >> 4) << 24);
     for (int i = 0; i < blocks; ++i) {
       const int s = i % S;
-      if (!(ok = __all_sync(0xffffffffu, wait_bar(full + 8 * s, (i / S) & 1)))) break;
+      if (!(ok = __all_sync(0xffffffffu, wait_bar(P, full + 8 * s, (i / S) & 1)))) break;
       tc_fence_after();
       const uint32_t at = ring + s * T::kStageBytes;
       const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
@@ -214,13 +220,13 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
     if (elect_one()) tc_commit(done);
   }
   __syncwarp();
-  ok = wait_bar(done, 0) && ok;
+  ok = wait_bar(P, done, 0) && ok;
   tc_fence_after();
   ok = !__syncthreads_or(!ok);
   if (!ok && warp == 0) {
-    // copies still under way end before the CTA does
-    for (int i = issued > S ? issued - S : 0; i < issued; ++i)
-      if (!wait_bar(full + 8 * (i % S), (i / S) & 1)) break;
+    // copies still under way end before the CTA does; the one whose wait ran out is not the last of them
+    for (int i = issued > S ? issued - S : 0; i < issued; ++i) wait_bar(P, full + 8 * (i % S), (i / S) & 1);
+    __syncwarp();
   }
   // The partial sums go to shared memory, over the operands: [TOKENS][channels].
   const int used = min(TOKENS, m_end - m0);
@@ -435,9 +441,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
       const PairTile w = walk.at(t);
       const int n0 = w.n0 + rank * kChannels, m0 = w.m0 + rank * ((w.rows + 31) / 32 * 16);
       for (int b = 0; b < blocks; ++b) {
-        if (!(ok = __all_sync(0xffffffffu, wait_bar(empty + 8 * stage, phase ^ 1)))) break;
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * stage, phase ^ 1)))) break;
         const uint32_t at = ring + stage * kPairStageBytes, bar = map_to_cta(full + 8 * stage, 0);
-        if (elect_one()) {
+        if (!(t == 0 && b == P.withhold) && elect_one()) {
           if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * bytes);
           tma_load_3d_pair(at, &maps.b, b * kKBytes, n0, w.g, bar);
           tma_load_2d_pair(at + kChannels * kKBytes, &maps.a, b * kKBytes, m0, bar);
@@ -447,10 +453,16 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
         if (++stage == S) stage = 0, phase ^= 1;
       }
     }
-    // after a wait that ran out: copies still under way end before the CTA does
+    // All that was loaded is used before the CTA ends, and the arrivals that say so have come (in both CTAs); after a
+    // wait that ran out (of the products, too) copies still under way end first.  Those of rank 1 count on rank 0's
+    // barriers.
+    if (ok && in_flight > 0) {
+      const int last = stage > 0 ? stage - 1 : S - 1;
+      ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * last, stage > 0 ? phase : phase ^ 1));
+    }
     for (int i = 0; !ok && rank == 0 && i < in_flight; ++i) {
       if (--stage < 0) stage = S - 1, phase ^= 1;
-      if (!wait_bar(full + 8 * stage, phase)) break;
+      wait_bar(P, full + 8 * stage, phase);
     }
   } else if (warp == 1) {
     if (rank == 0) {
@@ -461,11 +473,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
       for (int t = pair; ok && t < total; t += pairs, rows = next_rows) {
         const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (uint32_t((rows + 31) / 32 * 4) << 17) |
                                (uint32_t(kPairChannels >> 4) << 24);
-        if (!(ok = __all_sync(0xffffffffu, wait_bar(tempty + 8 * acc, acc_phase ^ 1)))) break;
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, tempty + 8 * acc, acc_phase ^ 1)))) break;
         tc_fence_after();
         const uint32_t d = tmem + acc * kPairTokens;
         for (int b = 0; b < blocks; ++b) {
-          if (!(ok = __all_sync(0xffffffffu, wait_bar(full + 8 * stage, phase)))) break;
+          if (!(ok = __all_sync(0xffffffffu, wait_bar(P, full + 8 * stage, phase)))) break;
           tc_fence_after();
           const uint32_t at = ring + stage * kPairStageBytes;
           const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
@@ -481,11 +493,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
         }
         if ((acc ^= 1) == 0) acc_phase ^= 1;
       }
-      if (!ok) {  // products under way end before the TMEM is given back
-        if (elect_one()) tc_commit_pair(drain);
-        __syncwarp();
-        wait_bar(drain, 0);
-      }
+      // products under way end before the TMEM is given back (the epilogue may have left after a wait that ran out)
+      if (elect_one()) tc_commit_pair(drain, 1);
+      __syncwarp();
+      wait_bar(P, drain, 0);
     }
   } else {
     // Epilogue: a warp owns 32 channels (its lane quarter of the accumulator), a lane one of them; groups of four
@@ -511,7 +522,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
         const int r = (group + 2 * i) * 32 + lane;
         scales[i] = r < w.rows ? P.scale_a[w.m0 + r] : 0.0f;
       }
-      if (!named_bar_and(1 + group, 128, wait_bar(tfull + 8 * acc, acc_phase))) break;  // the group leaves together
+      if (!named_bar_and(1 + group, 128, wait_bar(P, tfull + 8 * acc, acc_phase))) break;  // the group leaves together
       tc_fence_after();
       const int chunks = (w.rows + 31) / 32;
       const uint32_t sums = tmem + (uint32_t(q) << 21) + acc * kPairTokens;
@@ -725,6 +736,8 @@ int gemm(const void* A, int64_t lda, const float* scale_a, const void* B, int64_
   P.N = int(N);
   P.K = int(K);
   P.G = int(G);
+  P.withhold = int(g_withhold.load(std::memory_order_relaxed));
+  P.wait_ns = static_cast<unsigned long long>(g_wait_budget_ns.load(std::memory_order_relaxed));
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   switch (c_dtype) {
     case ENTWINE_BF16: return run_as<__nv_bfloat16>(A, lda, B, ldb, expert_stride, P, s);
@@ -752,6 +765,21 @@ int entwine_gemm_i8_grouped(const void* A, int64_t lda, const float* scale_a, co
                             void* stream) {
   if (M > 0 && bad_pointer(offsets, 4)) return ENTWINE_ERR_INVALID;
   return gemm(A, lda, scale_a, B, ldb, expert_stride, scale_b, bias, offsets, C, c_dtype, ldc, M, N, K, G, stream);
+}
+
+int entwine_ops_set_option(int key, int64_t value) {
+  switch (key) {
+    case ENTWINE_OPS_OPT_WAIT_BUDGET_NS:
+      // (a millisecond at least: after a wait that ran out, the same time is given to what is still under way)
+      if (value < 1000000) return ENTWINE_ERR_INVALID;
+      g_wait_budget_ns.store(value, std::memory_order_relaxed);
+      return ENTWINE_OK;
+    case ENTWINE_OPS_OPT_WITHHOLD_BLOCK:
+      if (value < -1 || value > kMaxK) return ENTWINE_ERR_INVALID;
+      g_withhold.store(value, std::memory_order_relaxed);
+      return ENTWINE_OK;
+    default: return ENTWINE_ERR_INVALID;
+  }
 }
 
 int entwine_ops_status(void* stream) {

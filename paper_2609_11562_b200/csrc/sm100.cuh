@@ -201,11 +201,11 @@ __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t cols)
   asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols)
                : "memory");
 }
-// commit of a CTA pair's MMAs, arriving on the barrier at the same offset in both CTAs
-__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
+// commit of a CTA pair's MMAs, arriving on the barrier at the same offset in both CTAs (or those of the mask)
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar, unsigned short ctas = 3) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-      ::"r"(bar), "h"((unsigned short)3)
+      ::"r"(bar), "h"(ctas)
       : "memory");
 }
 __device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,

@@ -81,6 +81,7 @@ _OP_ARGS = {
     "entwine_gemm_i8": [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _int, _i64, _i64, _i64, _i64, _vp],
     "entwine_gemm_i8_grouped": [_vp, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _int, _i64, _i64, _i64, _i64, _i64, _vp],
     "entwine_ops_status": [_vp],
+    "entwine_ops_set_option": [_int, _i64],
     "entwine_moe_dispatch": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp],
     "entwine_moe_dispatch_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp],
     "entwine_moe_combine": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp],
@@ -276,6 +277,7 @@ class Plan:
 # operators beside the fused call (include/entwine_ops.h)
 # ------------------------------------------------------------------------------------------
 DTYPE_BF16, DTYPE_FP16, DTYPE_FP32, DTYPE_I8 = 0, 1, 2, 3
+OPS_OPT_WAIT_BUDGET_NS, OPS_OPT_WITHHOLD_BLOCK = 1, 2
 
 
 def _bind_ops():
@@ -311,6 +313,12 @@ def gemm_i8_grouped(a, scale_a, b, scale_b, offsets, out, bias=None, stream=None
 def ops_status(stream=None):
     """Synchronises the stream; raises EntwineError(ERR_TIMEOUT) if a product's bounded device-side wait has run out."""
     _check(_lib.entwine_ops_status(_stream(stream)), "entwine_ops_status")
+
+
+def ops_set_option(key, value):
+    """A setting of the process for its later products: the budget of their device-side waits, or fault injection
+    (include/entwine_ops.h)."""
+    _check(_lib.entwine_ops_set_option(key, int(value)), f"entwine_ops_set_option({key})")
 
 
 def moe_dispatch(x, ids, n_experts, rows, offsets, row_of, x_scale=None, row_scale=None, stream=None):
