@@ -2,7 +2,7 @@
  * entwine_ops.h - operators beside the fused GEMM-ReduceScatter of entwine.h: the row-parallel layer's product in
  * 8-bit integers (serving) and its form with experts (tokens sorted by expert, and back with weights applied).
  * The conventions of entwine.h hold: every function returns ENTWINE_OK or a negative ENTWINE_ERR_* code, nothing
- * throws, nothing allocates, nothing synchronises (but entwine_ops_status), `stream` is a cudaStream_t passed as
+ * throws, nothing allocates, nothing synchronises (but entwine_ops_status and entwine_ops_failed_waits), `stream` is a cudaStream_t passed as
  * void* (NULL = the default stream), and device pointers belong to the current device.
  *
  * These calls have no plan: each is complete in itself, keeps nothing from one call for the next, and needs no
@@ -70,11 +70,18 @@ int entwine_gemm_i8_grouped(const void* A, int64_t lda, const float* scale_a, co
                             void* stream);
 
 /*
- * entwine_ops_status - synchronises `stream` and returns ENTWINE_ERR_TIMEOUT if a bounded device-side wait of a
- * product on the current device has run out since the last such query (the call's C is then incomplete), else
- * ENTWINE_OK.  Not allowed on a capturing stream (ENTWINE_ERR_INVALID).
+ * entwine_ops_status - synchronises `stream` and returns ENTWINE_ERR_TIMEOUT if bounded device-side waits of products on
+ * the current device have run out since the calling host thread's last such query for this device (its first: since
+ * the library was loaded), else ENTWINE_OK.  TIMEOUT does not say whose product it was: each one that this thread
+ * answers for and that had not ended before its last query may have an incomplete C.  A query takes nothing from
+ * other threads.  Not allowed on a capturing stream (ENTWINE_ERR_INVALID).
+ *
+ * entwine_ops_failed_waits - synchronises `stream` and gives the number of waits of products that have run out on the
+ * current device since the library was loaded; it only grows.  A caller that keeps the number from before its calls
+ * (so that several of them can share a thread) knows that they are complete if it has not changed after them.
  */
 int entwine_ops_status(void* stream);
+int entwine_ops_failed_waits(void* stream, uint64_t* count);
 
 /* Settings of the process for its later calls (a captured call keeps those that it was captured with). */
 enum {

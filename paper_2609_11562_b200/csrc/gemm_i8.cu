@@ -23,7 +23,8 @@ constexpr int kMaxGroups = 1024;
 constexpr int64_t kMaxK = 131071;    // 128 * 128 * K < 2^31
 constexpr int64_t kMaxExtent = 2147483647;
 
-__device__ int g_wait_failed;        // set when a bounded wait ran out, read by entwine_ops_status
+// Bounded waits that ran out on this device.  It only grows: nobody's reading of it takes a failure from anybody else.
+__device__ unsigned long long g_waits_failed;
 
 // entwine_ops_set_option
 std::atomic<int64_t> g_wait_budget_ns{2000000000}, g_withhold{-1};
@@ -66,7 +67,7 @@ __device__ __forceinline__ bool wait_bar(const Params& P, uint32_t bar, uint32_t
     const unsigned long long now = globaltimer_ns();
     if (t0 == 0) t0 = now;
     if (now - t0 > P.wait_ns) {
-      g_wait_failed = 1;
+      atomicAdd(&g_waits_failed, 1ull);
       return false;
     }
   }
@@ -782,21 +783,32 @@ int entwine_ops_set_option(int key, int64_t value) {
   }
 }
 
-int entwine_ops_status(void* stream) {
+int entwine_ops_failed_waits(void* stream, uint64_t* count) {
+  if (!count) return ENTWINE_ERR_INVALID;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
   if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) return launched(cudaErrorUnknown);
   if (capture != cudaStreamCaptureStatusNone) return ENTWINE_ERR_INVALID;
-  int failed = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(&failed, g_wait_failed, sizeof(failed), 0, cudaMemcpyDeviceToHost, s);
+  unsigned long long n = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(&n, g_waits_failed, sizeof(n), 0, cudaMemcpyDeviceToHost, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-  if (e == cudaSuccess && failed) {
-    const int none = 0;
-    e = cudaMemcpyToSymbolAsync(g_wait_failed, &none, sizeof(none), 0, cudaMemcpyHostToDevice, s);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-  }
   if (e != cudaSuccess) return launched(e);
-  return failed ? ENTWINE_ERR_TIMEOUT : ENTWINE_OK;
+  *count = n;
+  return ENTWINE_OK;
+}
+
+int entwine_ops_status(void* stream) {
+  constexpr int kDevices = 64;
+  static thread_local uint64_t told[kDevices];  // failures that this thread has been told of
+  uint64_t n = 0;
+  const int rc = entwine_ops_failed_waits(stream, &n);
+  if (rc != ENTWINE_OK) return rc;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return launched(cudaErrorUnknown);
+  if (dev < 0 || dev >= kDevices) return n ? ENTWINE_ERR_TIMEOUT : ENTWINE_OK;
+  const bool news = n != told[dev];
+  told[dev] = n;
+  return news ? ENTWINE_ERR_TIMEOUT : ENTWINE_OK;
 }
 
 }  // extern "C"

@@ -81,6 +81,7 @@ _OP_ARGS = {
     "entwine_gemm_i8": [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _int, _i64, _i64, _i64, _i64, _vp],
     "entwine_gemm_i8_grouped": [_vp, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _int, _i64, _i64, _i64, _i64, _i64, _vp],
     "entwine_ops_status": [_vp],
+    "entwine_ops_failed_waits": [_vp, ctypes.POINTER(ctypes.c_uint64)],
     "entwine_ops_set_option": [_int, _i64],
     "entwine_moe_dispatch": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp],
     "entwine_moe_dispatch_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp],
@@ -311,8 +312,18 @@ def gemm_i8_grouped(a, scale_a, b, scale_b, offsets, out, bias=None, stream=None
 
 
 def ops_status(stream=None):
-    """Synchronises the stream; raises EntwineError(ERR_TIMEOUT) if a product's bounded device-side wait has run out."""
+    """Synchronises the stream; raises EntwineError(ERR_TIMEOUT) if bounded device-side waits of products on the current
+    device have run out since this thread's last query: whosever product it was, all of this thread's since then may be
+    incomplete.  Other threads are told by their own queries."""
     _check(_lib.entwine_ops_status(_stream(stream)), "entwine_ops_status")
+
+
+def ops_failed_waits(stream=None) -> int:
+    """Synchronises the stream; the number of products' waits that have run out on the current device since the library
+    was loaded.  Unchanged from before some calls to after them: these are complete."""
+    n = ctypes.c_uint64(0)
+    _check(_lib.entwine_ops_failed_waits(_stream(stream), ctypes.byref(n)), "entwine_ops_failed_waits")
+    return n.value
 
 
 def ops_set_option(key, value):

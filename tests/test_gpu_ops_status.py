@@ -1,5 +1,7 @@
 """Bounded device-side waits of the int8 products: a block of operands that never comes makes them give up, say so and
 leave the GPU usable.  The block is withheld by the host (it is not loaded), under a short budget."""
+from concurrent.futures import ThreadPoolExecutor
+
 import pytest
 import torch
 
@@ -103,3 +105,49 @@ def test_a_captured_call_keeps_its_settings(withheld):
     E.gemm_i8(a, sa, b, sb, out)
     E.ops_status()
     assert torch.equal(out.double(), a.double() @ b.double().T)
+
+
+def _timed_out(stream=None):
+    try:
+        E.ops_status(stream)
+    except E.EntwineError as e:
+        assert e.code == E.ERR_TIMEOUT
+        return True
+    return False
+
+
+def test_a_query_takes_no_failure_from_another_thread(withheld):
+    """Whoever asks first, on whatever stream, the thread whose product it was is told too."""
+    a, sa, b, sb = _operands(16, 1000, 600)
+    out, side = torch.empty(16, 1000, device="cuda"), torch.cuda.Stream()
+    with ThreadPoolExecutor(1) as other:
+        other.submit(_timed_out).result()             # (that thread's first query: what failed before it)
+        before, others = E.ops_failed_waits(), other.submit(E.ops_failed_waits).result()
+        assert before == others
+        withheld(0)
+        E.gemm_i8(a, sa, b, sb, out)
+        withheld.off()
+        torch.cuda.synchronize()
+        assert other.submit(_timed_out, side).result()
+        assert not other.submit(_timed_out, side).result()
+        assert _timed_out()
+        assert not _timed_out() and not other.submit(_timed_out).result()
+        assert E.ops_failed_waits(side) > before      # and whoever kept the number sees it, whatever was asked between
+        now = E.ops_failed_waits()
+        E.gemm_i8(a, sa, b, sb, out)
+        assert E.ops_failed_waits() == now and torch.equal(out.double(), a.double() @ b.double().T)
+
+
+def test_status_on_a_capturing_stream_is_refused():
+    side, x = torch.cuda.Stream(), torch.zeros(8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        x.add_(1)
+        for ask in (E.ops_status, E.ops_failed_waits):
+            with pytest.raises(E.EntwineError) as e:
+                ask(side)
+            assert e.value.code == E.ERR_INVALID
+    graph.replay()
+    torch.cuda.synchronize()
+    assert x[0].item() == 1

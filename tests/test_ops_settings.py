@@ -19,3 +19,7 @@ def test_settings_in_range_are_taken():
     E.ops_set_option(E.OPS_OPT_WAIT_BUDGET_NS, 2_000_000_000)
     E.ops_set_option(E.OPS_OPT_WITHHOLD_BLOCK, 0)
     E.ops_set_option(E.OPS_OPT_WITHHOLD_BLOCK, -1)
+
+
+def test_the_count_needs_a_place():
+    assert E._lib.entwine_ops_failed_waits(None, None) == E.ERR_INVALID
