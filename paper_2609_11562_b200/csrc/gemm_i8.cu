@@ -420,7 +420,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
           const int v = __shfl_up_sync(0xffffffffu, sum, o);
           if (lane >= o) sum += v;
         }
-        sum += before;
+        // (offsets that decrease can claim rows many times over: no more tiles than the bound, within 32 bits)
+        sum = min(sum + before, P.token_tiles);
         if (g0 + lane < P.G) groups.first[g0 + lane + 1] = sum;
         before = __shfl_sync(0xffffffffu, sum, 31);
       }
@@ -593,6 +594,7 @@ int run_pairs(const Maps& maps, Params P, cudaStream_t stream) {
   const int64_t token_tiles = P.offsets ? P.M / P.tile_rows + P.G : (P.M + P.tile_rows - 1) / P.tile_rows;
   const int64_t tiles = token_tiles * ((P.N + kPairChannels - 1) / kPairChannels);
   if (tiles > kMaxExtent) return ENTWINE_ERR_INVALID;
+  P.token_tiles = int(token_tiles);
   auto kernel = gemm_i8_pair_kernel<Out>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   if (e != cudaSuccess) return launched(e);
