@@ -525,11 +525,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
         scales[i] = r < w.rows ? P.scale_a[w.m0 + r] : 0.0f;
       }
       if (!named_bar_and(1 + group, 128, wait_bar(P, tfull + 8 * acc, acc_phase))) break;  // the group leaves together
+      __syncwarp();  // (the lanes waited one by one; what follows wants the warp together)
       tc_fence_after();
       const int chunks = (w.rows + 31) / 32;
       const uint32_t sums = tmem + (uint32_t(q) << 21) + acc * kPairTokens;
-      // The accumulator has been read (its loads have completed).  Nothing else is handed over, so the arrival need
-      // not wait for this warp's stores to C: with release semantics it did, 1 us a tile.
+      // The accumulator has been read: this warp's loads have completed (tcgen05.wait::ld), the lanes have met, and the
+      // pair of tcgen05 fences, this one before the arrival and the issuing warp's behind its wait, orders the loads
+      // before the products that overwrite it, whatever the arrival's own semantics.  No ordinary memory is handed over
+      // (C is not read here), so the arrival is relaxed: a releasing one waits for this warp's stores to C, 1 us a tile.
       auto release = [&]() {
         tc_fence_before();
         __syncwarp();
@@ -562,6 +565,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
         else if (P.c_step == 8) store_rows<Out, 8 / sizeof(Out)>(in, out, P.ldc, rows, left, lane);
         else if (P.c_step == 4) store_rows<Out, 4 / sizeof(Out)>(in, out, P.ldc, rows, left, lane);
         else store_rows<Out, 1>(in, out, P.ldc, rows, left, lane);
+        __syncwarp();
         named_bar_sync(1 + group, 128);
       };
       uint32_t v[2][32];
