@@ -57,6 +57,9 @@ struct Params {
   unsigned long long wait_ns;  // budget of every wait
 };
 
+// Out of line: inlined at every wait, its code cost the loops around them 4 % (8192 x 8192 x 3584: 187 us, 179 without).
+__device__ __noinline__ void wait_failed() { atomicAdd(&g_waits_failed, 1ull); }
+
 // Bounded wait for a phase of a barrier.
 __device__ __forceinline__ bool wait_bar(const Params& P, uint32_t bar, uint32_t parity) {
   unsigned long long t0 = 0;
@@ -66,11 +69,10 @@ __device__ __forceinline__ bool wait_bar(const Params& P, uint32_t bar, uint32_t
       if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long now = globaltimer_ns();
     if (t0 == 0) t0 = now;
-    if (now - t0 > P.wait_ns) {
-      atomicAdd(&g_waits_failed, 1ull);
-      return false;
-    }
+    if (now - t0 > P.wait_ns) break;
   }
+  wait_failed();
+  return false;
 }
 
 template <int TOKENS>
