@@ -38,6 +38,28 @@ static dispatch_bwd_fn dispatch_bwd;
 static combine_fn combine;
 static combine_bwd_fn combine_bwd;
 
+/* What bind() has to be given is fetched at the first call, by a function that calls it: until then the package needs no
+ * torch. */
+static PyObject* binder;
+static int bound(void) {
+  PyObject* o;
+  if (error_class) return 1;
+  if (!binder) {
+    PyErr_SetString(PyExc_RuntimeError, "_opcalls: neither bind() nor on_first_call() has been called");
+    return 0;
+  }
+  o = PyObject_CallNoArgs(binder);
+  if (!o) return 0;
+  Py_DECREF(o);
+  if (error_class) return 1;
+  PyErr_SetString(PyExc_RuntimeError, "_opcalls: the function of on_first_call() did not call bind()");
+  return 0;
+}
+static PyObject* py_on_first_call(PyObject* self, PyObject* f) {
+  Py_XSETREF(binder, Py_NewRef(f));
+  Py_RETURN_NONE;
+}
+
 /* Raises EntwineError(code, what). */
 static PyObject* fail(int code, const char* what) {
   PyObject* e = PyObject_CallFunction(error_class, "is", code, what);
@@ -194,7 +216,7 @@ static PyObject* py_quant_i8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Matrix x, q;
   void *scale, *stream;
   long dev;
-  if (!count_is(n, 4) || (dev = first_device(a[0], "x")) < 0 || !matrix(a[0], "x", FLOATING, dev, &x) ||
+  if (!bound() || !count_is(n, 4) || (dev = first_device(a[0], "x")) < 0 || !matrix(a[0], "x", FLOATING, dev, &x) ||
       !result(a[1], "q", 1 << I8, dev, x.rows, x.cols, &q) ||
       !dense(a[2], "scale", 1 << FP32, dev, 1, x.rows, 0, &scale, NULL) || !stream_of(a[3], dev, &stream))
     return NULL;
@@ -206,7 +228,7 @@ static PyObject* py_gemm_i8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Matrix x, w, c;
   void *sx, *sw, *bias, *stream;
   long dev;
-  if (!count_is(n, 7) || (dev = first_device(a[0], "a")) < 0 || !matrix(a[0], "a", 1 << I8, dev, &x) ||
+  if (!bound() || !count_is(n, 7) || (dev = first_device(a[0], "a")) < 0 || !matrix(a[0], "a", 1 << I8, dev, &x) ||
       !matrix(a[2], "b", 1 << I8, dev, &w))
     return NULL;
   if (x.cols != w.cols) return refuse("a and b must have rows of one length"), NULL;
@@ -225,7 +247,7 @@ static PyObject* py_gemm_i8_grouped(PyObject* self, PyObject* const* a, Py_ssize
   int64_t s[3], d[3];
   int dtype;
   long dev;
-  if (!count_is(n, 8) || (dev = first_device(a[0], "a")) < 0 || !matrix(a[0], "a", 1 << I8, dev, &x) ||
+  if (!bound() || !count_is(n, 8) || (dev = first_device(a[0], "a")) < 0 || !matrix(a[0], "a", 1 << I8, dev, &x) ||
       !tensor(a[2], "b", 1 << I8, dev, &dtype, &w))
     return NULL;
   if (!numbers(PyObject_GetAttr(a[2], s_shape), 3, s) || !numbers(PyObject_CallMethodNoArgs(a[2], s_stride), 3, d) ||
@@ -251,7 +273,7 @@ static PyObject* py_moe_dispatch(PyObject* self, PyObject* const* a, Py_ssize_t 
   long long experts;
   int id_type;
   long dev;
-  if (!count_is(n, 9) || (dev = first_device(a[0], "x")) < 0 || !matrix(a[0], "x", ANY, dev, &x) ||
+  if (!bound() || !count_is(n, 9) || (dev = first_device(a[0], "x")) < 0 || !matrix(a[0], "x", ANY, dev, &x) ||
       !routing(a[1], "ids", e))
     return NULL;
   experts = PyLong_AsLongLong(a[2]);
@@ -277,7 +299,7 @@ static PyObject* py_moe_dispatch_bwd(PyObject* self, PyObject* const* a, Py_ssiz
   void *row_of, *stream;
   int64_t e[2];
   long dev;
-  if (!count_is(n, 4) || (dev = first_device(a[0], "d_rows")) < 0 || !matrix(a[0], "d_rows", FLOATING, dev, &r) ||
+  if (!bound() || !count_is(n, 4) || (dev = first_device(a[0], "d_rows")) < 0 || !matrix(a[0], "d_rows", FLOATING, dev, &r) ||
       !routing(a[1], "row_of", e) || !dense(a[1], "row_of", 1 << I32, dev, 2, e[0], e[1], &row_of, NULL) ||
       !result(a[2], "dx", 1u << r.dtype, dev, e[0], r.cols, &x) || !stream_of(a[3], dev, &stream))
     return NULL;
@@ -291,7 +313,7 @@ static PyObject* py_moe_combine(PyObject* self, PyObject* const* a, Py_ssize_t n
   void *w, *row_of, *stream;
   int64_t e[2];
   long dev;
-  if (!count_is(n, 5) || (dev = first_device(a[0], "y")) < 0 || !matrix(a[0], "y", FLOATING, dev, &y) ||
+  if (!bound() || !count_is(n, 5) || (dev = first_device(a[0], "y")) < 0 || !matrix(a[0], "y", FLOATING, dev, &y) ||
       !routing(a[2], "row_of", e) || !dense(a[2], "row_of", 1 << I32, dev, 2, e[0], e[1], &row_of, NULL) ||
       !dense(a[1], "weights", 1 << FP32, dev, 2, e[0], e[1], &w, NULL) ||
       !result(a[3], "out", 1u << y.dtype, dev, e[0], y.cols, &o) || !stream_of(a[4], dev, &stream))
@@ -305,7 +327,7 @@ static PyObject* py_moe_combine_bwd(PyObject* self, PyObject* const* a, Py_ssize
   void *w, *row_of, *dw, *stream;
   int64_t e[2];
   long dev;
-  if (!count_is(n, 7) || (dev = first_device(a[0], "dout")) < 0 || !matrix(a[0], "dout", FLOATING, dev, &g) ||
+  if (!bound() || !count_is(n, 7) || (dev = first_device(a[0], "dout")) < 0 || !matrix(a[0], "dout", FLOATING, dev, &g) ||
       !routing(a[3], "row_of", e) || !dense(a[3], "row_of", 1 << I32, dev, 2, g.rows, e[1], &row_of, NULL) ||
       !matrix(a[1], "y", 1u << g.dtype, dev, &y))
     return NULL;
@@ -351,6 +373,7 @@ static PyObject* py_bind(PyObject* self, PyObject* args) {
 
 static PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, "bind(addresses, dtypes, error, current_device, current_stream)"},
+    {"on_first_call", py_on_first_call, METH_O, "on_first_call(f): f() is called before the first operator and calls bind()"},
     {"quant_i8", (PyCFunction)(void (*)(void))py_quant_i8, METH_FASTCALL, "(x, q, scale, stream)"},
     {"gemm_i8", (PyCFunction)(void (*)(void))py_gemm_i8, METH_FASTCALL, "(a, scale_a, b, scale_b, out, bias, stream)"},
     {"gemm_i8_grouped", (PyCFunction)(void (*)(void))py_gemm_i8_grouped, METH_FASTCALL,

@@ -18,7 +18,6 @@ import ctypes
 import os
 
 import numpy as np
-import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libentwine.so")
@@ -122,6 +121,7 @@ def _ptr(t):
 
 def _stream(s):
     if s is None:
+        import torch
         return torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
@@ -282,7 +282,9 @@ OPS_OPT_WAIT_BUDGET_NS, OPS_OPT_WITHHOLD_BLOCK = 1, 2
 
 
 def _bind_ops():
-    """Hands the marshalling module the library's entry points and what it asks torch for."""
+    """Hands the marshalling module the library's entry points and what it asks torch for, before the operators' first
+    call: with raw addresses and stream handles the rest of the module needs no torch."""
+    import torch
     addresses = {name: ctypes.cast(getattr(_lib, name), _vp).value for name in OP_SYMBOLS}
     dtypes = (torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.int32, torch.int64)
     # the current stream's handle where torch gives it alone: building a Stream object takes 3 us, as long as a short kernel
@@ -290,7 +292,7 @@ def _bind_ops():
     _opcalls.bind(addresses, dtypes, EntwineError, torch.cuda.current_device, stream)
 
 
-_bind_ops()
+_opcalls.on_first_call(_bind_ops)
 
 
 def quant_i8(x, q, scale, stream=None):
