@@ -1,5 +1,8 @@
 """Builds the C-ABI library in-tree with nvcc for sm_100a (libentwine.so next to this file), and with the C compiler the
-extension module that marshals the operators' arguments (_opcalls.so)."""
+extension module that marshals the operators' arguments (_opcalls, for the running interpreter).
+
+The library needs nothing of Python.  Where the module cannot be built (no Python.h), the library stands all the same, with
+a warning: plans work, and the operators say why they do not."""
 from __future__ import annotations
 
 import os
@@ -13,6 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libentwine.so")
 OPCALLS = os.path.join(HERE, "_opcalls.so")
+OPCALLS_SOURCE = os.path.join(CSRC, "opcalls.c")
 INCLUDE = os.path.join(ROOT, "include")
 SOURCES = ["plan.cc", "entwine_kernels.cu", "quant.cu", "moe.cu", "gemm_i8.cu"]
 
@@ -25,31 +29,48 @@ def _nvcc() -> str:
 
 
 STAMP = LIB + ".srchash"
+OPCALLS_STAMP = OPCALLS + ".srchash"
 
 
-def _source_hash() -> str:
-    """Hash of everything the library is built from (file times do not survive a copy of the tree)."""
+def _hash(files, *settings) -> str:
+    """Hash of what a file is built from (file times do not survive a copy of the tree)."""
     import hashlib
     h = hashlib.sha256()
-    deps = sorted(os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d))
-    for d in deps:
+    for d in files:
         h.update(os.path.basename(d).encode())
         with open(d, "rb") as f:
             h.update(f.read())
-    h.update(os.environ.get("ENTWINE_NVCC_FLAGS", "").encode())
+    for v in settings:
+        h.update(v.encode())
     return h.hexdigest()
 
 
+def _source_hash() -> str:
+    deps = sorted(os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d))
+    return _hash([d for d in deps if d != OPCALLS_SOURCE], os.environ.get("ENTWINE_NVCC_FLAGS", ""))
+
+
+def _opcalls_hash() -> str:
+    return _hash([OPCALLS_SOURCE])
+
+
+def _stamped(built: str, stamp: str, want: str) -> bool:
+    if not (os.path.exists(built) and os.path.exists(stamp)):
+        return False
+    with open(stamp) as f:
+        return f.read().strip() == want
+
+
+def _stamp(stamp: str, value: str) -> None:
+    with open(stamp, "w") as f:
+        f.write(value + "\n")
+
+
 def needs_build() -> bool:
-    if not all(os.path.exists(f) for f in (LIB, OPCALLS, STAMP)):
-        return True
-    with open(STAMP) as f:
-        return f.read().strip() != _source_hash()
+    return not (_stamped(LIB, STAMP, _source_hash()) and _stamped(OPCALLS, OPCALLS_STAMP, _opcalls_hash()))
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
+def _build_library(verbose: bool) -> None:
     flags = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-Xcompiler", "-fPIC",
              "-I", INCLUDE, "-I", CSRC]
     if verbose:
@@ -59,8 +80,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
         # the sources side by side, then one link
         objs = [os.path.join(tmp, src + ".o") for src in SOURCES]
         cmds = [[_nvcc(), *flags, "-x", "cu", "-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
-        cmds.append([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I",
-                     sysconfig.get_paths()["include"], os.path.join(CSRC, "opcalls.c"), "-o", OPCALLS])
         cmds = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in cmds]
         outs = [(p.communicate()[0], p.returncode) for p in cmds]
         if all(rc == 0 for _, rc in outs):
@@ -70,9 +89,34 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose or rc != 0:
             sys.stderr.write(text)
     if any(rc != 0 for _, rc in outs):
-        raise RuntimeError("building libentwine.so or _opcalls.so failed")
-    with open(STAMP, "w") as f:
-        f.write(_source_hash() + "\n")
+        raise RuntimeError("building libentwine.so failed")
+    _stamp(STAMP, _source_hash())
+
+
+def _build_opcalls() -> None:
+    """Leaves no module where it cannot build one: a stale one is not loaded in its place."""
+    for old in (OPCALLS, OPCALLS_STAMP):
+        if os.path.exists(old):
+            os.remove(old)
+    try:
+        res = subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I",
+                              sysconfig.get_paths()["include"], OPCALLS_SOURCE, "-o", OPCALLS], capture_output=True, text=True)
+        text, failed = res.stdout + res.stderr, res.returncode != 0
+    except OSError as e:
+        text, failed = f"{e}\n", True
+    sys.stderr.write(text)
+    if failed:
+        sys.stderr.write("warning: building _opcalls failed (above); libentwine.so stands, the operators of entwine_ops.h "
+                         "cannot be called from Python\n")
+        return
+    _stamp(OPCALLS_STAMP, _opcalls_hash())
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    if force or not _stamped(LIB, STAMP, _source_hash()):
+        _build_library(verbose)
+    if force or not _stamped(OPCALLS, OPCALLS_STAMP, _opcalls_hash()):
+        _build_opcalls()
     return LIB
 
 

@@ -1,7 +1,8 @@
 """ctypes binding over the C-ABI library (include/entwine.h, include/entwine_ops.h).
 
 Argument marshalling only: every step of the path runs in the CUDA library.  Importing this
-module fails loudly if libentwine.so has not been built (there is no fallback).
+module fails loudly if libentwine.so has not been built, an operator if its marshalling module has not (there is
+no fallback).
 Device-buffer arguments are torch CUDA tensors (bf16, contiguous) or raw integer addresses;
 `stream` is a torch.cuda.Stream, a raw handle or None (the current torch stream).
 
@@ -26,10 +27,26 @@ if not os.path.exists(LIB_PATH):
         f"{LIB_PATH} is missing: build it with `python -m paper_2609_11562_b200.build` "
         "(or __graft_entry__.build()); this package has no CPU fallback")
 _lib = ctypes.CDLL(LIB_PATH)
+
+
+class _NoOpcalls:
+    """Stands where the operators' marshalling module could not be loaded: everything else works without it."""
+
+    def __init__(self, why: ImportError):
+        self._why = why
+
+    def on_first_call(self, f):
+        pass
+
+    def __getattr__(self, name):
+        raise ImportError(f"the operators need the extension module _opcalls, which could not be loaded ({self._why}): "
+                          "build it with `python -m paper_2609_11562_b200.build`") from self._why
+
+
 try:
     from . import _opcalls
 except ImportError as e:
-    raise ImportError("_opcalls.so is missing: build it with `python -m paper_2609_11562_b200.build`") from e
+    _opcalls = _NoOpcalls(e)
 
 ORDER_ROW_MAJOR, ORDER_INTERLEAVED, ORDER_M_MAJOR = 0, 1, 2
 OK, ERR_INVALID, ERR_RESOURCES, ERR_CUDA, ERR_TIMEOUT, ERR_INTERNAL = 0, -1, -2, -3, -4, -5
