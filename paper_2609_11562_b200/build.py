@@ -15,7 +15,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libentwine.so")
-OPCALLS = os.path.join(HERE, "_opcalls.so")
+# named for this interpreter, whose binary interface it uses: another one finds none instead of a wrong one
+OPCALLS = os.path.join(HERE, "_opcalls" + sysconfig.get_config_var("EXT_SUFFIX"))
+UNTAGGED = os.path.join(HERE, "_opcalls.so")  # as it was once named: any interpreter would load it
 OPCALLS_SOURCE = os.path.join(CSRC, "opcalls.c")
 INCLUDE = os.path.join(ROOT, "include")
 SOURCES = ["plan.cc", "entwine_kernels.cu", "quant.cu", "moe.cu", "gemm_i8.cu"]
@@ -66,8 +68,15 @@ def _stamp(stamp: str, value: str) -> None:
         f.write(value + "\n")
 
 
+def _beside(path: str) -> str:
+    """A name in the same folder, to build at before it takes the place of `path` at once: who loads that meanwhile has
+    the old file or the new one, whole."""
+    return os.path.join(HERE, f"tmp{os.getpid()}_{os.path.basename(path)}")
+
+
 def needs_build() -> bool:
-    return not (_stamped(LIB, STAMP, _source_hash()) and _stamped(OPCALLS, OPCALLS_STAMP, _opcalls_hash()))
+    return os.path.exists(UNTAGGED) or not (_stamped(LIB, STAMP, _source_hash()) and
+                                            _stamped(OPCALLS, OPCALLS_STAMP, _opcalls_hash()))
 
 
 def _build_library(verbose: bool) -> None:
@@ -83,39 +92,41 @@ def _build_library(verbose: bool) -> None:
         cmds = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in cmds]
         outs = [(p.communicate()[0], p.returncode) for p in cmds]
         if all(rc == 0 for _, rc in outs):
-            res = subprocess.run([_nvcc(), *flags, "-shared", *objs, "-o", LIB], capture_output=True, text=True)
+            res = subprocess.run([_nvcc(), *flags, "-shared", *objs, "-o", _beside(LIB)], capture_output=True, text=True)
             outs.append((res.stdout + res.stderr, res.returncode))
     for text, rc in outs:
         if verbose or rc != 0:
             sys.stderr.write(text)
     if any(rc != 0 for _, rc in outs):
         raise RuntimeError("building libentwine.so failed")
+    os.replace(_beside(LIB), LIB)
     _stamp(STAMP, _source_hash())
 
 
 def _build_opcalls() -> None:
     """Leaves no module where it cannot build one: a stale one is not loaded in its place."""
-    for old in (OPCALLS, OPCALLS_STAMP):
-        if os.path.exists(old):
-            os.remove(old)
     try:
         res = subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I",
-                              sysconfig.get_paths()["include"], OPCALLS_SOURCE, "-o", OPCALLS], capture_output=True, text=True)
+                              sysconfig.get_paths()["include"], OPCALLS_SOURCE, "-o", _beside(OPCALLS)], capture_output=True, text=True)
         text, failed = res.stdout + res.stderr, res.returncode != 0
     except OSError as e:
         text, failed = f"{e}\n", True
     sys.stderr.write(text)
+    for old in (UNTAGGED, UNTAGGED + ".srchash", *((OPCALLS_STAMP, OPCALLS) if failed else ())):
+        if os.path.exists(old):
+            os.remove(old)
     if failed:
         sys.stderr.write("warning: building _opcalls failed (above); libentwine.so stands, the operators of entwine_ops.h "
                          "cannot be called from Python\n")
         return
+    os.replace(_beside(OPCALLS), OPCALLS)
     _stamp(OPCALLS_STAMP, _opcalls_hash())
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     if force or not _stamped(LIB, STAMP, _source_hash()):
         _build_library(verbose)
-    if force or not _stamped(OPCALLS, OPCALLS_STAMP, _opcalls_hash()):
+    if force or os.path.exists(UNTAGGED) or not _stamped(OPCALLS, OPCALLS_STAMP, _opcalls_hash()):
         _build_opcalls()
     return LIB
 

@@ -3,6 +3,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 import pytest
 
@@ -53,3 +54,25 @@ def test_a_module_of_other_sources_is_not_left_in_place(tree):
         f.write("/* changed */\n")
     r = _python(tree, USE, CC="false")
     assert r.stdout.startswith("ImportError"), r.stderr
+
+
+def test_the_module_is_named_for_its_interpreter(tree):
+    """One that any interpreter would load is taken away, and the files are put in place whole."""
+    package = tree / "paper_2609_11562_b200"
+    (package / "_opcalls.so").write_bytes(b"built by another interpreter")
+    assert _python(tree, USE).stdout.startswith("EntwineError")
+    built = sorted(f.name for f in package.iterdir() if f.name.endswith(".so"))
+    assert built == ["_opcalls" + sysconfig.get_config_var("EXT_SUFFIX"), "libentwine.so"]
+
+
+def test_a_rebuilt_module_does_not_touch_the_loaded_one(tree):
+    """The module's file is replaced, not written over: the loaded one keeps its own."""
+    r = _python(tree, USE + """
+import os
+old = os.open(B.OPCALLS, os.O_RDONLY)
+before = os.read(old, 1 << 24)
+B._build_opcalls()
+os.lseek(old, 0, 0)
+assert os.read(old, 1 << 24) == before and os.fstat(old).st_ino != os.stat(B.OPCALLS).st_ino
+""")
+    assert r.returncode == 0, r.stderr
