@@ -230,8 +230,7 @@ int quant_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, void* q, 
   int log_threads = 5;
   while ((2 << log_threads) <= kMaxRowThreads && (int64_t(most) << log_threads) < pieces) ++log_threads;
   const int64_t each = (pieces + (1 << log_threads) - 1) >> log_threads;
-  auto kernel = each <= 2 ? quant_rows_kernel<T, 2> : each <= 4 ? quant_rows_kernel<T, 4>
-                : each <= 8 ? quant_rows_kernel<T, 8> : quant_rows_kernel<T, kMaxPieces>;
+  auto kernel = each <= 2 ? quant_rows_kernel<T, 2> : each <= 4 ? quant_rows_kernel<T, 4> : quant_rows_kernel<T, kMaxPieces>;
   const int threads = std::max(64, 1 << log_threads), per_cta = threads >> log_threads;
   kernel<<<unsigned((rows + per_cta - 1) / per_cta), threads, 0, stream>>>(xt, rows, int(cols), ldx, qt, ldq, scale,
                                                                            log_threads);
