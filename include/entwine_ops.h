@@ -47,7 +47,8 @@ int entwine_quant_i8(const void* x, int dtype, int64_t rows, int64_t cols, int64
  *   ldb multiples of 16 (K itself may be any length: what follows it in a row is not read into the sum)
  *   scale_a [M], scale_b [N], bias [N] fp32; bias may be NULL
  *   C [M, N], c_dtype ENTWINE_BF16, ENTWINE_FP16 or ENTWINE_FP32
- * M = 0 is allowed and does nothing; N >= 1; 1 <= K <= 131071 (the largest sum fits int32).
+ * M = 0 is allowed and does nothing, M <= 2147418111; 1 <= N <= 2147483392; 1 <= K <= 131071 (the largest sum fits
+ * int32).
  * Errors: ENTWINE_ERR_INVALID, ENTWINE_ERR_CUDA.  Device-side waits are bounded: see entwine_ops_status.
  */
 int entwine_gemm_i8(const void* A, int64_t lda, const float* scale_a, const void* B, int64_t ldb,

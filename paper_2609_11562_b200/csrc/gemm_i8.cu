@@ -22,6 +22,8 @@ constexpr int kMaxSplit = 8;
 constexpr int kMaxGroups = 1024;
 constexpr int64_t kMaxK = 131071;    // 128 * 128 * K < 2^31
 constexpr int64_t kMaxExtent = 2147483647;
+constexpr int64_t kMaxRows = kMaxExtent - 65536;                  // row and channel numbers of the last tiles, which reach
+constexpr int64_t kMaxChannels = kMaxExtent - 255;                // behind the matrix, fit 32 bits
 
 // Bounded waits that ran out on this device.  It only grows: nobody's reading of it takes a failure from anybody else.
 __device__ unsigned long long g_waits_failed;
@@ -718,7 +720,7 @@ int gemm(const void* A, int64_t lda, const float* scale_a, const void* B, int64_
          const float* scale_b, const float* bias, const int32_t* offsets, void* C, int c_dtype, int64_t ldc, int64_t M,
          int64_t N, int64_t K, int64_t G, void* stream) {
   if (c_dtype != ENTWINE_BF16 && c_dtype != ENTWINE_FP16 && c_dtype != ENTWINE_FP32) return ENTWINE_ERR_INVALID;
-  if (M < 0 || M > kMaxExtent - 65536 || N < 1 || N > kMaxExtent || K < 1 || K > kMaxK || G < 1 || G > kMaxGroups ||
+  if (M < 0 || M > kMaxRows || N < 1 || N > kMaxChannels || K < 1 || K > kMaxK || G < 1 || G > kMaxGroups ||
       G * N > kMaxExtent || ldc < N || lda < K || ldb < K)
     return ENTWINE_ERR_INVALID;
   // a matrix of one row has no row distance, a single expert no distance to the next
