@@ -7,11 +7,13 @@
  *
  * These calls have no plan: each is complete in itself, keeps nothing from one call for the next, and needs no
  * workspace.  Any of them may be captured into a CUDA graph (its first call too), and calls on different streams
- * may overlap as far as their buffers allow.  Outputs must not overlap inputs or each other.  The same inputs give the same bits on every call.
+ * may overlap as far as their buffers allow.  Outputs must not overlap inputs or each other.  The same inputs give the
+ * same bits on every call.
  *
  * Matrices are row-major; ld* is the distance between two rows in elements, at least the row's length.  Element
  * pointers need the alignment of their element only, except where a function says more; rows that start on
- * 16-byte boundaries are the fastest.
+ * 16-byte boundaries are the fastest (K or H need not fill them).  Contiguous rows of an odd number of 16-bit elements
+ * cost the dispatch a tenth more, the return, its gradients and the quantiser about twice as much.
  */
 #ifndef ENTWINE_OPS_H_
 #define ENTWINE_OPS_H_
@@ -42,7 +44,9 @@ int entwine_quant_i8(const void* x, int dtype, int64_t rows, int64_t cols, int64
 /*
  * entwine_gemm_i8 - the row-parallel layer's product in 8-bit integers, scaled per token and per output channel:
  *   C[m][n] = scale_a[m] scale_b[n] sum_k A[m][k] B[n][k] + bias[n]
- * The int32 sum is exact, the scaling is fp32, C is rounded once.
+ * The int32 sum is exact, the scaling is fp32, C is rounded once.  In fp32 the order is ((sum scale_a) scale_b) + bias:
+ * where |sum| scale_a passes fp32's range (a token scale of 2^97 is the least that can do it) C is infinite, whatever
+ * scale_b.
  *   A [M, K] int8, B [N, K] int8 (K contiguous, as entwine.h's default layout): both 16-byte aligned with lda and
  *   ldb multiples of 16 (K itself may be any length: what follows it in a row is not read into the sum)
  *   scale_a [M], scale_b [N], bias [N] fp32; bias may be NULL

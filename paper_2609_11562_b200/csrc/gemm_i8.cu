@@ -292,9 +292,9 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
 // many tokens: CTA pairs, persistent
 // ------------------------------------------------------------------------------------------
 // Two CTAs of a cluster compute 256 channels x up to 256 tokens (tcgen05 cta_group::2: 128 channels each, each loading
-// half of the tokens), so that an SM takes in 64 bytes per cycle at the full MMA rate instead of 96.  A tile is as
-// wide as its tokens, in steps of 32: an expert's last rows cost what they are.  Two accumulators in TMEM: the
-// epilogue of a tile runs beside the products of the next.
+// half of the tokens), so that an SM takes in 64 bytes per cycle at the full MMA rate instead of 96.  A tile's products
+// are as wide as its tokens, in steps of 32 (what is loaded is not: a whole tile's tokens, however few the expert has).
+// Two accumulators in TMEM: the epilogue of a tile runs beside the products of the next.
 struct PairTile {
   int g, m0, rows, n0;
 };

@@ -317,8 +317,8 @@ __global__ void __launch_bounds__(kThreads, 5) moe_combine_kernel(const T* y, in
 }
 
 // The same for rows that start anywhere: a thread takes an aligned piece of the token and puts the pieces of its rows
-// together from the words around them.  8192 tokens of 4095 bf16, eight experts each: 209 us (94 where rows start on
-// 16-byte boundaries); fp32 134.
+// together from the words around them.  8192 tokens of 4095 bf16, eight experts each: 209 to 219 us (94 to 99 of 4096,
+// where rows start on 16-byte boundaries); fp32 134.
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4) moe_combine_anywhere_kernel(const T* y, int64_t n_rows, int64_t H,
                                                                            int64_t ldy, const float* w,
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 4) moe_combine_bwd_kernel(const T* d
 }
 
 // The same for rows that start anywhere, one row of dy after another in its own aligned pieces (8192 tokens of 4095
-// bf16, eight experts each: 317 to 388 us, aligned 174).
+// bf16, eight experts each: 317 to 396 us, aligned 174 to 181).
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4) moe_combine_bwd_anywhere_kernel(const T* dout, int64_t H, int64_t ldo,
                                                                                const T* y, int64_t n_rows, int64_t ldy,

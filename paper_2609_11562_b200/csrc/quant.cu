@@ -189,7 +189,8 @@ __global__ void __launch_bounds__(kMaxRowThreads) quant_rows_kernel(const T* x, 
 }
 
 // One CTA per row, the row read twice: rows too long for the registers, and rows that do not start on 16-byte
-// boundaries (V = 1).
+// boundaries, element by element (V = 1).  8192 contiguous rows of 3583 bf16 take 37 us (padded to 3584: 20), of 1021 18 us;
+// four rows of 65536 fp32 23 us.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) quant_long_rows_kernel(const T* x, int64_t cols, int64_t ldx, int8_t* q,
                                                                    int64_t ldq, float* scale) {
