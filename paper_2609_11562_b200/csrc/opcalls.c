@@ -57,6 +57,7 @@ static int bound(void) {
 }
 static PyObject* py_on_first_call(PyObject* self, PyObject* f) {
   Py_XSETREF(binder, Py_NewRef(f));
+  Py_CLEAR(error_class); /* bound anew at the next call (a reloaded package has another error class) */
   Py_RETURN_NONE;
 }
 

@@ -43,3 +43,19 @@ print('ok')
 def test_importing_the_binding_does_not_import_torch():
     r = _python("import sys\nfrom paper_2609_11562_b200 import entwine\nprint('torch' in sys.modules)")
     assert r.stdout.strip() == "False", r.stderr
+
+
+def test_operators_follow_a_reloaded_binding():
+    """After a reload the operators raise the new module's error, although they were bound to the old one's."""
+    r = _python("""
+import importlib
+from paper_2609_11562_b200 import entwine as E
+for _ in range(2):
+    try:
+        E.quant_i8([[1.0]], None, None, stream=0)
+    except E.EntwineError as e:
+        assert e.code == E.ERR_INVALID
+    E = importlib.reload(E)
+print('ok')
+""")
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stderr
