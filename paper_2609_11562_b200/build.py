@@ -20,7 +20,8 @@ OPCALLS = os.path.join(HERE, "_opcalls" + sysconfig.get_config_var("EXT_SUFFIX")
 UNTAGGED = os.path.join(HERE, "_opcalls.so")  # as it was once named: any interpreter would load it
 OPCALLS_SOURCE = os.path.join(CSRC, "opcalls.c")
 INCLUDE = os.path.join(ROOT, "include")
-SOURCES = ["plan.cc", "entwine_kernels.cu", "quant.cu", "moe.cu", "gemm_i8.cu"]
+SOURCES = ["plan.cc", "entwine_kernels.cu", "quant.cu", "moe.cu", "gemm_i8.cu", "mxf4.cu", "gemm_mxf4.cu",
+           "norm.cu"]
 
 
 def _nvcc() -> str:

@@ -747,8 +747,9 @@ int gemm(const void* A, int64_t lda, const float* scale_a, const void* B, int64_
   P.N = int(N);
   P.K = int(K);
   P.G = int(G);
-  P.withhold = int(g_withhold.load(std::memory_order_relaxed));
-  P.wait_ns = static_cast<unsigned long long>(g_wait_budget_ns.load(std::memory_order_relaxed));
+  const WaitSettings w = wait_settings();
+  P.withhold = w.withhold;
+  P.wait_ns = w.budget_ns;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   switch (c_dtype) {
     case ENTWINE_BF16: return run_as<__nv_bfloat16>(A, lda, B, ldb, expert_stride, P, s);
@@ -758,6 +759,12 @@ int gemm(const void* A, int64_t lda, const float* scale_a, const void* B, int64_
 }
 
 }  // namespace
+
+WaitSettings wait_settings() {
+  return {static_cast<unsigned long long>(g_wait_budget_ns.load(std::memory_order_relaxed)),
+          int(g_withhold.load(std::memory_order_relaxed))};
+}
+
 }  // namespace entwine
 
 using namespace entwine;
@@ -799,11 +806,12 @@ int entwine_ops_failed_waits(void* stream, uint64_t* count) {
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
   if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) return launched(cudaErrorUnknown);
   if (capture != cudaStreamCaptureStatusNone) return ENTWINE_ERR_INVALID;
-  unsigned long long n = 0;
+  unsigned long long n = 0, n4 = 0;
   cudaError_t e = cudaMemcpyFromSymbolAsync(&n, g_waits_failed, sizeof(n), 0, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = mxf4_failed_waits(&n4, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) return launched(e);
-  *count = n;
+  *count = n + n4;
   return ENTWINE_OK;
 }
 

@@ -1,0 +1,794 @@
+// Dropout from a counter-based generator (entwine_dropout), layer norm of residual + dropout(x) and its gradients
+// (entwine_layer_norm, entwine_layer_norm_bwd).
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "ops_common.cuh"
+
+namespace entwine {
+namespace {
+
+constexpr int kGroup = 8;  // columns that one call of the generator decides on
+constexpr int64_t kMaxCols = 2147483647 - 65536;  // column numbers of a CTA's last, idle threads fit 32 bits
+constexpr int64_t kMaxRows = 2147483647;
+
+// ------------------------------------------------------------------------------------------
+// the generator
+// ------------------------------------------------------------------------------------------
+// Philox4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): a
+// bijection of a 128-bit counter under a 64-bit key.  The counter is (column / 8, row, offset), the key the seed; its
+// four words are eight 16-bit numbers, one for each column.  16 bits decide whether an element is kept with probability
+// 1 - t / 65536 exactly, and what is kept is multiplied with 65536 / (65536 - t): the expectation is exact, p itself is
+// taken to the nearest 2^-16.  With 32 bits an element the generator, about 70 instructions a call, would be the bound
+// instead of the memory.
+struct Dropout {
+  const int64_t* rng;  // {seed, offset}
+  uint32_t t;          // elements whose number is below are dropped
+  float scale;
+  uint32_t row0;       // number of the first row
+};
+
+struct Stream {
+  uint32_t k0, k1, o0, o1;
+  __device__ __forceinline__ explicit Stream(const int64_t* rng) {
+    const uint64_t seed = rng ? uint64_t(rng[0]) : 0, offset = rng ? uint64_t(rng[1]) : 0;
+    k0 = uint32_t(seed);
+    k1 = uint32_t(seed >> 32);
+    o0 = uint32_t(offset);
+    o1 = uint32_t(offset >> 32);
+  }
+  __device__ __forceinline__ void words(uint32_t group, uint32_t row, uint32_t (&c)[4]) const {
+    uint32_t x = group, y = row, z = o0, w = o1, a = k0, b = k1;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+      const uint64_t m = uint64_t(x) * 0xD2511F53u, n = uint64_t(z) * 0xCD9E8D57u;
+      x = uint32_t(n >> 32) ^ y ^ a;
+      y = uint32_t(n);
+      z = uint32_t(m >> 32) ^ w ^ b;
+      w = uint32_t(m);
+      a += 0x9E3779B9u;
+      b += 0xBB67AE85u;
+    }
+    c[0] = x;
+    c[1] = y;
+    c[2] = z;
+    c[3] = w;
+  }
+};
+__device__ __forceinline__ bool kept(const uint32_t (&c)[4], int e, uint32_t t) {
+  return ((c[e / 2] >> (16 * (e & 1))) & 0xffffu) >= t;
+}
+// A dropped element is 0 whatever it held.
+__device__ __forceinline__ void drop8(const Stream& s, const Dropout& d, uint32_t row, uint32_t group, float (&f)[8]) {
+  uint32_t c[4];
+  s.words(group, row, c);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = kept(c, e, d.t) ? f[e] * d.scale : 0.0f;
+}
+__device__ __forceinline__ float drop1(const Stream& s, const Dropout& d, uint32_t row, uint32_t col, float f) {
+  uint32_t c[4];
+  s.words(col / kGroup, row, c);
+  uint32_t w = c[0];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) w = int(col % kGroup) / 2 == i ? c[i] : w;
+  return ((w >> (16 * (col & 1))) & 0xffffu) >= d.t ? f * d.scale : 0.0f;
+}
+
+// ------------------------------------------------------------------------------------------
+// groups of eight elements
+// ------------------------------------------------------------------------------------------
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+  if constexpr (VEC) {
+    constexpr int V = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8 / V; ++i) {
+      float g[V];
+      unpack<T, V>(reinterpret_cast<const Piece<T, V>*>(p)[i], g);
+#pragma unroll
+      for (int e = 0; e < V; ++e) f[i * V + e] = g[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = Elem<T>::up(p[e]);
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
+  if constexpr (VEC) {
+    constexpr int V = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8 / V; ++i) {
+      float g[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) g[e] = f[i * V + e];
+      reinterpret_cast<Piece<T, V>*>(p)[i] = pack<T, V>(g);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = Elem<T>::down(f[e]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float rounded(float f) {
+  return Elem<T>::up(Elem<T>::down(f));
+}
+
+// Weights: of the rows' type, or fp32.
+template <typename T>
+struct Weights {
+  const void* at;
+  bool wide;
+  template <bool VEC>
+  __device__ __forceinline__ void load(int col, float (&f)[8]) const {
+    if (wide) load8<float, VEC>(static_cast<const float*>(at) + col, f);
+    else load8<T, VEC>(static_cast<const T*>(at) + col, f);
+  }
+  __device__ __forceinline__ float one(int col) const {
+    return wide ? static_cast<const float*>(at)[col] : Elem<T>::up(static_cast<const T*>(at)[col]);
+  }
+};
+
+// ------------------------------------------------------------------------------------------
+// dropout
+// ------------------------------------------------------------------------------------------
+struct DropParams {
+  const void* x;
+  const void* residual;
+  void* out;
+  int64_t rows, ldx, ldr, ldo;
+  int cols, row_threads;
+  Dropout d;
+};
+
+constexpr int kDropThreads = 256;
+
+// P groups of eight elements a thread; a CTA takes as many rows as fit.
+template <typename T, int P, bool VEC>
+__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams a) {
+  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
+  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
+  if (row >= a.rows) return;
+  const Stream rng(a.d.rng);
+  const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+  const T* const r = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
+  T* const out = static_cast<T*>(a.out) + row * a.ldo;
+  const uint32_t number = a.d.row0 + uint32_t(row);
+  const int full = a.cols / kGroup;
+  for (int64_t g0 = int64_t(blockIdx.y) * P * a.row_threads; g0 < full; g0 += int64_t(gridDim.y) * P * a.row_threads) {
+    float f[P][8], res[P][8];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int64_t g = g0 + i * a.row_threads + lane;
+      if (g < full) {
+        load8<T, VEC>(x + g * kGroup, f[i]);
+        if (r) load8<T, VEC>(r + g * kGroup, res[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int64_t g = g0 + i * a.row_threads + lane;
+      if (g < full) {
+        drop8(rng, a.d, number, uint32_t(g), f[i]);
+        if (r) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[i][e] += res[i][e];
+        }
+        store8<T, VEC>(out + g * kGroup, f[i]);
+      }
+    }
+  }
+  const int col = full * kGroup + lane;
+  if (blockIdx.y == 0 && lane < kGroup && col < a.cols) {
+    float f = drop1(rng, a.d, number, uint32_t(col), Elem<T>::up(x[col]));
+    if (r) f += Elem<T>::up(r[col]);
+    out[col] = Elem<T>::down(f);
+  }
+}
+
+template <typename T>
+int run_dropout(DropParams a, cudaStream_t stream) {
+  const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.out, a.ldo, sizeof(T)) &&
+                   (!a.residual || aligned_rows(a.residual, a.ldr, sizeof(T)));
+  constexpr int P = 2;
+  const int64_t full = a.cols / kGroup;
+  a.row_threads = 8;
+  while (a.row_threads < kDropThreads && int64_t(a.row_threads) * P < full) a.row_threads *= 2;
+  const int per_cta = kDropThreads / a.row_threads;
+  const int64_t chunks = std::max<int64_t>(1, (full + P * a.row_threads - 1) / (P * a.row_threads));
+  const dim3 grid(unsigned((a.rows + per_cta - 1) / per_cta), unsigned(std::min<int64_t>(chunks, 65535)));
+  auto kernel = vec ? dropout_kernel<T, P, true> : dropout_kernel<T, P, false>;
+  kernel<<<grid, kDropThreads, 0, stream>>>(a);
+  return launched(cudaSuccess);
+}
+
+// ------------------------------------------------------------------------------------------
+// layer norm
+// ------------------------------------------------------------------------------------------
+struct NormParams {
+  const void* x;
+  const void* residual;
+  const void* weight;
+  const void* bias;
+  void* hidden;
+  void* out;
+  float* mean;
+  float* rstd;
+  int64_t rows, ldx, ldr, ldh, ldo;
+  int cols, row_threads, wide;
+  float eps;
+  Dropout d;
+};
+
+// Sum over the threads of a row (row_threads of them, whole warps, from warp first_warp on).
+__device__ __forceinline__ float row_sum(float v, float* part, int first_warp, int warps) {
+  v = warp_sum(v);
+  if (warps == 1) return v;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = 0.0f;
+  for (int w = 0; w < warps; ++w) v += part[first_warp + w];
+  return v;
+}
+
+// A row in registers: up to P groups a thread and one element of the last, incomplete group.  The mean first, then the
+// mean of the squared distances from it: no difference of large sums.
+template <typename T, int P, bool VEC>
+__global__ void __launch_bounds__(1024) norm_rows_kernel(const NormParams a) {
+  __shared__ float part[2][32];
+  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
+  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
+  const bool there = row < a.rows;
+  const int full = a.cols / kGroup, tail = full * kGroup + lane;
+  const bool has_tail = there && lane < kGroup && tail < a.cols;
+  const uint32_t number = a.d.row0 + uint32_t(row);
+  const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+  const T* const res = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
+  T* const hidden = a.hidden ? static_cast<T*>(a.hidden) + row * a.ldh : nullptr;
+  float h[P][8], last = 0.0f, sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int g = i * a.row_threads + lane;
+    if (there && g < full) {
+      load8<T, VEC>(x + g * kGroup, h[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] = 0.0f;
+    }
+  }
+  if (has_tail) last = Elem<T>::up(x[tail]);
+  if (a.d.rng || res) {
+    float r[P][8];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int g = i * a.row_threads + lane;
+      if (res && there && g < full) load8<T, VEC>(res + g * kGroup, r[i]);
+    }
+    const Stream rng(a.d.rng);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int g = i * a.row_threads + lane;
+      if (there && g < full) {
+        if (a.d.rng) drop8(rng, a.d, number, uint32_t(g), h[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[i][e] = rounded<T>(res ? h[i][e] + r[i][e] : h[i][e]);
+        if (hidden) store8<T, VEC>(hidden + g * kGroup, h[i]);
+      }
+    }
+    if (has_tail) {
+      if (a.d.rng) last = drop1(rng, a.d, number, uint32_t(tail), last);
+      last = rounded<T>(res ? last + Elem<T>::up(res[tail]) : last);
+      if (hidden) hidden[tail] = Elem<T>::down(last);
+    }
+  } else if (hidden && there) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int g = i * a.row_threads + lane;
+      if (g < full) store8<T, VEC>(hidden + g * kGroup, h[i]);
+    }
+    if (has_tail) hidden[tail] = Elem<T>::down(last);
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += h[i][e];
+  sum += last;
+  const int first_warp = slot * (a.row_threads / 32), warps = a.row_threads / 32;
+  const float mean = row_sum(sum, part[0], first_warp, warps) / float(a.cols);
+  float square = 0.0f;
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    if (i * a.row_threads + lane < full) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) square = fmaf(h[i][e] - mean, h[i][e] - mean, square);
+    }
+  if (has_tail) square = fmaf(last - mean, last - mean, square);
+  const float rstd = 1.0f / sqrtf(row_sum(square, part[1], first_warp, warps) / float(a.cols) + a.eps);
+  if (!there) return;
+  if (lane == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  const Weights<T> weight{a.weight, a.wide != 0}, bias{a.bias, a.wide != 0};
+  T* const out = static_cast<T*>(a.out) + row * a.ldo;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int g = i * a.row_threads + lane;
+    if (g < full) {
+      float w[8], b[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      weight.template load<VEC>(g * kGroup, w);
+      if (a.bias) bias.template load<VEC>(g * kGroup, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] = fmaf((h[i][e] - mean) * rstd, w[e], b[e]);
+      store8<T, VEC>(out + g * kGroup, h[i]);
+    }
+  }
+  if (has_tail)
+    out[tail] = Elem<T>::down(fmaf((last - mean) * rstd, weight.one(tail), a.bias ? bias.one(tail) : 0.0f));
+}
+
+constexpr int kLongThreads = 512;
+
+// One element of a row: residual + dropout(x), as it is written.
+template <typename T>
+__device__ __forceinline__ float hidden_at(const NormParams& a, const Stream& rng, int64_t row, int col) {
+  float f = Elem<T>::up(static_cast<const T*>(a.x)[row * a.ldx + col]);
+  if (a.d.rng) f = drop1(rng, a.d, a.d.row0 + uint32_t(row), uint32_t(col), f);
+  if (a.residual) f += Elem<T>::up(static_cast<const T*>(a.residual)[row * a.ldr + col]);
+  return rounded<T>(f);
+}
+
+// Rows too long for registers: a CTA reads one three times, element by element.
+template <typename T>
+__global__ void __launch_bounds__(kLongThreads) norm_long_rows_kernel(const NormParams a) {
+  __shared__ float part[2][32];
+  const int64_t row = blockIdx.x;
+  const Stream rng(a.d.rng);
+  float sum = 0.0f;
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
+    const float h = hidden_at<T>(a, rng, row, int(c));
+    if (a.hidden) static_cast<T*>(a.hidden)[row * a.ldh + c] = Elem<T>::down(h);
+    sum += h;
+  }
+  const float mean = row_sum(sum, part[0], 0, kLongThreads / 32) / float(a.cols);
+  sum = 0.0f;
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
+    const float d = hidden_at<T>(a, rng, row, int(c)) - mean;
+    sum = fmaf(d, d, sum);
+  }
+  const float rstd = 1.0f / sqrtf(row_sum(sum, part[1], 0, kLongThreads / 32) / float(a.cols) + a.eps);
+  if (threadIdx.x == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  const Weights<T> weight{a.weight, a.wide != 0}, bias{a.bias, a.wide != 0};
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
+    const float h = hidden_at<T>(a, rng, row, int(c));
+    static_cast<T*>(a.out)[row * a.ldo + c] =
+        Elem<T>::down(fmaf((h - mean) * rstd, weight.one(int(c)), a.bias ? bias.one(int(c)) : 0.0f));
+  }
+}
+
+template <typename T>
+int run_norm(NormParams a, cudaStream_t stream) {
+  auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+  const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.out, a.ldo, sizeof(T)) &&
+                   (!a.residual || aligned_rows(a.residual, a.ldr, sizeof(T))) &&
+                   (!a.hidden || aligned_rows(a.hidden, a.ldh, sizeof(T))) && aligned(a.weight) &&
+                   (!a.bias || aligned(a.bias));
+  const int64_t groups = std::max(1, a.cols / kGroup);
+  if (groups > 4 * 1024) {
+    norm_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
+    return launched(cudaSuccess);
+  }
+  // few rows: many threads with little each, for the latency
+  const int most = a.rows < 512 ? 1 : a.rows < 2048 ? 2 : 4;
+  const int each = groups <= most * 1024 ? most : groups <= 2048 ? 2 : 4;
+  const int64_t warps = (groups + each * 32 - 1) / (each * 32);
+  a.row_threads = int(warps * 32);
+  const int per_cta = std::max(1, 128 / a.row_threads), threads = per_cta * a.row_threads;
+  const unsigned grid = unsigned((a.rows + per_cta - 1) / per_cta);
+  auto kernel = vec ? (each == 1 ? norm_rows_kernel<T, 1, true> : each == 2 ? norm_rows_kernel<T, 2, true> : norm_rows_kernel<T, 4, true>)
+                    : (each == 1 ? norm_rows_kernel<T, 1, false> : each == 2 ? norm_rows_kernel<T, 2, false> : norm_rows_kernel<T, 4, false>);
+  kernel<<<grid, threads, 0, stream>>>(a);
+  return launched(cudaSuccess);
+}
+
+// ------------------------------------------------------------------------------------------
+// layer norm, gradients
+// ------------------------------------------------------------------------------------------
+struct GradParams {
+  const void* dout;
+  const void* hidden;
+  const void* weight;
+  const float* mean;
+  const float* rstd;
+  const void* dhidden;
+  void* dx;
+  void* dresidual;
+  float* work;  // [parts][2][cols]: each part's sums over its rows, of the weight's gradient and the bias's
+  int64_t rows, ldo, ldh, lddh, lddx, lddr;
+  int cols, row_threads, wide;
+  Dropout d;
+};
+
+// How the rows are spread: parts of the sums are CTAs times the rows that each takes at a time.
+struct GradPlan {
+  int row_threads, per_cta, ctas;
+  bool in_registers;
+  int64_t parts() const { return int64_t(ctas) * per_cta; }
+};
+
+constexpr int kGradGroups = 2;           // groups of eight columns a thread
+constexpr int kGradThreads = 512;        // at most
+constexpr int kStripRows = 64;           // rows of a part where the columns are summed by themselves
+
+GradPlan grad_plan(int64_t rows, int64_t cols) {
+  GradPlan g;
+  const int64_t groups = std::max<int64_t>(1, cols / kGroup);
+  g.in_registers = groups <= kGradGroups * kGradThreads;
+  if (!g.in_registers) {
+    g.row_threads = kLongThreads;
+    g.per_cta = 1;
+    g.ctas = int(std::min<int64_t>(256, std::max<int64_t>(1, (rows + kStripRows - 1) / kStripRows)));
+    return g;
+  }
+  g.row_threads = int((groups + kGradGroups * 32 - 1) / (kGradGroups * 32)) * 32;
+  g.per_cta = std::max(1, 256 / g.row_threads);
+  const int resident = std::max(1, 512 / (g.row_threads * g.per_cta));
+  g.ctas = int(std::min<int64_t>((rows + g.per_cta - 1) / g.per_cta, int64_t(resident) * 148));
+  g.ctas = std::max(1, g.ctas);
+  return g;
+}
+
+// Two sums over the threads of a row.  `part` is one of two buffers in turn: one barrier a row.
+__device__ __forceinline__ float2 row_sum2(float2 v, float2* part, int first_warp, int warps) {
+  v.x = warp_sum(v.x);
+  v.y = warp_sum(v.y);
+  if (warps == 1) return v;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = make_float2(0.0f, 0.0f);
+  for (int w = 0; w < warps; ++w) {
+    v.x += part[first_warp + w].x;
+    v.y += part[first_warp + w].y;
+  }
+  return v;
+}
+
+// With g = dout weight and n = (hidden - mean) rstd: dh = rstd (g - mean(g) - n mean(g n)) + dhidden.  A thread keeps its
+// columns from row to row, and with them their sums of dout n and dout.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const GradParams a) {
+  constexpr int P = kGradGroups;
+  __shared__ float2 part[2][32];
+  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
+  const int per_cta = int(blockDim.x) / a.row_threads;
+  const int full = a.cols / kGroup, tail = full * kGroup + lane;
+  const bool has_tail = lane < kGroup && tail < a.cols;
+  const int first_warp = slot * (a.row_threads / 32), warps = a.row_threads / 32;
+  const Weights<T> weight{a.weight, a.wide != 0};
+  const Stream rng(a.d.rng);
+  const float per_col = 1.0f / float(a.cols);
+  float dw[P][8] = {}, db[P][8] = {}, dw_tail = 0.0f, db_tail = 0.0f;
+  int turn = 0;
+  for (int64_t row0 = int64_t(blockIdx.x) * per_cta; row0 < a.rows; row0 += int64_t(gridDim.x) * per_cta, turn ^= 1) {
+    const int64_t row = row0 + slot;
+    const bool there = row < a.rows;
+    const T* const dout = static_cast<const T*>(a.dout) + row * a.ldo;
+    const T* const hidden = static_cast<const T*>(a.hidden) + row * a.ldh;
+    float g[P][8], n[P][8], g_tail = 0.0f, n_tail = 0.0f;
+    float2 s = make_float2(0.0f, 0.0f);
+    const float mean = there ? a.mean[row] : 0.0f, rstd = there ? a.rstd[row] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int at = i * a.row_threads + lane;
+      if (there && at < full) {
+        load8<T, VEC>(dout + at * kGroup, g[i]);
+        load8<T, VEC>(hidden + at * kGroup, n[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int at = i * a.row_threads + lane;
+      if (there && at < full) {
+        float w[8];
+        weight.template load<VEC>(at * kGroup, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          n[i][e] = (n[i][e] - mean) * rstd;
+          dw[i][e] = fmaf(g[i][e], n[i][e], dw[i][e]);
+          db[i][e] += g[i][e];
+          g[i][e] *= w[e];
+          s.x += g[i][e];
+          s.y = fmaf(g[i][e], n[i][e], s.y);
+        }
+      }
+    }
+    if (has_tail && there) {
+      g_tail = Elem<T>::up(dout[tail]);
+      n_tail = (Elem<T>::up(hidden[tail]) - mean) * rstd;
+      dw_tail = fmaf(g_tail, n_tail, dw_tail);
+      db_tail += g_tail;
+      g_tail *= weight.one(tail);
+      s.x += g_tail;
+      s.y = fmaf(g_tail, n_tail, s.y);
+    }
+    s = row_sum2(s, part[turn], first_warp, warps);
+    s.x *= per_col;
+    s.y *= per_col;
+    if (!there) continue;
+    const T* const dhidden = a.dhidden ? static_cast<const T*>(a.dhidden) + row * a.lddh : nullptr;
+    T* const dresidual = a.dresidual ? static_cast<T*>(a.dresidual) + row * a.lddr : nullptr;
+    T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
+    const uint32_t number = a.d.row0 + uint32_t(row);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int at = i * a.row_threads + lane;
+      if (at < full) {
+        float f[8] = {};
+        if (dhidden) load8<T, VEC>(dhidden + at * kGroup, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, g[i][e] - s.x - n[i][e] * s.y, f[e]);
+        if (dresidual) store8<T, VEC>(dresidual + at * kGroup, f);
+        if (a.d.rng) drop8(rng, a.d, number, uint32_t(at), f);
+        store8<T, VEC>(dx + at * kGroup, f);
+      }
+    }
+    if (has_tail) {
+      float f = fmaf(rstd, g_tail - s.x - n_tail * s.y, dhidden ? Elem<T>::up(dhidden[tail]) : 0.0f);
+      if (dresidual) dresidual[tail] = Elem<T>::down(f);
+      if (a.d.rng) f = drop1(rng, a.d, number, uint32_t(tail), f);
+      dx[tail] = Elem<T>::down(f);
+    }
+  }
+  float* const sums = a.work + (int64_t(blockIdx.x) * per_cta + slot) * 2 * a.cols;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int at = i * a.row_threads + lane;
+    if (at < full) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sums[at * kGroup + e] = dw[i][e];
+        sums[int64_t(a.cols) + at * kGroup + e] = db[i][e];
+      }
+    }
+  }
+  if (has_tail) {
+    sums[tail] = dw_tail;
+    sums[int64_t(a.cols) + tail] = db_tail;
+  }
+}
+
+// Rows too long for that: dx by a CTA that reads a row twice, ...
+template <typename T>
+__global__ void __launch_bounds__(kLongThreads) norm_grad_long_rows_kernel(const GradParams a) {
+  __shared__ float2 part[32];
+  const int64_t row = blockIdx.x;
+  const T* const dout = static_cast<const T*>(a.dout) + row * a.ldo;
+  const T* const hidden = static_cast<const T*>(a.hidden) + row * a.ldh;
+  const Weights<T> weight{a.weight, a.wide != 0};
+  const Stream rng(a.d.rng);
+  const float mean = a.mean[row], rstd = a.rstd[row];
+  float2 s = make_float2(0.0f, 0.0f);
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
+    const float g = Elem<T>::up(dout[c]) * weight.one(int(c)), n = (Elem<T>::up(hidden[c]) - mean) * rstd;
+    s.x += g;
+    s.y = fmaf(g, n, s.y);
+  }
+  s = row_sum2(s, part, 0, kLongThreads / 32);
+  s.x /= float(a.cols);
+  s.y /= float(a.cols);
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
+    const float g = Elem<T>::up(dout[c]) * weight.one(int(c)), n = (Elem<T>::up(hidden[c]) - mean) * rstd;
+    float f = a.dhidden ? Elem<T>::up(static_cast<const T*>(a.dhidden)[row * a.lddh + c]) : 0.0f;
+    f = fmaf(rstd, g - s.x - n * s.y, f);
+    if (a.dresidual) static_cast<T*>(a.dresidual)[row * a.lddr + c] = Elem<T>::down(f);
+    if (a.d.rng) f = drop1(rng, a.d, a.d.row0 + uint32_t(row), uint32_t(c), f);
+    static_cast<T*>(a.dx)[row * a.lddx + c] = Elem<T>::down(f);
+  }
+}
+
+// ... and the sums of a column over a part of the rows by a thread.
+template <typename T>
+__global__ void __launch_bounds__(128) norm_grad_columns_kernel(const GradParams a, int parts) {
+  const int64_t c = int64_t(blockIdx.x) * 128 + threadIdx.x;
+  if (c >= a.cols) return;
+  const int part = int(blockIdx.y);
+  const int64_t first = a.rows * part / parts, end = a.rows * (part + 1) / parts;
+  float dw = 0.0f, db = 0.0f;
+  for (int64_t row = first; row < end; ++row) {
+    const float dy = Elem<T>::up(static_cast<const T*>(a.dout)[row * a.ldo + c]);
+    const float n = (Elem<T>::up(static_cast<const T*>(a.hidden)[row * a.ldh + c]) - a.mean[row]) * a.rstd[row];
+    dw = fmaf(dy, n, dw);
+    db += dy;
+  }
+  a.work[int64_t(part) * 2 * a.cols + c] = dw;
+  a.work[int64_t(part) * 2 * a.cols + a.cols + c] = db;
+}
+
+constexpr int kSumRows = 16;
+
+// The parts' sums added up, in their order: 32 columns a CTA.
+__global__ void __launch_bounds__(32 * kSumRows) norm_sum_kernel(const float* work, int64_t parts, int cols, float* dweight,
+                                                                 float* dbias) {
+  __shared__ float sums[kSumRows][33];
+  const int lane = int(threadIdx.x) % 32, y = int(threadIdx.x) / 32;
+  const int64_t c = int64_t(blockIdx.x) * 32 + lane;
+  const float* const in = work + int64_t(blockIdx.y) * cols + c;
+  float v = 0.0f;
+  if (c < cols)
+    for (int64_t i = y; i < parts; i += kSumRows) v += in[i * 2 * cols];
+  sums[y][lane] = v;
+  __syncthreads();
+  if (y == 0 && c < cols) {
+    for (int i = 1; i < kSumRows; ++i) v += sums[i][lane];
+    (blockIdx.y == 0 ? dweight : dbias)[c] = v;
+  }
+}
+
+template <typename T>
+int run_grad(GradParams a, float* dweight, float* dbias, cudaStream_t stream) {
+  const GradPlan plan = grad_plan(a.rows, a.cols);
+  a.row_threads = plan.row_threads;
+  auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+  if (plan.in_registers) {
+    const bool vec = aligned_rows(a.dout, a.ldo, sizeof(T)) && aligned_rows(a.hidden, a.ldh, sizeof(T)) &&
+                     aligned_rows(a.dx, a.lddx, sizeof(T)) && (!a.dhidden || aligned_rows(a.dhidden, a.lddh, sizeof(T))) &&
+                     (!a.dresidual || aligned_rows(a.dresidual, a.lddr, sizeof(T))) && aligned(a.weight);
+    auto kernel = vec ? norm_grad_kernel<T, true> : norm_grad_kernel<T, false>;
+    kernel<<<unsigned(plan.ctas), plan.row_threads * plan.per_cta, 0, stream>>>(a);
+  } else {
+    if (a.rows > 0) norm_grad_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
+    const dim3 grid(unsigned((int64_t(a.cols) + 127) / 128), unsigned(plan.ctas));
+    norm_grad_columns_kernel<T><<<grid, 128, 0, stream>>>(a, plan.ctas);
+  }
+  const int rc = launched(cudaSuccess);
+  if (rc != ENTWINE_OK) return rc;
+  const dim3 grid(unsigned((int64_t(a.cols) + 31) / 32), dbias ? 2 : 1);
+  norm_sum_kernel<<<grid, 32 * kSumRows, 0, stream>>>(a.work, plan.parts(), a.cols, dweight, dbias);
+  return launched(cudaSuccess);
+}
+
+bool floating(int dtype) { return dtype == ENTWINE_BF16 || dtype == ENTWINE_FP16 || dtype == ENTWINE_FP32; }
+int64_t bytes_of(int dtype) { return dtype == ENTWINE_FP32 ? 4 : 2; }
+
+// p, the generator's state and the first row's number; false where they cannot be.
+bool make_dropout(double p, const int64_t* rng, int64_t row0, int64_t rows, Dropout* d) {
+  if (!(p >= 0.0 && p < 1.0) || row0 < 0 || row0 > (int64_t(1) << 32) - rows) return false;
+  const double t = std::nearbyint(p * 65536.0);
+  if (t > 65535.0 || (p > 0.0 && bad_pointer(rng, 8))) return false;
+  d->rng = t > 0.0 ? rng : nullptr;
+  d->t = uint32_t(t);
+  d->scale = float(65536.0 / (65536.0 - t));
+  d->row0 = uint32_t(row0);
+  return true;
+}
+
+}  // namespace
+}  // namespace entwine
+
+using namespace entwine;
+
+extern "C" {
+
+int entwine_dropout(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* residual, int64_t ldr,
+                    double p, const int64_t* rng, int64_t row0, void* out, int64_t ldo, void* stream) {
+  if (!floating(dtype) || rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols || ldx < cols || ldo < cols ||
+      (residual && ldr < cols))
+    return ENTWINE_ERR_INVALID;
+  DropParams a;
+  std::memset(&a, 0, sizeof(a));
+  if (!make_dropout(p, rng, row0, rows, &a.d)) return ENTWINE_ERR_INVALID;
+  if (rows == 0) return ENTWINE_OK;
+  const int64_t elem = bytes_of(dtype);
+  if (bad_pointer(x, elem) || bad_pointer(out, elem) || (residual && bad_pointer(residual, elem))) return ENTWINE_ERR_INVALID;
+  a.x = x;
+  a.residual = residual;
+  a.out = out;
+  a.rows = rows;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.ldo = ldo;
+  a.cols = int(cols);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  switch (dtype) {
+    case ENTWINE_BF16: return run_dropout<__nv_bfloat16>(a, s);
+    case ENTWINE_FP16: return run_dropout<__half>(a, s);
+    default: return run_dropout<float>(a, s);
+  }
+}
+
+int entwine_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* residual,
+                       int64_t ldr, double p, const int64_t* rng, int64_t row0, const void* weight, const void* bias,
+                       int w_dtype, float eps, void* hidden, int64_t ldh, void* out, int64_t ldo, float* mean, float* rstd,
+                       void* stream) {
+  if (!floating(dtype) || (w_dtype != dtype && w_dtype != ENTWINE_FP32) || rows < 0 || rows > kMaxRows || cols < 1 ||
+      cols > kMaxCols || ldx < cols || ldo < cols || (residual && ldr < cols) || (hidden && ldh < cols) || !(eps >= 0.0f))
+    return ENTWINE_ERR_INVALID;
+  NormParams a;
+  std::memset(&a, 0, sizeof(a));
+  if (!make_dropout(p, rng, row0, rows, &a.d)) return ENTWINE_ERR_INVALID;
+  if (rows == 0) return ENTWINE_OK;
+  const int64_t elem = bytes_of(dtype), w_elem = bytes_of(w_dtype);
+  if (bad_pointer(x, elem) || bad_pointer(out, elem) || (residual && bad_pointer(residual, elem)) ||
+      (hidden && bad_pointer(hidden, elem)) || bad_pointer(weight, w_elem) || (bias && bad_pointer(bias, w_elem)) ||
+      (mean && bad_pointer(mean, 4)) || (rstd && bad_pointer(rstd, 4)))
+    return ENTWINE_ERR_INVALID;
+  a.x = x;
+  a.residual = residual;
+  a.weight = weight;
+  a.bias = bias;
+  a.hidden = hidden;
+  a.out = out;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.rows = rows;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.ldh = ldh;
+  a.ldo = ldo;
+  a.cols = int(cols);
+  a.wide = w_dtype == ENTWINE_FP32;
+  a.eps = eps;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  switch (dtype) {
+    case ENTWINE_BF16: return run_norm<__nv_bfloat16>(a, s);
+    case ENTWINE_FP16: return run_norm<__half>(a, s);
+    default: return run_norm<float>(a, s);
+  }
+}
+
+int entwine_layer_norm_bwd_work(int64_t rows, int64_t cols, int64_t* floats) {
+  if (!floats || rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols) return ENTWINE_ERR_INVALID;
+  *floats = grad_plan(rows, cols).parts() * 2 * cols;
+  return ENTWINE_OK;
+}
+
+int entwine_layer_norm_bwd(const void* dout, int dtype, int64_t rows, int64_t cols, int64_t ldo, const void* hidden,
+                           int64_t ldh, const void* weight, int w_dtype, const float* mean, const float* rstd,
+                           const void* dhidden, int64_t lddh, double p, const int64_t* rng, int64_t row0, void* dx,
+                           int64_t lddx, void* dresidual, int64_t lddr, float* dweight, float* dbias, float* work,
+                           int64_t work_floats, void* stream) {
+  if (!floating(dtype) || (w_dtype != dtype && w_dtype != ENTWINE_FP32) || rows < 0 || rows > kMaxRows || cols < 1 ||
+      cols > kMaxCols || ldo < cols || ldh < cols || lddx < cols || (dhidden && lddh < cols) || (dresidual && lddr < cols))
+    return ENTWINE_ERR_INVALID;
+  GradParams a;
+  std::memset(&a, 0, sizeof(a));
+  if (!make_dropout(p, rng, row0, rows, &a.d)) return ENTWINE_ERR_INVALID;
+  const int64_t elem = bytes_of(dtype), w_elem = bytes_of(w_dtype);
+  if (bad_pointer(dweight, 4) || (dbias && bad_pointer(dbias, 4)) || bad_pointer(work, 4) ||
+      work_floats < grad_plan(rows, cols).parts() * 2 * cols)
+    return ENTWINE_ERR_INVALID;
+  // (without rows the sums are still written)
+  if (rows > 0 && (bad_pointer(dout, elem) || bad_pointer(hidden, elem) || bad_pointer(weight, w_elem) ||
+                   bad_pointer(mean, 4) || bad_pointer(rstd, 4) || (dhidden && bad_pointer(dhidden, elem)) ||
+                   bad_pointer(dx, elem) || (dresidual && bad_pointer(dresidual, elem))))
+    return ENTWINE_ERR_INVALID;
+  a.dout = dout;
+  a.hidden = hidden;
+  a.weight = weight;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.dhidden = dhidden;
+  a.dx = dx;
+  a.dresidual = dresidual;
+  a.work = work;
+  a.rows = rows;
+  a.ldo = ldo;
+  a.ldh = ldh;
+  a.lddh = lddh;
+  a.lddx = lddx;
+  a.lddr = lddr;
+  a.cols = int(cols);
+  a.wide = w_dtype == ENTWINE_FP32;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  switch (dtype) {
+    case ENTWINE_BF16: return run_grad<__nv_bfloat16>(a, dweight, dbias, s);
+    case ENTWINE_FP16: return run_grad<__half>(a, dweight, dbias, s);
+    default: return run_grad<float>(a, dweight, dbias, s);
+  }
+}
+
+}  // extern "C"

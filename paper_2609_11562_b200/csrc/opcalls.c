@@ -10,7 +10,8 @@
 #include <stdint.h>
 #include <string.h>
 
-enum { BF16, FP16, FP32, I8, I32, I64, DTYPES };  /* the first four as in entwine_ops.h */
+enum { BF16, FP16, FP32, I8, I32, I64, U8, DTYPES };  /* the first four as in entwine_ops.h */
+enum { LEAST_DTYPES = U8 };  /* bind() may be given no uint8: nothing is of that type then */
 enum { FLOATING = 1 << BF16 | 1 << FP16 | 1 << FP32, ANY = FLOATING | 1 << I8, IDS = 1 << I32 | 1 << I64 };
 
 static PyObject *dtypes[DTYPES], *error_class, *current_device, *current_stream;
@@ -30,6 +31,21 @@ typedef int (*combine_fn)(const void*, int, int64_t, int64_t, int64_t, const flo
 typedef int (*combine_bwd_fn)(const void*, int, int64_t, int64_t, int64_t, const void*, int64_t, int64_t, const float*,
                               const int32_t*, int64_t, void*, int64_t, float*, void*);
 
+typedef int (*quant4_fn)(const void*, int, int64_t, int64_t, int64_t, void*, int64_t, void*, int64_t, void*);
+typedef int (*dequant4_fn)(const void*, int64_t, const void*, int64_t, int64_t, int64_t, void*, int, int64_t, void*);
+typedef int (*gemm4_fn)(const void*, int64_t, const void*, int64_t, const void*, int64_t, const void*, int64_t, const float*,
+                        void*, int, int64_t, int64_t, int64_t, int64_t, void*);
+typedef int (*grouped4_fn)(const void*, int64_t, const void*, int64_t, const void*, int64_t, int64_t, const void*, int64_t,
+                           int64_t, const float*, const int32_t*, void*, int, int64_t, int64_t, int64_t, int64_t, int64_t,
+                           void*);
+typedef int (*dropout_fn)(const void*, int, int64_t, int64_t, int64_t, const void*, int64_t, double, const int64_t*, int64_t,
+                          void*, int64_t, void*);
+typedef int (*norm_fn)(const void*, int, int64_t, int64_t, int64_t, const void*, int64_t, double, const int64_t*, int64_t,
+                       const void*, const void*, int, float, void*, int64_t, void*, int64_t, float*, float*, void*);
+typedef int (*norm_bwd_fn)(const void*, int, int64_t, int64_t, int64_t, const void*, int64_t, const void*, int, const float*,
+                           const float*, const void*, int64_t, double, const int64_t*, int64_t, void*, int64_t, void*,
+                           int64_t, float*, float*, float*, int64_t, void*);
+
 static quant_fn quant;
 static gemm_fn gemm;
 static grouped_fn grouped;
@@ -37,6 +53,13 @@ static dispatch_fn dispatch;
 static dispatch_bwd_fn dispatch_bwd;
 static combine_fn combine;
 static combine_bwd_fn combine_bwd;
+static quant4_fn quant4;
+static dequant4_fn dequant4;
+static gemm4_fn gemm4;
+static grouped4_fn grouped4;
+static dropout_fn dropout;
+static norm_fn norm;
+static norm_bwd_fn norm_bwd;
 
 /* What bind() has to be given is fetched at the first call, by a function that calls it: until then the package needs no
  * torch. */
@@ -113,7 +136,7 @@ static int tensor(PyObject* t, const char* name, unsigned allowed, long dev, int
   o = PyObject_GetAttr(t, s_dtype);
   if (!o) return refuse("%s must be a tensor", name);
   Py_DECREF(o); /* (the bound dtype objects live on) */
-  for (i = 0; i < DTYPES && o != dtypes[i]; ++i) {}
+  for (i = 0; i < DTYPES && o != dtypes[i]; ++i) {} /* (a slot that bind() was not given is NULL) */
   if (i == DTYPES || !(allowed >> i & 1)) return refuse("%s is of a type that this argument cannot have", name);
   *dtype = i;
   o = PyObject_CallMethodNoArgs(t, s_data_ptr);
@@ -341,6 +364,177 @@ static PyObject* py_moe_combine_bwd(PyObject* self, PyObject* const* a, Py_ssize
                                               dy.at, dy.ld, dw, stream));
 }
 
+/* Codes of rows of `cols` elements, or of as many as two a byte make, and their scales. */
+static int codes(PyObject* q, const char* q_name, PyObject* scale, const char* scale_name, long dev, int64_t rows,
+                 int64_t cols, Matrix* m, Matrix* s) {
+  if (rows < 0) {
+    if (!matrix(q, q_name, 1 << U8, dev, m)) return 0;
+  } else if (!result(q, q_name, 1 << U8, dev, rows, (cols + 1) / 2, m)) {
+    return 0;
+  }
+  return result(scale, scale_name, 1 << U8, dev, m->rows, (rows < 0 ? 2 * m->cols + 31 : cols + 31) / 32, s);
+}
+
+/* (x, q, scale, stream) */
+static PyObject* py_quant_mxf4(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Matrix x, q, s;
+  void* stream;
+  long dev;
+  if (!bound() || !count_is(n, 4) || (dev = first_device(a[0], "x")) < 0 || !matrix(a[0], "x", FLOATING, dev, &x) ||
+      !codes(a[1], "q", a[2], "scale", dev, x.rows, x.cols, &q, &s) || !stream_of(a[3], dev, &stream))
+    return NULL;
+  CALL("entwine_quant_mxf4", quant4(x.at, x.dtype, x.rows, x.cols, x.ld, q.at, q.ld, s.at, s.ld, stream));
+}
+
+/* (q, scale, x, stream) */
+static PyObject* py_dequant_mxf4(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Matrix x, q, s;
+  void* stream;
+  long dev;
+  if (!bound() || !count_is(n, 4) || (dev = first_device(a[0], "q")) < 0 || !matrix(a[2], "x", FLOATING, dev, &x) ||
+      !codes(a[0], "q", a[1], "scale", dev, x.rows, x.cols, &q, &s) || !stream_of(a[3], dev, &stream))
+    return NULL;
+  CALL("entwine_dequant_mxf4", dequant4(q.at, q.ld, s.at, s.ld, x.rows, x.cols, x.at, x.dtype, x.ld, stream));
+}
+
+/* (a, scale_a, b, scale_b, out, bias, stream) */
+static PyObject* py_gemm_mxf4(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Matrix x, sx, w, sw, c;
+  void *bias, *stream;
+  long dev;
+  if (!bound() || !count_is(n, 7) || (dev = first_device(a[0], "a")) < 0 ||
+      !codes(a[0], "a", a[1], "scale_a", dev, -1, 0, &x, &sx) || !codes(a[2], "b", a[3], "scale_b", dev, -1, 0, &w, &sw))
+    return NULL;
+  if (x.cols != w.cols) return refuse("a and b must have rows of one length"), NULL;
+  if (!result(a[4], "out", FLOATING, dev, x.rows, w.rows, &c) || !optional(a[5], "bias", dev, 1, w.rows, 0, &bias) ||
+      !stream_of(a[6], dev, &stream))
+    return NULL;
+  CALL("entwine_gemm_mxf4", gemm4(x.at, x.ld, sx.at, sx.ld, w.at, w.ld, sw.at, sw.ld, bias, c.at, c.dtype, c.ld, x.rows,
+                                  w.rows, 2 * x.cols, stream));
+}
+
+/* Matrices [G, N, cols] whose rows are contiguous and do not overlap. */
+static int stacked(PyObject* t, const char* name, long dev, int64_t cols, void** at, int64_t* s, int64_t* d) {
+  int dtype;
+  if (!tensor(t, name, 1 << U8, dev, &dtype, at)) return 0;
+  if (!numbers(PyObject_GetAttr(t, s_shape), 3, s) || !numbers(PyObject_CallMethodNoArgs(t, s_stride), 3, d) || s[0] < 1 ||
+      s[1] < 1 || s[2] != cols)
+    return refuse("%s must be [G, N, %lld]", name, (long long)cols);
+  if ((d[2] != 1 && s[2] > 1) || (d[1] < s[2] && s[1] > 1) || (d[0] < (s[1] - 1) * d[1] + s[2] && s[0] > 1))
+    return refuse("%s must be matrices of contiguous rows that do not overlap", name);
+  if (d[1] < s[2]) d[1] = s[2];
+  return 1;
+}
+
+/* (a, scale_a, b, scale_b, offsets, out, bias, stream) */
+static PyObject* py_gemm_mxf4_grouped(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Matrix x, sx, c;
+  void *w, *sw, *bias, *offsets, *stream;
+  int64_t s[3], d[3], ss[3], sd[3];
+  long dev;
+  if (!bound() || !count_is(n, 8) || (dev = first_device(a[0], "a")) < 0 ||
+      !codes(a[0], "a", a[1], "scale_a", dev, -1, 0, &x, &sx) || !stacked(a[2], "b", dev, x.cols, &w, s, d) ||
+      !stacked(a[3], "scale_b", dev, sx.cols, &sw, ss, sd))
+    return NULL;
+  if (ss[0] != s[0] || ss[1] != s[1]) return refuse("b and scale_b must have as many experts and rows"), NULL;
+  if (!result(a[5], "out", FLOATING, dev, x.rows, s[1], &c) ||
+      !dense(a[4], "offsets", 1 << I32, dev, 1, s[0] + 1, 0, &offsets, NULL) ||
+      !optional(a[6], "bias", dev, 2, s[0], s[1], &bias) || !stream_of(a[7], dev, &stream))
+    return NULL;
+  CALL("entwine_gemm_mxf4_grouped", grouped4(x.at, x.ld, sx.at, sx.ld, w, d[1], d[0], sw, sd[1], sd[0], bias, offsets, c.at,
+                                             c.dtype, c.ld, x.rows, s[1], 2 * x.cols, s[0], stream));
+}
+
+/* p, the generator's state and the first row's number. */
+typedef struct {
+  double p;
+  void* rng;
+  long long row0;
+} Drop;
+static int drop_of(PyObject* p, PyObject* rng, PyObject* row0, long dev, Drop* d) {
+  d->p = PyFloat_AsDouble(p);
+  if (d->p == -1.0 && PyErr_Occurred()) return 0;
+  d->row0 = PyLong_AsLongLong(row0);
+  if (d->row0 == -1 && PyErr_Occurred()) {
+    if (!PyErr_ExceptionMatches(PyExc_OverflowError)) return 0;
+    return refuse("row0 is out of range");
+  }
+  d->rng = NULL;
+  if (!(d->p >= 0.0 && d->p < 1.0)) return refuse("p must be at least 0 and below 1");
+  if (rng == Py_None) return d->p == 0.0 ? 1 : refuse("rng must be a tensor where p is not 0");
+  return dense(rng, "rng", 1 << I64, dev, 1, 2, 0, &d->rng, NULL);
+}
+/* A matrix of known size, or None. */
+static int optional_matrix(PyObject* t, const char* name, unsigned allowed, long dev, int64_t rows, int64_t cols, Matrix* m) {
+  memset(m, 0, sizeof(*m));
+  return t == Py_None || result(t, name, allowed, dev, rows, cols, m);
+}
+
+/* (x, out, p, rng, row0, residual, stream) */
+static PyObject* py_dropout(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Matrix x, o, r;
+  Drop d;
+  void* stream;
+  long dev;
+  if (!bound() || !count_is(n, 7) || (dev = first_device(a[0], "x")) < 0 || !matrix(a[0], "x", FLOATING, dev, &x) ||
+      !result(a[1], "out", 1u << x.dtype, dev, x.rows, x.cols, &o) ||
+      !optional_matrix(a[5], "residual", 1u << x.dtype, dev, x.rows, x.cols, &r) || !drop_of(a[2], a[3], a[4], dev, &d) ||
+      !stream_of(a[6], dev, &stream))
+    return NULL;
+  CALL("entwine_dropout", dropout(x.at, x.dtype, x.rows, x.cols, x.ld, r.at, r.ld, d.p, d.rng, d.row0, o.at, o.ld, stream));
+}
+
+/* (x, weight, bias, out, eps, mean, rstd, residual, hidden, p, rng, row0, stream) */
+static PyObject* py_layer_norm(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Matrix x, o, r, h;
+  Drop d;
+  void *w, *b = NULL, *mean, *rstd, *stream;
+  int w_type;
+  double eps;
+  long dev;
+  if (!bound() || !count_is(n, 13) || (dev = first_device(a[0], "x")) < 0 || !matrix(a[0], "x", FLOATING, dev, &x) ||
+      !dense(a[1], "weight", 1u << x.dtype | 1 << FP32, dev, 1, x.cols, 0, &w, &w_type) ||
+      (a[2] != Py_None && !dense(a[2], "bias", 1u << w_type, dev, 1, x.cols, 0, &b, NULL)) ||
+      !result(a[3], "out", 1u << x.dtype, dev, x.rows, x.cols, &o))
+    return NULL;
+  eps = PyFloat_AsDouble(a[4]);
+  if (eps == -1.0 && PyErr_Occurred()) return NULL;
+  if (!optional(a[5], "mean", dev, 1, x.rows, 0, &mean) || !optional(a[6], "rstd", dev, 1, x.rows, 0, &rstd) ||
+      !optional_matrix(a[7], "residual", 1u << x.dtype, dev, x.rows, x.cols, &r) ||
+      !optional_matrix(a[8], "hidden", 1u << x.dtype, dev, x.rows, x.cols, &h) ||
+      !drop_of(a[9], a[10], a[11], dev, &d) || !stream_of(a[12], dev, &stream))
+    return NULL;
+  CALL("entwine_layer_norm", norm(x.at, x.dtype, x.rows, x.cols, x.ld, r.at, r.ld, d.p, d.rng, d.row0, w, b, w_type,
+                                  (float)eps, h.at, h.ld, o.at, o.ld, mean, rstd, stream));
+}
+
+/* (dout, hidden, weight, mean, rstd, dx, dweight, dbias, work, dhidden, dresidual, p, rng, row0, stream) */
+static PyObject* py_layer_norm_bwd(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Matrix g, h, dx, dh, dr;
+  Drop d;
+  void *w, *mean, *rstd, *dw, *db, *work, *stream;
+  int64_t floats[1];
+  int w_type;
+  long dev;
+  if (!bound() || !count_is(n, 15) || (dev = first_device(a[0], "dout")) < 0 || !matrix(a[0], "dout", FLOATING, dev, &g) ||
+      !result(a[1], "hidden", 1u << g.dtype, dev, g.rows, g.cols, &h) ||
+      !dense(a[2], "weight", 1u << g.dtype | 1 << FP32, dev, 1, g.cols, 0, &w, &w_type) ||
+      !dense(a[3], "mean", 1 << FP32, dev, 1, g.rows, 0, &mean, NULL) ||
+      !dense(a[4], "rstd", 1 << FP32, dev, 1, g.rows, 0, &rstd, NULL) ||
+      !result(a[5], "dx", 1u << g.dtype, dev, g.rows, g.cols, &dx) ||
+      !dense(a[6], "dweight", 1 << FP32, dev, 1, g.cols, 0, &dw, NULL) || !optional(a[7], "dbias", dev, 1, g.cols, 0, &db))
+    return NULL;
+  if (!numbers(PyObject_GetAttr(a[8], s_shape), 1, floats)) return refuse("work must have one dimension"), NULL;
+  if (!dense(a[8], "work", 1 << FP32, dev, 1, floats[0], 0, &work, NULL) ||
+      !optional_matrix(a[9], "dhidden", 1u << g.dtype, dev, g.rows, g.cols, &dh) ||
+      !optional_matrix(a[10], "dresidual", 1u << g.dtype, dev, g.rows, g.cols, &dr) ||
+      !drop_of(a[11], a[12], a[13], dev, &d) || !stream_of(a[14], dev, &stream))
+    return NULL;
+  CALL("entwine_layer_norm_bwd",
+       norm_bwd(g.at, g.dtype, g.rows, g.cols, g.ld, h.at, h.ld, w, w_type, mean, rstd, dh.at, dh.ld, d.p, d.rng, d.row0, dx.at,
+                dx.ld, dr.at, dr.ld, dw, db, work, floats[0], stream));
+}
+
 static int entry(PyObject* addresses, const char* name, void* out) {
   PyObject* o = PyDict_GetItemString(addresses, name); /* borrowed */
   void* p;
@@ -359,13 +553,19 @@ static PyObject* py_bind(PyObject* self, PyObject* args) {
   int i;
   if (!PyArg_ParseTuple(args, "O!O!OOO", &PyDict_Type, &addresses, &PyTuple_Type, &types, &error, &device, &stream))
     return NULL;
-  if (PyTuple_GET_SIZE(types) != DTYPES) return PyErr_Format(PyExc_ValueError, "%d dtypes", DTYPES);
+  if (PyTuple_GET_SIZE(types) < LEAST_DTYPES || PyTuple_GET_SIZE(types) > DTYPES)
+    return PyErr_Format(PyExc_ValueError, "%d to %d dtypes", LEAST_DTYPES, DTYPES);
   if (!entry(addresses, "entwine_quant_i8", &quant) || !entry(addresses, "entwine_gemm_i8", &gemm) ||
       !entry(addresses, "entwine_gemm_i8_grouped", &grouped) || !entry(addresses, "entwine_moe_dispatch", &dispatch) ||
       !entry(addresses, "entwine_moe_dispatch_bwd", &dispatch_bwd) ||
-      !entry(addresses, "entwine_moe_combine", &combine) || !entry(addresses, "entwine_moe_combine_bwd", &combine_bwd))
+      !entry(addresses, "entwine_moe_combine", &combine) || !entry(addresses, "entwine_moe_combine_bwd", &combine_bwd) ||
+      !entry(addresses, "entwine_quant_mxf4", &quant4) || !entry(addresses, "entwine_dequant_mxf4", &dequant4) ||
+      !entry(addresses, "entwine_gemm_mxf4", &gemm4) || !entry(addresses, "entwine_gemm_mxf4_grouped", &grouped4) ||
+      !entry(addresses, "entwine_dropout", &dropout) || !entry(addresses, "entwine_layer_norm", &norm) ||
+      !entry(addresses, "entwine_layer_norm_bwd", &norm_bwd))
     return NULL;
-  for (i = 0; i < DTYPES; ++i) Py_XSETREF(dtypes[i], Py_NewRef(PyTuple_GET_ITEM(types, i)));
+  for (i = 0; i < DTYPES; ++i)
+    Py_XSETREF(dtypes[i], i < PyTuple_GET_SIZE(types) ? Py_NewRef(PyTuple_GET_ITEM(types, i)) : NULL);
   Py_XSETREF(error_class, Py_NewRef(error));
   Py_XSETREF(current_device, Py_NewRef(device));
   Py_XSETREF(current_stream, Py_NewRef(stream));
@@ -385,6 +585,16 @@ static PyMethodDef methods[] = {
     {"moe_combine", (PyCFunction)(void (*)(void))py_moe_combine, METH_FASTCALL, "(y, weights, row_of, out, stream)"},
     {"moe_combine_bwd", (PyCFunction)(void (*)(void))py_moe_combine_bwd, METH_FASTCALL,
      "(dout, y, weights, row_of, dy, dw, stream)"},
+    {"quant_mxf4", (PyCFunction)(void (*)(void))py_quant_mxf4, METH_FASTCALL, "(x, q, scale, stream)"},
+    {"dequant_mxf4", (PyCFunction)(void (*)(void))py_dequant_mxf4, METH_FASTCALL, "(q, scale, x, stream)"},
+    {"gemm_mxf4", (PyCFunction)(void (*)(void))py_gemm_mxf4, METH_FASTCALL, "(a, scale_a, b, scale_b, out, bias, stream)"},
+    {"gemm_mxf4_grouped", (PyCFunction)(void (*)(void))py_gemm_mxf4_grouped, METH_FASTCALL,
+     "(a, scale_a, b, scale_b, offsets, out, bias, stream)"},
+    {"dropout", (PyCFunction)(void (*)(void))py_dropout, METH_FASTCALL, "(x, out, p, rng, row0, residual, stream)"},
+    {"layer_norm", (PyCFunction)(void (*)(void))py_layer_norm, METH_FASTCALL,
+     "(x, weight, bias, out, eps, mean, rstd, residual, hidden, p, rng, row0, stream)"},
+    {"layer_norm_bwd", (PyCFunction)(void (*)(void))py_layer_norm_bwd, METH_FASTCALL,
+     "(dout, hidden, weight, mean, rstd, dx, dweight, dbias, work, dhidden, dresidual, p, rng, row0, stream)"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_opcalls",

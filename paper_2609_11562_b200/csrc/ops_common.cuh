@@ -211,6 +211,15 @@ inline int launched(cudaError_t e) {
   return ENTWINE_ERR_CUDA;
 }
 
+// What the products share beyond their kernels: entwine_ops_set_option's values for the next launch, and the number of
+// bounded waits of the 4-bit products that ran out on the current device.
+struct WaitSettings {
+  unsigned long long budget_ns;
+  int withhold;
+};
+WaitSettings wait_settings();
+cudaError_t mxf4_failed_waits(unsigned long long* n, cudaStream_t stream);
+
 // SMs of the current device (148 where that cannot be told).
 inline int sm_count() {
   static std::atomic<int> known[64];

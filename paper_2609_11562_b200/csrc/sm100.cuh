@@ -267,6 +267,41 @@ __device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t a_desc, u
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// 4-bit floats (e2m1, two a byte) with a power-of-two scale per 32 elements of K, fp32 accumulator, 64 elements of K per
+// instruction.  The scales lie in TMEM: row r of an operand in lane r % 32 (of every quarter), column r / 32, a column's
+// four bytes for four blocks of K of which the instruction descriptor names the two that it uses.
+__device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                          uint32_t a_scales, uint32_t b_scales, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate)
+      : "memory");
+}
+// 32 rows of 16 bytes, 512 contiguous bytes of shared memory, to four columns of every lane quarter (ordered before the
+// products that the same thread issues after it).
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// Descriptor of such rows: no swizzle, groups of eight rows 128 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t saddr) {
+  return uint64_t((saddr & 0x3FFFF) >> 4) | uint64_t(128 >> 4) << 32 | uint64_t(1) << 46;
+}
+// Instruction descriptor: e2m1 operands, both K-major, power-of-two scales; `half` 0 or 1: which two of a column's bytes.
+__device__ __forceinline__ constexpr uint32_t instr_desc_mxf4(int n, int m, int half) {
+  return (1u << 7) | (1u << 10) | (1u << 23) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24) |
+         (uint32_t(2 * half) << 4) | (uint32_t(2 * half) << 29);
+}
+// Four bytes to shared memory, the last 4 - bytes of them zeros.
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {  // <= N groups still under way
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 // 32 lanes x 16 consecutive 32-bit columns: thread i of the warp receives lane (base + i).
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
   asm volatile(

@@ -69,7 +69,7 @@ SYMBOLS = ("entwine_plan", "entwine_set_option", "entwine_gemm_rs", "entwine_gem
            "entwine_gemm_rs_host_begin", "entwine_gemm_rs_host_wait", "entwine_last_sm_clock",
            "entwine_plan_workspace_bytes", "entwine_plan_set_workspace")
 
-_vp, _i64, _int = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
+_vp, _i64, _int, _f64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_double
 _lib.entwine_plan.argtypes = [ctypes.POINTER(_vp), _i64, _i64, _i64, _int, _int, _int]
 _lib.entwine_set_option.argtypes = [_vp, _int, _i64]
 _lib.entwine_gemm_rs_norm.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]
@@ -103,6 +103,17 @@ _OP_ARGS = {
     "entwine_moe_dispatch_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp],
     "entwine_moe_combine": [_vp, _int, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp],
     "entwine_moe_combine_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp],
+    "entwine_quant_mxf4": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp],
+    "entwine_dequant_mxf4": [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _int, _i64, _vp],
+    "entwine_gemm_mxf4": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _int, _i64, _i64, _i64, _i64, _vp],
+    "entwine_gemm_mxf4_grouped": [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _int, _i64, _i64, _i64,
+                                  _i64, _i64, _vp],
+    "entwine_dropout": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _f64, _vp, _i64, _vp, _i64, _vp],
+    "entwine_layer_norm": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _f64, _vp, _i64, _vp, _vp, _int, ctypes.c_float, _vp, _i64,
+                           _vp, _i64, _vp, _vp, _vp],
+    "entwine_layer_norm_bwd_work": [_i64, _i64, ctypes.POINTER(_i64)],
+    "entwine_layer_norm_bwd": [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _int, _vp, _vp, _vp, _i64, _f64, _vp, _i64, _vp, _i64,
+                               _vp, _i64, _vp, _vp, _vp, _i64, _vp],
 }
 OP_SYMBOLS = tuple(_OP_ARGS)
 for _name, _args in _OP_ARGS.items():
@@ -303,7 +314,7 @@ def _bind_ops():
     call: with raw addresses and stream handles the rest of the module needs no torch."""
     import torch
     addresses = {name: ctypes.cast(getattr(_lib, name), _vp).value for name in OP_SYMBOLS}
-    dtypes = (torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.int32, torch.int64)
+    dtypes = (torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.int32, torch.int64, torch.uint8)
     # the current stream's handle where torch gives it alone: building a Stream object takes 3 us, as long as a short kernel
     stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
     _opcalls.bind(addresses, dtypes, EntwineError, torch.cuda.current_device, stream)
@@ -373,3 +384,62 @@ def moe_combine_bwd(dout, y, weights, row_of, dy, dw, stream=None):
     """Gradients of moe_combine: dy[row_of[t, j]] = weights[t, j] dout[t], dw[t, j] = <dout[t], y[row_of[t, j]]>
     (fp32; 0 where dropped).  Rows of dy that no assignment names are left as they were."""
     _opcalls.moe_combine_bwd(dout, y, weights, row_of, dy, dw, stream)
+
+
+def quant_mxf4(x, q, scale, stream=None):
+    """Rows to 4-bit floats (e2m1) with a power-of-two scale per 32 elements (e8m0), the OCP MXFP4 format.  x [M, K] bf16,
+    fp16 or fp32; q [M, ceil(K/2)] uint8, element 2i in the lower half of byte i; scale [M, ceil(K/32)] uint8."""
+    _opcalls.quant_mxf4(x, q, scale, stream)
+
+
+def dequant_mxf4(q, scale, x, stream=None):
+    """Back to values, rounded once to x's type: x = code 2^(scale - 127), NaN where scale is 255."""
+    _opcalls.dequant_mxf4(q, scale, x, stream)
+
+
+def gemm_mxf4(a, scale_a, b, scale_b, out, bias=None, stream=None):
+    """out[m, n] = sum_k a[m, k] b[n, k] (+ bias[n]) of the values that codes and scales stand for.  a [M, ceil(K/2)],
+    b [N, ceil(K/2)] uint8 with rows on 16-byte boundaries; scale_a [M, ceil(K/32)], scale_b [N, ceil(K/32)] uint8 with rows on
+    4-byte boundaries; bias [N] fp32; out [M, N] bf16, fp16 or fp32."""
+    _opcalls.gemm_mxf4(a, scale_a, b, scale_b, out, bias, stream)
+
+
+def gemm_mxf4_grouped(a, scale_a, b, scale_b, offsets, out, bias=None, stream=None):
+    """Rows [offsets[g], offsets[g+1]) of a times expert g's matrix: b [G, N, ceil(K/2)], scale_b [G, N, ceil(K/32)] uint8, bias
+    [G, N] fp32, offsets [G+1] int32 on the device; the rest as gemm_mxf4.  Rows of no expert are left as they were."""
+    _opcalls.gemm_mxf4_grouped(a, scale_a, b, scale_b, offsets, out, bias, stream)
+
+
+def dropout(x, out, p, rng, row0=0, residual=None, stream=None):
+    """out = residual + dropout(x): kept with probability 1 - p (to the nearest 2^-16) by a number computed from rng, the
+    row's number row0 + r and the column; the mask is not stored.  rng: int64 [2] on the device, seed and offset (None is
+    allowed with p = 0); x, out, residual [M, K] of one type, bf16, fp16 or fp32."""
+    _opcalls.dropout(x, out, p, rng, row0, residual, stream)
+
+
+def dropout_bwd(dout, dx, p, rng, row0=0, stream=None):
+    """Gradient of dropout: the same mask and factor on dout."""
+    _opcalls.dropout(dout, dx, p, rng, row0, None, stream)
+
+
+def layer_norm(x, weight, bias, out, eps=1e-5, mean=None, rstd=None, residual=None, hidden=None, p=0.0, rng=None, row0=0,
+               stream=None):
+    """hidden = residual + dropout(x) (rounded to x's type), out = (hidden - mean) rstd weight + bias.  x, out, residual, hidden
+    [M, K] of one type; weight and bias (or None) [K] of that type or fp32; mean, rstd [M] fp32 for the gradients; p, rng, row0
+    as in dropout.  Outputs that are None are not written."""
+    _opcalls.layer_norm(x, weight, bias, out, eps, mean, rstd, residual, hidden, p, rng, row0, stream)
+
+
+def layer_norm_bwd_work(rows, cols) -> int:
+    """fp32 elements of layer_norm_bwd's workspace."""
+    n = _i64(0)
+    _check(_lib.entwine_layer_norm_bwd_work(int(rows), int(cols), ctypes.byref(n)), "entwine_layer_norm_bwd_work")
+    return n.value
+
+
+def layer_norm_bwd(dout, hidden, weight, mean, rstd, dx, dweight, dbias, work, dhidden=None, dresidual=None, p=0.0, rng=None,
+                   row0=0, stream=None):
+    """Gradients of layer_norm: dx [M, K] (of x, through the dropout), dresidual [M, K] (of the residual and of hidden; None: not
+    written), dweight and dbias (or None) [K] fp32.  dhidden: the gradient that reaches hidden itself.  work: contiguous fp32,
+    layer_norm_bwd_work(M, K) elements or more, one for each call that may overlap."""
+    _opcalls.layer_norm_bwd(dout, hidden, weight, mean, rstd, dx, dweight, dbias, work, dhidden, dresidual, p, rng, row0, stream)
