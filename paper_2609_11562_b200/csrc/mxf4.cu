@@ -12,7 +12,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlock = 32;  // elements that share a scale
 constexpr int64_t kMaxRows = 2147483647;
-constexpr int64_t kMaxCols = 2147483647 - 65536;
+constexpr int64_t kMaxCols = 2147483647 - 65536;  // column numbers of a CTA's last, idle threads fit 32 bits
 
 struct Params {
   void* x;         // values, read or written
@@ -49,30 +49,31 @@ __device__ __forceinline__ uint32_t codes2(float a, float b) {
 // code).  The product with the inverse power of two is exact as far as the rounding to a code can see.
 template <typename T, int P, bool VEC>
 __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
-  const int64_t row = int64_t(blockIdx.x) * (kThreads / a.row_threads) + slot;
+  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
+  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
   const bool there = row < a.rows;
   const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
   uint8_t* const q = a.q + row * a.ldq;
   uint8_t* const scale = a.scale + row * a.lds;
-  const int step = P * a.row_threads;
+  const int step = 8 * P * a.row_threads, cols = there ? a.cols : 0;
   // (whole warps go through the loop together: they vote on the blocks' scales)
-  for (int64_t g0 = int64_t(blockIdx.y) * step; g0 * 8 < a.cols; g0 += int64_t(gridDim.y) * step) {
+  for (int64_t base = int64_t(blockIdx.y) * step; base < a.cols; base += int64_t(gridDim.y) * step) {
+    const int c0 = int(base);
     float f[P][8];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int64_t at = (g0 + i * a.row_threads + lane) * 8;
-      load8<T, VEC>(x + at, there && at < a.cols ? int(a.cols - at) : 0, f[i]);
+      const int at = c0 + 8 * (i * a.row_threads + lane);
+      load8<T, VEC>(x + at, max(cols - at, 0), f[i]);
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int64_t at = (g0 + i * a.row_threads + lane) * 8;
+      const int at = c0 + 8 * (i * a.row_threads + lane);
       uint32_t top = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7fffffffu);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2)) >> 23;
-      if (!there || at >= a.cols) continue;
+      if (at >= cols) continue;
       const bool fine = top < 255;
       const uint32_t byte = fine ? (top > 2 ? top - 2 : 0) : 255;
       const float up = __uint_as_float((254 - byte) << 23);
@@ -95,18 +96,19 @@ __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
 
 template <typename T, int P, bool VEC>
 __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) {
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
-  const int64_t row = int64_t(blockIdx.x) * (kThreads / a.row_threads) + slot;
+  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
+  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
   if (row >= a.rows) return;
   T* const x = static_cast<T*>(a.x) + row * a.ldx;
   const uint8_t* const q = a.q + row * a.ldq;
   const uint8_t* const scale = a.scale + row * a.lds;
-  const int step = P * a.row_threads;
-  for (int64_t g0 = int64_t(blockIdx.y) * step; g0 * 8 < a.cols; g0 += int64_t(gridDim.y) * step) {
+  const int step = 8 * P * a.row_threads;
+  for (int64_t base = int64_t(blockIdx.y) * step; base < a.cols; base += int64_t(gridDim.y) * step) {
+    const int c0 = int(base);
     uint32_t w[P], byte[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int64_t at = (g0 + i * a.row_threads + lane) * 8;
+      const int at = c0 + 8 * (i * a.row_threads + lane);
       w[i] = byte[i] = 0;
       if (at < a.cols) {
         byte[i] = scale[at / kBlock];
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) 
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int64_t at = (g0 + i * a.row_threads + lane) * 8;
+      const int at = c0 + 8 * (i * a.row_threads + lane);
       if (at >= a.cols) continue;
       // 2^(byte-127); 2^-127 is half of the least normal number, 255 stands for NaN
       const float s = __uint_as_float(byte[i] == 255 ? 0x7fffffffu : byte[i] ? byte[i] << 23 : 0x00400000u);
@@ -151,21 +153,26 @@ __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) 
   }
 }
 
-constexpr int kEach = 2;  // groups of eight elements a thread
+template <typename T, int P>
+int run_by(Params a, bool back, bool vec, cudaStream_t stream) {
+  const int64_t groups = (int64_t(a.cols) + 7) / 8;
+  // whole warps of a row's threads where a row has that much
+  a.row_threads = int(std::min<int64_t>(kThreads, (groups + P * 32 - 1) / (P * 32) * 32));
+  while (a.row_threads > 4 && a.row_threads / 2 * P >= groups) a.row_threads /= 2;
+  const int per_cta = kThreads / a.row_threads;
+  const int64_t chunks = (groups + P * a.row_threads - 1) / (P * a.row_threads);
+  const dim3 grid(unsigned((a.rows + per_cta - 1) / per_cta), unsigned(std::min<int64_t>(chunks, 65535)));
+  auto kernel = back ? (vec ? dequant_mxf4_kernel<T, P, true> : dequant_mxf4_kernel<T, P, false>)
+                     : (vec ? quant_mxf4_kernel<T, P, true> : quant_mxf4_kernel<T, P, false>);
+  kernel<<<grid, per_cta * a.row_threads, 0, stream>>>(a);
+  return launched(cudaSuccess);
+}
 
 template <typename T>
-int run(Params a, bool back, cudaStream_t stream) {
+int run(const Params& a, bool back, cudaStream_t stream) {
   const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.q, a.ldq, 1, 4);
-  const int64_t groups = (int64_t(a.cols) + 7) / 8;
-  a.row_threads = 4;
-  while (a.row_threads < kThreads && int64_t(a.row_threads) * kEach < groups) a.row_threads *= 2;
-  const int per_cta = kThreads / a.row_threads;
-  const int64_t chunks = (groups + kEach * a.row_threads - 1) / (kEach * a.row_threads);
-  const dim3 grid(unsigned((a.rows + per_cta - 1) / per_cta), unsigned(std::min<int64_t>(chunks, 65535)));
-  auto kernel = back ? (vec ? dequant_mxf4_kernel<T, kEach, true> : dequant_mxf4_kernel<T, kEach, false>)
-                     : (vec ? quant_mxf4_kernel<T, kEach, true> : quant_mxf4_kernel<T, kEach, false>);
-  kernel<<<grid, kThreads, 0, stream>>>(a);
-  return launched(cudaSuccess);
+  // little work: one group a thread, for the latency
+  return a.rows * int64_t(a.cols) < (1 << 20) ? run_by<T, 1>(a, back, vec, stream) : run_by<T, 4>(a, back, vec, stream);
 }
 
 int convert(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* q, int64_t ldq,

@@ -20,11 +20,11 @@ constexpr int64_t kMaxRows = 2147483647;
 // bijection of a 128-bit counter under a 64-bit key.  The counter is (column / 8, row, offset), the key the seed; its
 // four words are eight 16-bit numbers, one for each column.  16 bits decide whether an element is kept with probability
 // 1 - t / 65536 exactly, and what is kept is multiplied with 65536 / (65536 - t): the expectation is exact, p itself is
-// taken to the nearest 2^-16.  With 32 bits an element the generator, about 70 instructions a call, would be the bound
-// instead of the memory.
+// taken to the nearest 2^-16.  With 32 bits an element the generator, 50 instructions a call, would be the bound instead
+// of the memory.
 struct Dropout {
   const int64_t* rng;  // {seed, offset}
-  uint32_t t;          // elements whose number is below are dropped
+  uint32_t t16;        // t * 65536: elements whose number is below t are dropped
   float scale;
   uint32_t row0;       // number of the first row
 };
@@ -38,77 +38,112 @@ struct Stream {
     o0 = uint32_t(offset);
     o1 = uint32_t(offset >> 32);
   }
-  __device__ __forceinline__ void words(uint32_t group, uint32_t row, uint32_t (&c)[4]) const {
-    uint32_t x = group, y = row, z = o0, w = o1, a = k0, b = k1;
+  // The words of P groups of a row, `step` groups apart, round by round together: they share the keys.
+  template <int P>
+  __device__ __forceinline__ void words(uint32_t group, uint32_t step, uint32_t row, uint32_t (&c)[P][4]) const {
+    uint32_t a = k0, b = k1;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      c[i][0] = group + i * step;
+      c[i][1] = row;
+      c[i][2] = o0;
+      c[i][3] = o1;
+    }
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
-      const uint64_t m = uint64_t(x) * 0xD2511F53u, n = uint64_t(z) * 0xCD9E8D57u;
-      x = uint32_t(n >> 32) ^ y ^ a;
-      y = uint32_t(n);
-      z = uint32_t(m >> 32) ^ w ^ b;
-      w = uint32_t(m);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const uint64_t m = uint64_t(c[i][0]) * 0xD2511F53u, n = uint64_t(c[i][2]) * 0xCD9E8D57u;
+        c[i][0] = uint32_t(n >> 32) ^ c[i][1] ^ a;
+        c[i][1] = uint32_t(n);
+        c[i][2] = uint32_t(m >> 32) ^ c[i][3] ^ b;
+        c[i][3] = uint32_t(m);
+      }
       a += 0x9E3779B9u;
       b += 0xBB67AE85u;
     }
-    c[0] = x;
-    c[1] = y;
-    c[2] = z;
-    c[3] = w;
   }
 };
-__device__ __forceinline__ bool kept(const uint32_t (&c)[4], int e, uint32_t t) {
-  return ((c[e / 2] >> (16 * (e & 1))) & 0xffffu) >= t;
+// Number e of a group's eight is at least t: its word, the number shifted to the top, is at least t * 65536.
+__device__ __forceinline__ bool kept(const uint32_t (&c)[4], int e, uint32_t t16) {
+  return (e & 1 ? c[e / 2] : c[e / 2] << 16) >= t16;
 }
-// A dropped element is 0 whatever it held.
-__device__ __forceinline__ void drop8(const Stream& s, const Dropout& d, uint32_t row, uint32_t group, float (&f)[8]) {
-  uint32_t c[4];
-  s.words(group, row, c);
+// residual + dropout: a dropped element is 0 whatever it held.
+__device__ __forceinline__ void drop8(const uint32_t (&c)[4], const Dropout& d, float (&f)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = kept(c, e, d.t) ? f[e] * d.scale : 0.0f;
+  for (int e = 0; e < 8; ++e) f[e] = kept(c, e, d.t16) ? f[e] * d.scale : 0.0f;
 }
 __device__ __forceinline__ float drop1(const Stream& s, const Dropout& d, uint32_t row, uint32_t col, float f) {
-  uint32_t c[4];
-  s.words(col / kGroup, row, c);
-  uint32_t w = c[0];
+  uint32_t c[1][4];
+  s.words<1>(col / kGroup, 0, row, c);
+  uint32_t w = c[0][0];
 #pragma unroll
-  for (int i = 1; i < 4; ++i) w = int(col % kGroup) / 2 == i ? c[i] : w;
-  return ((w >> (16 * (col & 1))) & 0xffffu) >= d.t ? f * d.scale : 0.0f;
+  for (int i = 1; i < 4; ++i) w = int(col % kGroup) / 2 == i ? c[0][i] : w;
+  return (col & 1 ? w : w << 16) >= d.t16 ? f * d.scale : 0.0f;
 }
 
 // ------------------------------------------------------------------------------------------
 // groups of eight elements
 // ------------------------------------------------------------------------------------------
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
-  if constexpr (VEC) {
-    constexpr int V = 16 / sizeof(T);
+// Eight elements as they lie in memory: four words of a 16-bit type, eight of fp32.
+template <typename T>
+struct Raw {
+  static constexpr int V = 16 / sizeof(T), N = 8 / V;
+  Piece<T, V> v[N];
+  template <bool VEC>
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VEC) {
 #pragma unroll
-    for (int i = 0; i < 8 / V; ++i) {
+      for (int i = 0; i < N; ++i) v[i] = reinterpret_cast<const Piece<T, V>*>(p)[i];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e / V].e[e % V] = p[e];
+    }
+  }
+  template <bool VEC>
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) reinterpret_cast<Piece<T, V>*>(p)[i] = v[i];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = v[e / V].e[e % V];
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
       float g[V];
-      unpack<T, V>(reinterpret_cast<const Piece<T, V>*>(p)[i], g);
+      unpack<T, V>(v[i], g);
 #pragma unroll
       for (int e = 0; e < V; ++e) f[i * V + e] = g[e];
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = Elem<T>::up(p[e]);
   }
-}
-template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
-  if constexpr (VEC) {
-    constexpr int V = 16 / sizeof(T);
+  __device__ __forceinline__ void set(const float (&f)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8 / V; ++i) {
+    for (int i = 0; i < N; ++i) {
       float g[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) g[e] = f[i * V + e];
-      reinterpret_cast<Piece<T, V>*>(p)[i] = pack<T, V>(g);
+      v[i] = pack<T, V>(g);
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = Elem<T>::down(f[e]);
   }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = Piece<T, V>{};
+  }
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+  Raw<T> r;
+  r.template load<VEC>(p);
+  r.get(f);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
+  Raw<T> r;
+  r.set(f);
+  r.template store<VEC>(p);
 }
 template <typename T>
 __device__ __forceinline__ float rounded(float f) {
@@ -147,7 +182,7 @@ constexpr int kDropThreads = 256;
 // P groups of eight elements a thread; a CTA takes as many rows as fit.
 template <typename T, int P, bool VEC>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams a) {
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
+  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
   const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
   if (row >= a.rows) return;
   const Stream rng(a.d.rng);
@@ -155,27 +190,33 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams 
   const T* const r = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
   T* const out = static_cast<T*>(a.out) + row * a.ldo;
   const uint32_t number = a.d.row0 + uint32_t(row);
-  const int full = a.cols / kGroup;
-  for (int64_t g0 = int64_t(blockIdx.y) * P * a.row_threads; g0 < full; g0 += int64_t(gridDim.y) * P * a.row_threads) {
-    float f[P][8], res[P][8];
+  const int full = a.cols / kGroup, step = P * a.row_threads;
+  for (int g0 = int(blockIdx.y) * step + lane; g0 < full; g0 += int(gridDim.y) * step) {
+    Raw<T> v[P], res[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int64_t g = g0 + i * a.row_threads + lane;
+      const int g = g0 + i * a.row_threads;
       if (g < full) {
-        load8<T, VEC>(x + g * kGroup, f[i]);
-        if (r) load8<T, VEC>(r + g * kGroup, res[i]);
+        v[i].template load<VEC>(x + int64_t(g) * kGroup);
+        if (r) res[i].template load<VEC>(r + int64_t(g) * kGroup);
       }
     }
+    uint32_t c[P][4];
+    rng.words<P>(uint32_t(g0), uint32_t(a.row_threads), number, c);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int64_t g = g0 + i * a.row_threads + lane;
+      const int g = g0 + i * a.row_threads;
       if (g < full) {
-        drop8(rng, a.d, number, uint32_t(g), f[i]);
+        float f[8];
+        v[i].get(f);
+        drop8(c[i], a.d, f);
         if (r) {
+          float h[8];
+          res[i].get(h);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[i][e] += res[i][e];
+          for (int e = 0; e < 8; ++e) f[e] += h[e];
         }
-        store8<T, VEC>(out + g * kGroup, f[i]);
+        store8<T, VEC>(out + int64_t(g) * kGroup, f);
       }
     }
   }
@@ -187,20 +228,26 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams 
   }
 }
 
-template <typename T>
-int run_dropout(DropParams a, cudaStream_t stream) {
-  const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.out, a.ldo, sizeof(T)) &&
-                   (!a.residual || aligned_rows(a.residual, a.ldr, sizeof(T)));
-  constexpr int P = 2;
-  const int64_t full = a.cols / kGroup;
-  a.row_threads = 8;
-  while (a.row_threads < kDropThreads && int64_t(a.row_threads) * P < full) a.row_threads *= 2;
+template <typename T, int P>
+int run_dropout_by(DropParams a, bool vec, cudaStream_t stream) {
+  const int64_t full = std::max(1, a.cols / kGroup);
+  // whole warps of a row's threads where a row has that much
+  a.row_threads = int(std::min<int64_t>(kDropThreads, (full + 31) / 32 * 32 < 32 * P ? 32 : (full + P * 32 - 1) / (P * 32) * 32));
+  while (a.row_threads > 8 && a.row_threads / 2 * P >= full) a.row_threads /= 2;
   const int per_cta = kDropThreads / a.row_threads;
-  const int64_t chunks = std::max<int64_t>(1, (full + P * a.row_threads - 1) / (P * a.row_threads));
+  const int64_t chunks = (full + P * a.row_threads - 1) / (P * a.row_threads);
   const dim3 grid(unsigned((a.rows + per_cta - 1) / per_cta), unsigned(std::min<int64_t>(chunks, 65535)));
   auto kernel = vec ? dropout_kernel<T, P, true> : dropout_kernel<T, P, false>;
-  kernel<<<grid, kDropThreads, 0, stream>>>(a);
+  kernel<<<grid, per_cta * a.row_threads, 0, stream>>>(a);
   return launched(cudaSuccess);
+}
+
+template <typename T>
+int run_dropout(const DropParams& a, cudaStream_t stream) {
+  const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.out, a.ldo, sizeof(T)) &&
+                   (!a.residual || aligned_rows(a.residual, a.ldr, sizeof(T)));
+  // little work: one group a thread, for the latency
+  return a.rows * int64_t(a.cols) < (1 << 20) ? run_dropout_by<T, 1>(a, vec, stream) : run_dropout_by<T, 2>(a, vec, stream);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -234,65 +281,68 @@ __device__ __forceinline__ float row_sum(float v, float* part, int first_warp, i
 
 // A row in registers: up to P groups a thread and one element of the last, incomplete group.  The mean first, then the
 // mean of the squared distances from it: no difference of large sums.
-template <typename T, int P, bool VEC>
-__global__ void __launch_bounds__(1024) norm_rows_kernel(const NormParams a) {
+template <typename T, int P, bool VEC, bool DROP>
+__global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const NormParams a) {
   __shared__ float part[2][32];
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
+  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
   const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
   const bool there = row < a.rows;
-  const int full = a.cols / kGroup, tail = full * kGroup + lane;
+  const int full = there ? a.cols / kGroup : 0, tail = full * kGroup + lane;
   const bool has_tail = there && lane < kGroup && tail < a.cols;
   const uint32_t number = a.d.row0 + uint32_t(row);
   const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
   const T* const res = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
   T* const hidden = a.hidden ? static_cast<T*>(a.hidden) + row * a.ldh : nullptr;
-  float h[P][8], last = 0.0f, sum = 0.0f;
+  Raw<T> v[P];
+  float last = 0.0f, sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const int g = i * a.row_threads + lane;
-    if (there && g < full) {
-      load8<T, VEC>(x + g * kGroup, h[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) h[i][e] = 0.0f;
-    }
+    if (g < full) v[i].template load<VEC>(x + g * kGroup);
+    else v[i].zero();
   }
   if (has_tail) last = Elem<T>::up(x[tail]);
-  if (a.d.rng || res) {
-    float r[P][8];
+  if (DROP || res) {
+    Raw<T> r[P];
+    if (res) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int g = i * a.row_threads + lane;
-      if (res && there && g < full) load8<T, VEC>(res + g * kGroup, r[i]);
+      for (int i = 0; i < P; ++i) {
+        const int g = i * a.row_threads + lane;
+        if (g < full) r[i].template load<VEC>(res + g * kGroup);
+      }
     }
-    const Stream rng(a.d.rng);
+    uint32_t c[P][4];
+    const Stream rng(DROP ? a.d.rng : nullptr);
+    if constexpr (DROP) rng.words<P>(uint32_t(lane), uint32_t(a.row_threads), number, c);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int g = i * a.row_threads + lane;
-      if (there && g < full) {
-        if (a.d.rng) drop8(rng, a.d, number, uint32_t(g), h[i]);
+      if (i * a.row_threads + lane < full) {
+        float f[8];
+        v[i].get(f);
+        if constexpr (DROP) drop8(c[i], a.d, f);
+        if (res) {
+          float h[8];
+          r[i].get(h);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[i][e] = rounded<T>(res ? h[i][e] + r[i][e] : h[i][e]);
-        if (hidden) store8<T, VEC>(hidden + g * kGroup, h[i]);
+          for (int e = 0; e < 8; ++e) f[e] += h[e];
+        }
+        v[i].set(f);  // rounded, as it is written
       }
     }
     if (has_tail) {
-      if (a.d.rng) last = drop1(rng, a.d, number, uint32_t(tail), last);
+      if (DROP) last = drop1(rng, a.d, number, uint32_t(tail), last);
       last = rounded<T>(res ? last + Elem<T>::up(res[tail]) : last);
-      if (hidden) hidden[tail] = Elem<T>::down(last);
     }
-  } else if (hidden && there) {
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int g = i * a.row_threads + lane;
-      if (g < full) store8<T, VEC>(hidden + g * kGroup, h[i]);
-    }
-    if (has_tail) hidden[tail] = Elem<T>::down(last);
   }
+  float h[P][8];
 #pragma unroll
-  for (int i = 0; i < P; ++i)
+  for (int i = 0; i < P; ++i) {
+    if (hidden && i * a.row_threads + lane < full) v[i].template store<VEC>(hidden + (i * a.row_threads + lane) * kGroup);
+    v[i].get(h[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += h[i][e];
+  }
+  if (hidden && has_tail) hidden[tail] = Elem<T>::down(last);
   sum += last;
   const int first_warp = slot * (a.row_threads / 32), warps = a.row_threads / 32;
   const float mean = row_sum(sum, part[0], first_warp, warps) / float(a.cols);
@@ -301,9 +351,15 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(const NormParams a) {
   for (int i = 0; i < P; ++i)
     if (i * a.row_threads + lane < full) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) square = fmaf(h[i][e] - mean, h[i][e] - mean, square);
+      for (int e = 0; e < 8; ++e) {
+        h[i][e] -= mean;
+        square = fmaf(h[i][e], h[i][e], square);
+      }
     }
-  if (has_tail) square = fmaf(last - mean, last - mean, square);
+  if (has_tail) {
+    last -= mean;
+    square = fmaf(last, last, square);
+  }
   const float rstd = 1.0f / sqrtf(row_sum(square, part[1], first_warp, warps) / float(a.cols) + a.eps);
   if (!there) return;
   if (lane == 0) {
@@ -320,12 +376,11 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(const NormParams a) {
       weight.template load<VEC>(g * kGroup, w);
       if (a.bias) bias.template load<VEC>(g * kGroup, b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[i][e] = fmaf((h[i][e] - mean) * rstd, w[e], b[e]);
+      for (int e = 0; e < 8; ++e) h[i][e] = fmaf(h[i][e] * rstd, w[e], b[e]);
       store8<T, VEC>(out + g * kGroup, h[i]);
     }
   }
-  if (has_tail)
-    out[tail] = Elem<T>::down(fmaf((last - mean) * rstd, weight.one(tail), a.bias ? bias.one(tail) : 0.0f));
+  if (has_tail) out[tail] = Elem<T>::down(fmaf(last * rstd, weight.one(tail), a.bias ? bias.one(tail) : 0.0f));
 }
 
 constexpr int kLongThreads = 512;
@@ -370,6 +425,12 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_rows_kernel(const Norm
   }
 }
 
+template <typename T, bool DROP>
+auto pick_norm(int each, bool vec) {
+  if (!vec) return each == 1 ? norm_rows_kernel<T, 1, false, DROP> : each == 2 ? norm_rows_kernel<T, 2, false, DROP> : norm_rows_kernel<T, 4, false, DROP>;
+  return each == 1 ? norm_rows_kernel<T, 1, true, DROP> : each == 2 ? norm_rows_kernel<T, 2, true, DROP> : norm_rows_kernel<T, 4, true, DROP>;
+}
+
 template <typename T>
 int run_norm(NormParams a, cudaStream_t stream) {
   auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
@@ -378,19 +439,18 @@ int run_norm(NormParams a, cudaStream_t stream) {
                    (!a.hidden || aligned_rows(a.hidden, a.ldh, sizeof(T))) && aligned(a.weight) &&
                    (!a.bias || aligned(a.bias));
   const int64_t groups = std::max(1, a.cols / kGroup);
-  if (groups > 4 * 1024) {
+  if (groups > 4 * 512) {
     norm_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
     return launched(cudaSuccess);
   }
   // few rows: many threads with little each, for the latency
   const int most = a.rows < 512 ? 1 : a.rows < 2048 ? 2 : 4;
-  const int each = groups <= most * 1024 ? most : groups <= 2048 ? 2 : 4;
+  const int each = groups <= most * 512 ? most : groups <= 1024 ? 2 : 4;
   const int64_t warps = (groups + each * 32 - 1) / (each * 32);
   a.row_threads = int(warps * 32);
   const int per_cta = std::max(1, 128 / a.row_threads), threads = per_cta * a.row_threads;
   const unsigned grid = unsigned((a.rows + per_cta - 1) / per_cta);
-  auto kernel = vec ? (each == 1 ? norm_rows_kernel<T, 1, true> : each == 2 ? norm_rows_kernel<T, 2, true> : norm_rows_kernel<T, 4, true>)
-                    : (each == 1 ? norm_rows_kernel<T, 1, false> : each == 2 ? norm_rows_kernel<T, 2, false> : norm_rows_kernel<T, 4, false>);
+  auto kernel = a.d.rng ? pick_norm<T, true>(each, vec) : pick_norm<T, false>(each, vec);
   kernel<<<grid, threads, 0, stream>>>(a);
   return launched(cudaSuccess);
 }
@@ -532,7 +592,11 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const GradParam
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, g[i][e] - s.x - n[i][e] * s.y, f[e]);
         if (dresidual) store8<T, VEC>(dresidual + at * kGroup, f);
-        if (a.d.rng) drop8(rng, a.d, number, uint32_t(at), f);
+        if (a.d.rng) {
+          uint32_t c[1][4];
+          rng.words<1>(uint32_t(at), 0, number, c);
+          drop8(c[0], a.d, f);
+        }
         store8<T, VEC>(dx + at * kGroup, f);
       }
     }
@@ -660,7 +724,7 @@ bool make_dropout(double p, const int64_t* rng, int64_t row0, int64_t rows, Drop
   const double t = std::nearbyint(p * 65536.0);
   if (t > 65535.0 || (p > 0.0 && bad_pointer(rng, 8))) return false;
   d->rng = t > 0.0 ? rng : nullptr;
-  d->t = uint32_t(t);
+  d->t16 = uint32_t(t) << 16;
   d->scale = float(65536.0 / (65536.0 - t));
   d->row0 = uint32_t(row0);
   return true;
