@@ -9,6 +9,7 @@
 #include <atomic>
 #include <cstring>
 
+#include "gemm_tiles.cuh"
 #include "ops_common.cuh"
 #include "sm100.cuh"
 
@@ -19,7 +20,6 @@ constexpr int kChannels = 128;       // channels of a tile
 constexpr int kKBytes = 128;         // elements of K per pipeline stage (one swizzled row)
 constexpr int kThreads = 128;
 constexpr int kMaxSplit = 8;
-constexpr int kMaxGroups = 1024;
 constexpr int64_t kMaxK = 131071;    // 128 * 128 * K < 2^31
 constexpr int64_t kMaxExtent = 2147483647;
 constexpr int64_t kMaxRows = kMaxExtent - 65536;                  // row and channel numbers of the last tiles, which reach
@@ -38,10 +38,8 @@ struct Maps {
 
 // (a pair tile: 256 channels, up to 256 tokens)
 constexpr int kPairThreads = 320;    // TMA warp, MMA warp, eight epilogue warps
-constexpr int kPairChannels = 256;
 constexpr int kPairTokens = 256;
 constexpr int kPairStageBytes = 32768;
-constexpr int kBand = 16;            // token tiles that share a walk over the channels: their rows stay in L2
 
 struct Params {
   const float* scale_a;
@@ -85,38 +83,6 @@ struct Tile {
   static constexpr int kSmem = kStages * kStageBytes + 1024;
   static constexpr int kTmemCols = TOKENS < 32 ? 32 : TOKENS;
 };
-
-// Expert and token rows of token tile `tile`, found by one warp: experts have ceil(rows / TOKENS) tiles each.
-template <int TOKENS>
-__device__ __forceinline__ void find_tile(const Params& P, int tile, int lane, int* group, int* m0, int* m_end) {
-  *group = -1;
-  int before = 0;
-  for (int g0 = 0; g0 < P.G; g0 += 32) {
-    const int g = g0 + lane;
-    int lo = 0, hi = 0;
-    if (g < P.G) {
-      lo = min(max(P.offsets[g], 0), P.M);
-      hi = min(max(P.offsets[g + 1], lo), P.M);
-    }
-    const int tiles = (hi - lo + TOKENS - 1) / TOKENS;
-    int sum = tiles;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += v;
-    }
-    const int first = before + sum - tiles;
-    const unsigned here = __ballot_sync(0xffffffffu, tile >= first && tile < first + tiles);
-    if (here) {
-      const int src = __ffs(here) - 1;
-      *group = g0 + src;
-      *m0 = __shfl_sync(0xffffffffu, lo + (tile - first) * TOKENS, src);
-      *m_end = __shfl_sync(0xffffffffu, hi, src);
-      return;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
-  }
-}
 
 // One tile of 128 channels x TOKENS tokens per cluster of one to eight CTAs, which share the length K: each sums its
 // blocks of K, then the int32 partial sums (exact in any order) meet through distributed shared memory, each CTA
@@ -295,10 +261,6 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
 // half of the tokens), so that an SM takes in 64 bytes per cycle at the full MMA rate instead of 96.  A tile's products
 // are as wide as its tokens, in steps of 32 (what is loaded is not: a whole tile's tokens, however few the expert has).
 // Two accumulators in TMEM: the epilogue of a tile runs beside the products of the next.
-struct PairTile {
-  int g, m0, rows, n0;
-};
-
 template <typename Out>
 struct PairCfg {
   static constexpr int kStages = sizeof(Out) == 4 ? 5 : 6;
@@ -331,40 +293,6 @@ __device__ __forceinline__ void store_rows(const Out* in, Out* out, int64_t ldc,
   }
 }
 
-// What the walk over the tiles needs of each expert.
-struct PairGroups {
-  int first[kMaxGroups + 1];  // token tiles of the experts before
-  int start[kMaxGroups];      // first row
-  int end[kMaxGroups];
-  int height[kMaxGroups];     // rows of a tile: an expert's tiles are as equal as steps of 32 rows allow
-};
-
-// The tiles of a pair, in order.  An expert's bands of kBand token tiles each walk over the channels together.
-struct PairWalk {
-  const PairGroups& G;
-  int channel_tiles;
-  int g = 0;
-  __device__ __forceinline__ PairTile at(int t) {
-    while (G.first[g + 1] * channel_tiles <= t) ++g;
-    const int tiles = G.first[g + 1] - G.first[g];
-    int local = t - G.first[g] * channel_tiles, m = 0, in_band = tiles;
-    if (tiles > kBand) {
-      const int band = local / (kBand * channel_tiles);
-      local -= band * kBand * channel_tiles;
-      m = band * kBand;
-      in_band = min(kBand, tiles - m);
-    }
-    const int channel = int(unsigned(local) / unsigned(in_band));
-    m += local - channel * in_band;
-    PairTile r;
-    r.g = g;
-    r.m0 = G.start[g] + m * G.height[g];
-    r.rows = min(G.height[g], G.end[g] - r.m0);
-    r.n0 = channel * kPairChannels;
-    return r;
-  }
-};
-
 template <typename Out>
 __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __grid_constant__ Maps maps,
                                                                        const __grid_constant__ Params P) {
@@ -394,42 +322,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_i8_pair_kernel(const __g
     }
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    groups.first[0] = 0;
   }
   if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
-  // token tiles of each expert, then their running sum
-  for (int g = threadIdx.x; g < P.G; g += kPairThreads) {
-    int lo = 0, hi = P.M;
-    if (P.offsets) {
-      lo = min(max(P.offsets[g], 0), P.M);
-      hi = min(max(P.offsets[g + 1], lo), P.M);
-    }
-    const int tiles = (hi - lo + P.tile_rows - 1) / P.tile_rows;
-    groups.start[g] = lo;
-    groups.end[g] = hi;
-    groups.height[g] = tiles > 0 ? ((hi - lo + tiles - 1) / tiles + 31) / 32 * 32 : 0;
-    groups.first[g + 1] = tiles;
-  }
+  groups.count(P, kPairThreads);
   __syncwarp();
   tc_fence_before();
   cluster_sync_all();  // (of this CTA's threads, too) both CTAs' barriers exist before either signals
   tc_fence_after();
   if (P.G > 1) {
-    if (warp == 0) {
-      int before = 0;
-      for (int g0 = 0; g0 < P.G; g0 += 32) {
-        int sum = g0 + lane < P.G ? groups.first[g0 + lane + 1] : 0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, sum, o);
-          if (lane >= o) sum += v;
-        }
-        // (offsets that decrease can claim rows many times over: no more tiles than the bound, within 32 bits)
-        sum = min(sum + before, P.token_tiles);
-        if (g0 + lane < P.G) groups.first[g0 + lane + 1] = sum;
-        before = __shfl_sync(0xffffffffu, sum, 31);
-      }
-    }
+    if (warp == 0) groups.add_up(P, lane);
     __syncthreads();
   }
   const uint32_t tmem = tmem_slot;

@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <cstring>
 
+#include "gemm_tiles.cuh"
 #include "ops_common.cuh"
 #include "sm100.cuh"
 
@@ -20,7 +21,6 @@ constexpr int kKBytes = 128;         // bytes of codes per row and pipeline stag
 constexpr int kScaleBytes = 8;       // their scales
 constexpr int kThreads = 128;
 constexpr int kMaxSplit = 8;
-constexpr int kMaxGroups = 1024;
 constexpr int64_t kMaxK = int64_t(1) << 24;
 constexpr int64_t kMaxExtent = 2147483647;
 constexpr int64_t kMaxRows = kMaxExtent - 65536;                  // row and channel numbers of the last tiles, which reach
@@ -46,6 +46,7 @@ struct Params {
   int kbytes, kscales;     // bytes of a row's codes and scales
   int token_tiles;         // an upper bound with experts
   int split;               // CTAs that share the length K of a tile
+  int tile_rows;           // most tokens of a pair tile, a multiple of 32
   int withhold;            // block of K that the first tile's first CTA or pair does not load; -1: none
   unsigned long long wait_ns;  // budget of every wait
 };
@@ -80,54 +81,39 @@ struct Tile {
   static constexpr int kTmemCols = TOKENS <= 32 ? 64 : 2 * TOKENS;
 };
 
-// Expert and token rows of token tile `tile`, found by one warp: experts have ceil(rows / TOKENS) tiles each.
-template <int TOKENS>
-__device__ __forceinline__ void find_tile(const Params& P, int tile, int lane, int* group, int* m0, int* m_end) {
-  *group = -1;
-  int before = 0;
-  for (int g0 = 0; g0 < P.G; g0 += 32) {
-    const int g = g0 + lane;
-    int lo = 0, hi = 0;
-    if (g < P.G) {
-      lo = min(max(P.offsets[g], 0), P.M);
-      hi = min(max(P.offsets[g + 1], lo), P.M);
-    }
-    const int tiles = (hi - lo + TOKENS - 1) / TOKENS;
-    int sum = tiles;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += v;
-    }
-    const int first = before + sum - tiles;
-    const unsigned here = __ballot_sync(0xffffffffu, tile >= first && tile < first + tiles);
-    if (here) {
-      const int src = __ffs(here) - 1;
-      *group = g0 + src;
-      *m0 = __shfl_sync(0xffffffffu, lo + (tile - first) * TOKENS, src);
-      *m_end = __shfl_sync(0xffffffffu, hi, src);
-      return;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
-  }
-}
-
-// Scales of one stage of ROWS rows, by THREADS threads: two words a row, zeros (a scale that nothing is multiplied with)
-// for rows and blocks that are not there.  Word w of row r goes to place w * 512 + r % 32 * 16 + r / 32 * 4 of its 128 rows.
+// The scales of up to ROWS rows of an operand, fetched stage by stage by THREADS threads: two words of four bytes a row and
+// stage.  Word w of row r goes to place w * 512 + r % 32 * 16 + r / 32 * 4 of its 128 rows; a thread's rows are THREADS / 2
+// apart, so that its places differ by constants.  Rows and blocks that are not there get zeros, a scale that nothing is
+// multiplied with.
 template <int ROWS, int THREADS>
-__device__ __forceinline__ void fetch_scales(const uint8_t* scales, int64_t ld, int rows, int at, int row_bytes,
-                                             uint32_t smem, int thread) {
+struct Scales {
+  static constexpr int N = (2 * ROWS + THREADS - 1) / THREADS, kStep = THREADS / 64;  // rows / 32 from one word to the next
+  static_assert(THREADS % 64 == 0, "whole groups of 32 rows");
+  const uint8_t* from[N];
+  uint32_t place, there, word;
+  // `rows` rows of the matrix lie at and behind `first`, `most` of them are wanted
+  __device__ __forceinline__ Scales(const uint8_t* all, int64_t first, int64_t ld, int rows, int most, int thread) {
+    const int r0 = thread / 2;
+    word = thread % 2;
+    place = word * 512 + r0 % 32 * 16 + r0 / 32 * 4;
+    there = 0;
 #pragma unroll
-  for (int i0 = 0; i0 < 2 * ROWS; i0 += THREADS) {
-    const int i = i0 + thread, r = i / 2, w = i % 2;
-    if (2 * ROWS % THREADS == 0 || i < 2 * ROWS) {
-      const int left = row_bytes - at - 4 * w;
-      const bool there = r < rows && left > 0;
-      cp_async4(smem + r / 128 * 1024 + w * 512 + r % 32 * 16 + r % 128 / 32 * 4,
-                there ? scales + r * ld + at + 4 * w : scales, there ? uint32_t(min(left, 4)) : 0u);
+    for (int k = 0; k < N; ++k) {
+      const int r = r0 + k * (THREADS / 2);
+      const bool ok = r < min(rows, most);
+      from[k] = all + (ok ? first + r * ld : 0) + 4 * word;
+      there |= uint32_t(ok) << k;
     }
   }
-}
+  __device__ __forceinline__ void fetch(uint32_t smem, int at, int row_bytes) const {
+    const int left = row_bytes - at - int(4 * word);
+    const uint32_t bytes = uint32_t(max(0, min(left, 4)));
+    if (left <= 0) at = -int(4 * word);  // (nothing is read there)
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      cp_async4(smem + place + k * kStep / 4 * 1024 + k * kStep % 4 * 4, from[k] + at, there >> k & 1 ? bytes : 0u);
+  }
+};
 
 // One tile of 128 channels x TOKENS tokens per cluster of one to eight CTAs, which share the length K: each sums its
 // blocks of K, then the partial sums meet through distributed shared memory, added in the order of the CTAs, each CTA
@@ -136,7 +122,7 @@ template <int TOKENS, typename Out>
 __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_constant__ Maps maps,
                                                              const __grid_constant__ Params P) {
   using T = Tile<TOKENS>;
-  constexpr int S = T::kStages;
+  constexpr int S = T::kStages, kScaleThreads = kThreads - 64;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * S + 1];
   __shared__ uint32_t tmem_slot;
@@ -178,7 +164,7 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
       job[1] = m0;
       job[2] = m_end;
       for (int s = 0; s < S; ++s) {
-        mbar_init(full + 8 * s, 3);  // the codes, two warps' scales
+        mbar_init(full + 8 * s, 1 + kScaleThreads);  // the codes, every thread's share of the scales
         mbar_init(empty + 8 * s, 1);
       }
       mbar_init(done, 1);
@@ -218,6 +204,7 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
       // the products that read this buffer of scales are done
       if (i >= 2 && !(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * ((i - 2) % S), ((i - 2) / S) & 1)))) break;
       tc_fence_after();
+      fence_async_smem();  // the scales were written by ordinary copies
       const uint32_t at = ring + s * T::kStageBytes, scales = tmem + T::kScaleCol + i % 2 * 16;
       const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
       const uint64_t ds = smem_desc_scales(at + T::kCodes);
@@ -234,28 +221,20 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
     }
     if (elect_one()) tc_commit(done);
   } else {
-    // scales, two stages under way
-    constexpr int kLag = 2;
-    const uint8_t* const sa = P.scale_a + int64_t(m0) * P.ldsa;
-    const uint8_t* const sb = P.scale_b + int64_t(g) * P.scale_stride + int64_t(n0) * P.ldsb;
+    // Scales, as many stages ahead as the ring holds.  (The copies arrive by themselves: a thread that waited for its oldest
+    // ones and fenced them waited for the youngest too.)
     const int thread = threadIdx.x - 64;
-    auto hand_over = [&](int i) {  // stage i's words have arrived
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(full + 8 * (i % S));
-    };
-    int i = 0;
-    for (; i < blocks; ++i) {
+    const Scales<kChannels, kScaleThreads> channels(P.scale_b, int64_t(g) * P.scale_stride + int64_t(n0) * P.ldsb, P.ldsb,
+                                                    P.N - n0, kChannels, thread);
+    const Scales<TOKENS, kScaleThreads> tokens(P.scale_a, int64_t(m0) * P.ldsa, P.ldsa, P.M - m0, TOKENS, thread);
+    for (int i = 0; i < blocks; ++i) {
       if (i >= S && !(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * (i % S), (i / S - 1) & 1)))) break;
       const uint32_t at = ring + i % S * T::kStageBytes + T::kCodes;
-      fetch_scales<kChannels, 64>(sb, P.ldsb, P.N - n0, (first + i) * kScaleBytes, P.kscales, at, thread);
-      fetch_scales<TOKENS, 64>(sa, P.ldsa, P.M - m0, (first + i) * kScaleBytes, P.kscales, at + T::kScales, thread);
-      cp_async_commit();
-      cp_async_wait<kLag>();
-      if (i >= kLag) hand_over(i - kLag);
+      channels.fetch(at, (first + i) * kScaleBytes, P.kscales);
+      tokens.fetch(at + T::kScales, (first + i) * kScaleBytes, P.kscales);
+      cp_async_arrive(full + 8 * (i % S));
     }
-    cp_async_wait<0>();
-    for (int j = max(0, i - kLag); j < i; ++j) hand_over(j);
+    cp_async_wait_all();
   }
   __syncwarp();
   ok = wait_bar(P, done, 0) && ok;
@@ -317,6 +296,346 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
   if (warp == 1) tmem_dealloc(tmem, T::kTmemCols);
 }
 
+// ------------------------------------------------------------------------------------------
+// many tokens: CTA pairs, persistent
+// ------------------------------------------------------------------------------------------
+// Two CTAs of a cluster compute 256 channels x up to 192 tokens (tcgen05 cta_group::2: 128 channels each, each loading
+// half of the tokens' codes and all of their scales).  Two accumulators in TMEM, 2 x 192 of its 512 columns, so that the
+// epilogue of a tile runs beside the products of the next, and five buffers of scales of 24 columns.  (224 tokens leave
+// room for two: the way from products that are done to the next but one's scales is then longer than the products between.)
+constexpr int kScaleWarps = 4;
+constexpr int kPairThreads = 32 * (2 + 8 + kScaleWarps + 1);  // TMA, MMA, eight epilogue warps, scale warps, their messenger
+constexpr int kPairTokens = 192;
+constexpr int kPairCodes = (kChannels + kPairTokens / 2) * kKBytes;  // bytes of a stage
+constexpr int kPairStageBytes = kPairCodes + 3 * 1024;               // and the scales of 128 channels and 256 tokens
+constexpr int kPairStages = 6;
+constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024;
+constexpr int kPairScaleCol = 2 * kPairTokens;
+constexpr int kPairBuffers = 5;
+static_assert(kPairScaleCol + 24 * kPairBuffers <= 512 && kPairBuffers < kPairStages, "TMEM, and barriers that tell a buffer's last use");
+
+// 32 channels (lanes) x 32 tokens (registers) to C: neighbouring lanes exchange halves until each has four consecutive
+// channels of one token, and eight lanes store a token's 64 or 128 bytes.  (Staging the chunk in shared memory cost twice
+// the shared-memory cycles and two barriers.)  `rows` tokens and `left` channels lie inside C.
+template <typename Out>
+__device__ __forceinline__ void store_chunk(const float (&f)[32], Out* out, int64_t ldc, int rows, int left, int step, int lane) {
+  const bool one = lane & 1, two = lane & 2;
+  const int col = lane & ~3;
+  out += int64_t(lane & 3) * ldc + col;
+  const bool vec = step >= int(4 * sizeof(Out)) && col + 4 <= left;
+  auto put = [&](int token, const Piece<Out, 4>& v) {
+    if (token >= rows) return;
+    if (vec) {
+      *reinterpret_cast<Piece<Out, 4>*>(out) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < left) out[e] = v.e[e];
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < 32; j += 4, out += 4 * ldc) {
+    uint32_t w[2 * sizeof(Out)];  // per pair of tokens: two channels of one
+    if constexpr (sizeof(Out) == 2) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float g[2] = {f[j + 2 * i], f[j + 2 * i + 1]};
+        const Piece<Out, 2> p = pack<Out, 2>(g);
+        uint32_t mine;
+        memcpy(&mine, &p, 4);
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
+        w[i] = __byte_perm(mine, other, one ? 0x3276 : 0x5410);
+      }
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, two ? w[0] : w[1], 2);
+      const uint32_t o[2] = {two ? other : w[0], two ? w[1] : other};
+      Piece<Out, 4> v;
+      memcpy(&v, o, 8);
+      put(j + (lane & 3), v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float a = f[j + 2 * i], b = f[j + 2 * i + 1];
+        const float other = __shfl_xor_sync(0xffffffffu, one ? a : b, 1);
+        w[2 * i] = __float_as_uint(one ? other : a);
+        w[2 * i + 1] = __float_as_uint(one ? b : other);
+      }
+      uint32_t o[4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, two ? w[e] : w[2 + e], 2);
+        o[e] = two ? other : w[e];
+        o[2 + e] = two ? w[2 + e] : other;
+      }
+      Piece<Out, 4> v;
+      memcpy(&v, o, 16);
+      put(j + (lane & 3), v);
+    }
+  }
+}
+
+template <typename Out>
+__global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const __grid_constant__ Maps maps,
+                                                                         const __grid_constant__ Params P) {
+  constexpr int S = kPairStages;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[3 * S + 5];
+  __shared__ uint32_t tmem_slot;
+  __shared__ PairGroups groups;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int rank = int(cluster_ctarank());
+  const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * S, tfull = full + 16 * S, tempty = tfull + 16,
+                 drain = tempty + 16, scaled = drain + 8;
+
+  if (threadIdx.x == 0) {
+    tma_prefetch_map(&maps.a);
+    tma_prefetch_map(&maps.b);
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full + 8 * s, 1 + 2);  // the codes, both CTAs' scales
+      mbar_init(empty + 8 * s, 1);
+      mbar_init(scaled + 8 * s, 32 * kScaleWarps);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(tfull + 8 * a, 1);
+      mbar_init(tempty + 8 * a, 16);
+    }
+    mbar_init(drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
+  groups.count(P, kPairThreads);
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync_all();  // (of this CTA's threads, too) both CTAs' barriers exist before either signals
+  tc_fence_after();
+  if (P.G > 1) {
+    if (warp == 0) groups.add_up(P, lane);
+    __syncthreads();
+  }
+  const uint32_t tmem = tmem_slot;
+  const int channel_tiles = (P.N + kPairChannels - 1) / kPairChannels;
+  const int total = groups.first[P.G] * channel_tiles, pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2;
+  const int blocks = (P.kbytes + kKBytes - 1) / kKBytes;
+  PairWalk walk{groups, channel_tiles};
+
+  if (warp == 0) {
+    const uint32_t bytes = kChannels * kKBytes + P.tile_rows / 2 * kKBytes;  // that each CTA brings
+    int stage = 0, in_flight = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int t = pair; ok && t < total; t += pairs) {
+      const PairTile w = walk.at(t);
+      const int n0 = w.n0 + rank * kChannels, m0 = w.m0 + rank * ((w.rows + 31) / 32 * 16);
+      for (int b = 0; b < blocks; ++b) {
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * stage, phase ^ 1)))) break;
+        const uint32_t at = ring + stage * kPairStageBytes, bar = map_to_cta(full + 8 * stage, 0);
+        if (!(t == 0 && b == P.withhold) && elect_one()) {
+          if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * bytes);
+          tma_load_3d_pair(at, &maps.b, b * kKBytes, n0, w.g, bar);
+          tma_load_2d_pair(at + kChannels * kKBytes, &maps.a, b * kKBytes, m0, bar);
+        }
+        __syncwarp();
+        if (in_flight < S) ++in_flight;
+        if (++stage == S) stage = 0, phase ^= 1;
+      }
+    }
+    // All that was loaded is used before the CTA ends, and the arrivals that say so have come (in both CTAs); after a
+    // wait that ran out (of the products, too) copies still under way end first.  Those of rank 1 count on rank 0's
+    // barriers.
+    if (ok && in_flight > 0) {
+      const int last = stage > 0 ? stage - 1 : S - 1;
+      ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * last, stage > 0 ? phase : phase ^ 1));
+    }
+    for (int i = 0; !ok && rank == 0 && i < in_flight; ++i) {
+      if (--stage < 0) stage = S - 1, phase ^= 1;
+      wait_bar(P, full + 8 * stage, phase);
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      // (from uniform registers, where the instructions want their addresses and descriptors)
+      const uint32_t base = uniform(tmem);
+      const int tiles = int(uniform(uint32_t(total)));
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0, buffer = 0;
+      bool ok = true, there = false;
+      int rows = pair < tiles ? walk.at(pair).rows : 0, next_rows = 0;
+      for (int t = pair; ok && t < tiles; t += pairs, rows = next_rows) {
+        const int columns = int(uniform(uint32_t((rows + 31) / 32 * 32)));
+        const uint32_t idesc[2] = {instr_desc_mxf4(columns, kPairChannels, 0), instr_desc_mxf4(columns, kPairChannels, 1)};
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, tempty + 8 * acc, acc_phase ^ 1)))) break;
+        tc_fence_after();
+        const uint32_t d = base + acc * kPairTokens;
+        for (int b = 0; b < blocks; ++b) {
+          if (!(ok = __all_sync(0xffffffffu, there || wait_bar(P, full + 8 * stage, phase)))) break;
+          // (a look at the next block's barrier takes as long as the issue of these products: both at once)
+          there = mbar_test(full + 8 * (stage + 1 < S ? stage + 1 : 0), stage + 1 < S ? phase : phase ^ 1);
+          tc_fence_after();
+          const uint32_t at = ring + stage * kPairStageBytes, scales = base + kPairScaleCol + buffer * 24;
+          const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
+          const uint64_t ds = smem_desc_scales(at + kPairCodes);
+          if (elect_one()) {
+            // channels: two words of K; tokens: two words of the first 128, of the others
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              tmem_copy_scales_pair(scales + 4 * w, ds + w * (512 >> 4));
+              tmem_copy_scales_pair(scales + 8 + 8 * w, ds + ((1024 + 512 * w) >> 4));
+              if (columns > 128) tmem_copy_scales_pair(scales + 12 + 8 * w, ds + ((2048 + 512 * w) >> 4));
+            }
+#pragma unroll
+            for (int k = 0; k < kKBytes / 32; ++k)
+              umma_mxf4_pair(d, da + 2 * k, db + 2 * k, idesc[k % 2], scales + k / 2 * 4, scales + 8 + k / 2 * 8,
+                             b > 0 || k > 0);
+            tc_commit_pair(empty + 8 * stage);
+            if (b == blocks - 1) tc_commit_pair(tfull + 8 * acc);
+          }
+          __syncwarp();
+          if (++buffer == kPairBuffers) buffer = 0;
+          if (++stage == S) stage = 0, phase ^= 1;
+          if (b == 0 && t + pairs < tiles) next_rows = walk.at(t + pairs).rows;  // (while these products run)
+        }
+        if ((acc ^= 1) == 0) acc_phase ^= 1;
+      }
+      // products under way end before the TMEM is given back (the epilogue may have left after a wait that ran out)
+      if (elect_one()) tc_commit_pair(drain, 1);
+      __syncwarp();
+      wait_bar(P, drain, 0);
+    }
+  } else if (warp < 10) {
+    // Epilogue: a warp owns 32 channels (its lane quarter of the accumulator), a lane one of them; groups of four warps
+    // take turns at the 32-token chunks of a tile, a chunk's sums read while the chunk before is worked on.
+    const int q = warp & 3, group = (warp - 2) / 4;
+    constexpr int kTurns = (kPairTokens / 32 + 1) / 2;  // chunks of a tile that a group takes, at most
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int t = pair; t < total; t += pairs) {
+      const PairTile w = walk.at(t);
+      const int n0 = w.n0 + rank * kChannels + q * 32, n = n0 + lane;
+      const float add = n < P.N && P.bias ? P.bias[int64_t(w.g) * P.N + n] : 0.0f;
+      if (!__all_sync(0xffffffffu, wait_bar(P, tfull + 8 * acc, acc_phase))) break;
+      tc_fence_after();
+      const int chunks = (w.rows + 31) / 32;
+      const uint32_t sums = tmem + (uint32_t(q) << 21) + acc * kPairTokens;
+      // (as in the int8 product: this warp's loads have completed, the lanes have met, the tcgen05 fences order the loads
+      // before the products that overwrite the accumulator; no ordinary memory is handed over)
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(tempty + 8 * acc, 0));
+      };
+      uint32_t v[2][32];
+      if (group < chunks) tmem_ld32(sums + group * 32, v[0]);
+      else release();
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int c = group + 2 * i;
+        if (c < chunks) {
+          tmem_ld_wait(v[i % 2]);
+          if (c + 2 < chunks) tmem_ld32(sums + (c + 2) * 32, v[(i + 1) % 2]);
+          else release();
+          float f[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[i % 2][j]) + add;
+          store_chunk<Out>(f, static_cast<Out*>(P.c) + int64_t(w.m0 + c * 32) * P.ldc + n0, P.ldc, w.rows - c * 32, P.N - n0,
+                           P.c_step, lane);
+        }
+      }
+      if ((acc ^= 1) == 0) acc_phase ^= 1;
+    }
+  } else if (warp < 10 + kScaleWarps) {
+    // Scales of both operands, as many stages ahead as the ring holds: the copies arrive on their stage's barrier by
+    // themselves.
+    const int thread = int(threadIdx.x) - 320;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int t = pair; ok && t < total; t += pairs) {
+      const PairTile w = walk.at(t);
+      const int n0 = w.n0 + rank * kChannels, columns = (w.rows + 31) / 32 * 32;
+      const Scales<kChannels, 32 * kScaleWarps> channels(P.scale_b, int64_t(w.g) * P.scale_stride + int64_t(n0) * P.ldsb, P.ldsb,
+                                                         P.N - n0, kChannels, thread);
+      const Scales<kPairTokens, 32 * kScaleWarps> tokens(P.scale_a, int64_t(w.m0) * P.ldsa, P.ldsa, P.M - w.m0, columns, thread);
+      for (int b = 0; b < blocks; ++b) {
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * stage, phase ^ 1)))) break;
+        const uint32_t at = ring + stage * kPairStageBytes + kPairCodes;
+        channels.fetch(at, b * kScaleBytes, P.kscales);
+        tokens.fetch(at + 1024, b * kScaleBytes, P.kscales);
+        cp_async_arrive(scaled + 8 * stage);
+        if (++stage == S) stage = 0, phase ^= 1;
+      }
+    }
+    cp_async_wait_all();
+  } else {
+    // The messenger tells rank 0, whose warp has both CTAs' scales copied to TMEM, that this CTA's of a stage are there and
+    // that the buffer for them is free: the products that read it, five blocks ago, are done.  The fence makes the words,
+    // written by ordinary copies, visible to the tensor core, which reads them in this CTA; by a thread that has copies of
+    // its own under way it would wait for them.  So would an arrival that releases to the cluster: 225 us instead of 134
+    // (8192 x 8192 x 3584).
+    int stage = 0, before = 0;  // before: blocks so far, kPairBuffers at most
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int t = pair; ok && t < total; t += pairs) {
+      for (int b = 0; b < blocks; ++b) {
+        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, scaled + 8 * stage, phase)))) break;
+        if (before == kPairBuffers) {
+          const int s = stage >= kPairBuffers ? stage - kPairBuffers : stage + S - kPairBuffers;
+          if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * s, stage >= kPairBuffers ? phase : phase ^ 1)))) break;
+        } else {
+          ++before;
+        }
+        fence_async_smem();
+        if (lane == 0) mbar_arrive_there(map_to_cta(full + 8 * stage, 0));
+        __syncwarp();
+        if (++stage == S) stage = 0, phase ^= 1;
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // neither CTA signals the other's barriers any more
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+template <typename Out>
+int run_pairs(const Maps& maps, Params P, cudaStream_t stream) {
+  const int64_t token_tiles = P.offsets ? P.M / P.tile_rows + P.G : (P.M + P.tile_rows - 1) / P.tile_rows;
+  const int64_t tiles = token_tiles * ((P.N + kPairChannels - 1) / kPairChannels);
+  if (tiles > kMaxExtent) return ENTWINE_ERR_INVALID;
+  P.token_tiles = int(token_tiles);
+  auto kernel = gemm_mxf4_pair_kernel<Out>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+  if (e != cudaSuccess) return launched(e);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(std::min<int64_t>(2 * tiles, sm_count() / 2 * 2)));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = kPairSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {2, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return launched(cudaLaunchKernelEx(&cfg, kernel, maps, P));
+}
+
+// The height of the pair tiles.  Four instructions of a tile h tokens high move 32 KB + 128 h bytes through an SM's
+// shared memory (operands written by TMA, read by the tensor core, half of the tokens by either CTA), 256 + h cycles;
+// the products themselves take 2 h.  So a tile costs 256 + h, and the rows of one matrix are cut so that the waves of
+// the pairs cost least together.
+int pair_rows(const Params& P) {
+  if (P.G > 1) return kPairTokens;
+  const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels, pairs = sm_count() / 2;
+  int best = kPairTokens;
+  int64_t least = 0;
+  for (int rows = kPairTokens; rows >= 96; rows -= 32) {
+    const int64_t token_tiles = (P.M + rows - 1) / rows, waves = (token_tiles * channel_tiles + pairs - 1) / pairs;
+    const int64_t cost = waves * (rows + 256);
+    if (least == 0 || cost < least) least = cost, best = rows;
+  }
+  return best;
+}
+
 template <int TOKENS, typename Out>
 int run(const Maps& maps, Params P, cudaStream_t stream) {
   using T = Tile<TOKENS>;
@@ -371,7 +690,14 @@ template <typename Out>
 int run_as(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t expert_stride, const Params& P,
            cudaStream_t stream) {
   const int rows = (P.M + P.G - 1) / P.G;  // of an average expert
+  const int64_t pair_tiles = int64_t(std::min(P.G, P.M)) * ((P.N + kPairChannels - 1) / kPairChannels);
   Maps maps;
+  if (rows > 128 ? (rows + 127) / 128 * pair_tiles >= sm_count() / 4 : pair_tiles >= sm_count()) {
+    Params Q = P;
+    Q.tile_rows = pair_rows(P);
+    if (!make_maps(&maps, A, lda, B, ldb, expert_stride, Q, Q.tile_rows / 2)) return ENTWINE_ERR_CUDA;
+    return run_pairs<Out>(maps, Q, stream);
+  }
   // the narrowest tile that holds them
   const int tokens = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   if (!make_maps(&maps, A, lda, B, ldb, expert_stride, P, tokens)) return ENTWINE_ERR_CUDA;
