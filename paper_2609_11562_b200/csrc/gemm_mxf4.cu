@@ -67,6 +67,10 @@ __device__ __forceinline__ bool wait_bar(const Params& P, uint32_t bar, uint32_t
   wait_failed();
   return false;
 }
+// The same by a whole warp.
+__device__ __forceinline__ bool warp_wait(const Params& P, uint32_t bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, wait_bar(P, bar, parity));
+}
 
 template <int TOKENS>
 struct Tile {
@@ -194,15 +198,15 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
 
   if (warp == 0) {
     while (issued < blocks) {
-      if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * (issued % S), (issued / S - 1) & 1)))) break;
+      if (!(ok = warp_wait(P, empty + 8 * (issued % S), (issued / S - 1) & 1))) break;
       load();
     }
   } else if (warp == 1) {
     for (int i = 0; i < blocks; ++i) {
       const int s = i % S;
-      if (!(ok = __all_sync(0xffffffffu, wait_bar(P, full + 8 * s, (i / S) & 1)))) break;
+      if (!(ok = warp_wait(P, full + 8 * s, (i / S) & 1))) break;
       // the products that read this buffer of scales are done
-      if (i >= 2 && !(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * ((i - 2) % S), ((i - 2) / S) & 1)))) break;
+      if (i >= 2 && !(ok = warp_wait(P, empty + 8 * ((i - 2) % S), ((i - 2) / S) & 1))) break;
       tc_fence_after();
       fence_async_smem();  // the scales were written by ordinary copies
       const uint32_t at = ring + s * T::kStageBytes, scales = tmem + T::kScaleCol + i % 2 * 16;
@@ -228,7 +232,7 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
                                                     P.N - n0, kChannels, thread);
     const Scales<TOKENS, kScaleThreads> tokens(P.scale_a, int64_t(m0) * P.ldsa, P.ldsa, P.M - m0, TOKENS, thread);
     for (int i = 0; i < blocks; ++i) {
-      if (i >= S && !(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * (i % S), (i / S - 1) & 1)))) break;
+      if (i >= S && !(ok = warp_wait(P, empty + 8 * (i % S), (i / S - 1) & 1))) break;
       const uint32_t at = ring + i % S * T::kStageBytes + T::kCodes;
       channels.fetch(at, (first + i) * kScaleBytes, P.kscales);
       tokens.fetch(at + T::kScales, (first + i) * kScaleBytes, P.kscales);
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
     cp_async_wait_all();
   }
   __syncwarp();
-  ok = wait_bar(P, done, 0) && ok;
+  ok = warp_wait(P, done, 0) && ok;
   tc_fence_after();
   ok = !__syncthreads_or(!ok);
   if (!ok && warp == 0) {
@@ -307,85 +311,120 @@ constexpr int kScaleWarps = 4;
 constexpr int kPairThreads = 32 * (2 + 8 + kScaleWarps + 1);  // TMA, MMA, eight epilogue warps, scale warps, their messenger
 constexpr int kPairTokens = 192;
 constexpr int kPairCodes = (kChannels + kPairTokens / 2) * kKBytes;  // bytes of a stage
-constexpr int kPairStageBytes = kPairCodes + 3 * 1024;               // and the scales of 128 channels and 256 tokens
 constexpr int kPairStages = 6;
-constexpr int kPairSmem = kPairStages * kPairStageBytes + 1024;
+// Scales come by groups of four stages, 32 bytes of a row: eight words of 128 rows each, a little apart from one another so
+// that the words of a row, and rows 32 apart, are written to different banks.  (Stage by stage, eight bytes of a row, a
+// warp's copies touched four times as many lines: 138 us instead of 112 at 8192 x 8192 x 3584.)
+constexpr int kGroupStages = 4, kGroupWords = 2 * kGroupStages, kGroups = 3;
+constexpr int kWordBytes = 512 + 16, kSectionBytes = kGroupWords * kWordBytes;  // (a section: 128 rows)
+constexpr int kGroupBytes = 3 * kSectionBytes;                                  // channels, tokens, tokens from 128 on
+constexpr int kPairSmem = kPairStages * kPairCodes + kGroups * kGroupBytes + 1024;
 constexpr int kPairScaleCol = 2 * kPairTokens;
 constexpr int kPairBuffers = 5;
 static_assert(kPairScaleCol + 24 * kPairBuffers <= 512 && kPairBuffers < kPairStages, "TMEM, and barriers that tell a buffer's last use");
 
 // 32 channels (lanes) x 32 tokens (registers) to C: neighbouring lanes exchange halves until each has four consecutive
-// channels of one token, and eight lanes store a token's 64 or 128 bytes.  (Staging the chunk in shared memory cost twice
-// the shared-memory cycles and two barriers.)  `rows` tokens and `left` channels lie inside C.
+// channels of one token, and eight lanes store a token's 64 or 128 bytes.  (Staging the chunk in shared memory costs twice
+// the shared-memory cycles and two barriers.)  `rows` tokens and `left` channels lie inside C.  All exchanges come before
+// the first store, and whole chunks are stored without a look at their borders: with a branch between them each group of
+// four tokens waited for the one before.
 template <typename Out>
 __device__ __forceinline__ void store_chunk(const float (&f)[32], Out* out, int64_t ldc, int rows, int left, int step, int lane) {
   const bool one = lane & 1, two = lane & 2;
   const int col = lane & ~3;
-  out += int64_t(lane & 3) * ldc + col;
-  const bool vec = step >= int(4 * sizeof(Out)) && col + 4 <= left;
-  auto put = [&](int token, const Piece<Out, 4>& v) {
-    if (token >= rows) return;
-    if (vec) {
-      *reinterpret_cast<Piece<Out, 4>*>(out) = v;
-    } else {
+  Piece<Out, 4> v[8];  // [i]: token 4 i + lane % 4, channels col to col + 3
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (col + e < left) out[e] = v.e[e];
-    }
-  };
-#pragma unroll
-  for (int j = 0; j < 32; j += 4, out += 4 * ldc) {
-    uint32_t w[2 * sizeof(Out)];  // per pair of tokens: two channels of one
+  for (int i = 0; i < 8; ++i) {
+    const int j = 4 * i;
     if constexpr (sizeof(Out) == 2) {
+      uint32_t w[2];  // per pair of tokens: two channels of one
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float g[2] = {f[j + 2 * i], f[j + 2 * i + 1]};
+      for (int h = 0; h < 2; ++h) {
+        const float g[2] = {f[j + 2 * h], f[j + 2 * h + 1]};
         const Piece<Out, 2> p = pack<Out, 2>(g);
         uint32_t mine;
         memcpy(&mine, &p, 4);
         const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
-        w[i] = __byte_perm(mine, other, one ? 0x3276 : 0x5410);
+        w[h] = __byte_perm(mine, other, one ? 0x3276 : 0x5410);
       }
       const uint32_t other = __shfl_xor_sync(0xffffffffu, two ? w[0] : w[1], 2);
       const uint32_t o[2] = {two ? other : w[0], two ? w[1] : other};
-      Piece<Out, 4> v;
-      memcpy(&v, o, 8);
-      put(j + (lane & 3), v);
+      memcpy(&v[i], o, 8);
     } else {
+      float w[4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float a = f[j + 2 * i], b = f[j + 2 * i + 1];
+      for (int h = 0; h < 2; ++h) {
+        const float a = f[j + 2 * h], b = f[j + 2 * h + 1];
         const float other = __shfl_xor_sync(0xffffffffu, one ? a : b, 1);
-        w[2 * i] = __float_as_uint(one ? other : a);
-        w[2 * i + 1] = __float_as_uint(one ? b : other);
+        w[2 * h] = one ? other : a;
+        w[2 * h + 1] = one ? b : other;
       }
-      uint32_t o[4];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, two ? w[e] : w[2 + e], 2);
-        o[e] = two ? other : w[e];
-        o[2 + e] = two ? w[2 + e] : other;
+        const float other = __shfl_xor_sync(0xffffffffu, two ? w[e] : w[2 + e], 2);
+        v[i].e[e] = two ? other : w[e];
+        v[i].e[2 + e] = two ? w[2 + e] : other;
       }
-      Piece<Out, 4> v;
-      memcpy(&v, o, 16);
-      put(j + (lane & 3), v);
+    }
+  }
+  out += int64_t(lane & 3) * ldc + col;
+  const bool wide = step >= int(4 * sizeof(Out));
+  if (wide && rows >= 32 && left >= 32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<Piece<Out, 4>*>(out + 4 * i * ldc) = v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (4 * i + (lane & 3) >= rows) continue;
+      Out* const at = out + 4 * i * ldc;
+      if (wide && col + 4 <= left) {
+        *reinterpret_cast<Piece<Out, 4>*>(at) = v[i];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < left) at[e] = v[i].e[e];
+      }
     }
   }
 }
+
+// What a thread fetches of a section: word lane % 8 of rows lane / 8 * 32 + warp + 4 k, k = 0 to 7, those below `rows`.
+struct Section {
+  const uint8_t* from;
+  int64_t step;
+  int count;
+  __device__ __forceinline__ Section(const uint8_t* first_row, int64_t ld, int rows, int warp, int lane) {
+    const int r = lane / 8 * 32 + warp;
+    from = first_row + r * ld + lane % 8 * 4;
+    step = 4 * ld;
+    count = max(0, min(8, (rows - r + 3) / 4));
+  }
+  // The group's words, from byte `at` of the rows on; zeros (a scale that nothing is multiplied with) for what is not there.
+  __device__ __forceinline__ void fetch(uint32_t smem, int at, int row_bytes, const uint8_t* somewhere, int warp, int lane) const {
+    const int left = row_bytes - at - lane % 8 * 4, n = left > 0 ? count : 0;
+    const uint32_t to = smem + lane % 8 * kWordBytes + warp * 16 + lane / 8 * 4;
+    const uint8_t* p = from + at;
+#pragma unroll
+    for (int k = 0; k < 8; ++k, p += step)
+      cp_async4(to + k * 64, k < n ? p : somewhere, k < n ? uint32_t(min(left, 4)) : 0u);
+  }
+};
 
 template <typename Out>
 __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const __grid_constant__ Maps maps,
                                                                          const __grid_constant__ Params P) {
   constexpr int S = kPairStages;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[3 * S + 5];
+  __shared__ __align__(8) uint64_t bars[2 * S + 2 * kGroups + 5];
   __shared__ uint32_t tmem_slot;
+  __shared__ int tile_columns[8];
   __shared__ PairGroups groups;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int rank = int(cluster_ctarank());
   const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * S, tfull = full + 16 * S, tempty = tfull + 16,
-                 drain = tempty + 16, scaled = drain + 8;
+                 drain = tempty + 16, scaled = drain + 8, sempty = scaled + 8 * kGroups;
+  const uint32_t scale_ring = ring + S * kPairCodes;
 
   if (threadIdx.x == 0) {
     tma_prefetch_map(&maps.a);
@@ -393,7 +432,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
     for (int s = 0; s < S; ++s) {
       mbar_init(full + 8 * s, 1 + 2);  // the codes, both CTAs' scales
       mbar_init(empty + 8 * s, 1);
+    }
+    for (int s = 0; s < kGroups; ++s) {
       mbar_init(scaled + 8 * s, 32 * kScaleWarps);
+      mbar_init(sempty + 8 * s, 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(tfull + 8 * a, 1);
@@ -427,8 +469,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
       const PairTile w = walk.at(t);
       const int n0 = w.n0 + rank * kChannels, m0 = w.m0 + rank * ((w.rows + 31) / 32 * 16);
       for (int b = 0; b < blocks; ++b) {
-        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * stage, phase ^ 1)))) break;
-        const uint32_t at = ring + stage * kPairStageBytes, bar = map_to_cta(full + 8 * stage, 0);
+        if (!(ok = warp_wait(P, empty + 8 * stage, phase ^ 1))) break;
+        const uint32_t at = ring + stage * kPairCodes, bar = map_to_cta(full + 8 * stage, 0);
         if (!(t == 0 && b == P.withhold) && elect_one()) {
           if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * bytes);
           tma_load_3d_pair(at, &maps.b, b * kKBytes, n0, w.g, bar);
@@ -444,7 +486,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
     // barriers.
     if (ok && in_flight > 0) {
       const int last = stage > 0 ? stage - 1 : S - 1;
-      ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * last, stage > 0 ? phase : phase ^ 1));
+      ok = warp_wait(P, empty + 8 * last, stage > 0 ? phase : phase ^ 1);
     }
     for (int i = 0; !ok && rank == 0 && i < in_flight; ++i) {
       if (--stage < 0) stage = S - 1, phase ^= 1;
@@ -455,43 +497,57 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
       // (from uniform registers, where the instructions want their addresses and descriptors)
       const uint32_t base = uniform(tmem);
       const int tiles = int(uniform(uint32_t(total)));
-      int stage = 0, acc = 0;
+      int stage = 0, acc = 0, turn = 0, group = 0;
       uint32_t phase = 0, acc_phase = 0, buffer = 0;
-      bool ok = true, there = false;
-      int rows = pair < tiles ? walk.at(pair).rows : 0, next_rows = 0;
-      for (int t = pair; ok && t < tiles; t += pairs, rows = next_rows) {
-        const int columns = int(uniform(uint32_t((rows + 31) / 32 * 32)));
-        const uint32_t idesc[2] = {instr_desc_mxf4(columns, kPairChannels, 0), instr_desc_mxf4(columns, kPairChannels, 1)};
-        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, tempty + 8 * acc, acc_phase ^ 1)))) break;
-        tc_fence_after();
+      bool ok = true, there[2] = {false, false};
+      for (int t = pair; ok && t < tiles; t += pairs, ++turn) {
+        if (!(ok = warp_wait(P, tempty + 8 * acc, acc_phase ^ 1))) break;
         const uint32_t d = base + acc * kPairTokens;
-        for (int b = 0; b < blocks; ++b) {
-          if (!(ok = __all_sync(0xffffffffu, there || wait_bar(P, full + 8 * stage, phase)))) break;
-          // (a look at the next block's barrier takes as long as the issue of these products: both at once)
-          there = mbar_test(full + 8 * (stage + 1 < S ? stage + 1 : 0), stage + 1 < S ? phase : phase ^ 1);
+        int columns = 0;
+        // two blocks at a time: what a turn costs beside the products is paid half as often (one: 671 cycles a block of
+        // 8192 x 8192 x 3584, of which the products are 384)
+        for (int b = 0; b < blocks; b += 2) {
+          const bool two = b + 1 < blocks, last = b + 2 >= blocks, group_ends = last || b % kGroupStages == kGroupStages - 2;
+          const int next = stage + 1 < S ? stage + 1 : 0, after = next + 1 < S ? next + 1 : 0;
+          const uint32_t next_phase = stage + 1 < S ? phase : phase ^ 1, after_phase = next + 1 < S ? next_phase : next_phase ^ 1;
+          ok = (there[0] || wait_bar(P, full + 8 * stage, phase)) && (!two || there[1] || wait_bar(P, full + 8 * next, next_phase));
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          if (b == 0) columns = int(uniform(uint32_t(tile_columns[turn % 8])));
+          const uint32_t idesc[2] = {instr_desc_mxf4(columns, kPairChannels, 0), instr_desc_mxf4(columns, kPairChannels, 1)};
+          // (a look at the next blocks' barriers takes as long as the issue of these products: both at once)
+          const int third = after + 1 < S ? after + 1 : 0;
+          there[0] = mbar_test(full + 8 * (two ? after : next), two ? after_phase : next_phase);
+          there[1] = mbar_test(full + 8 * (two ? third : after), two && after + 1 == S ? after_phase ^ 1 : after_phase);
           tc_fence_after();
-          const uint32_t at = ring + stage * kPairStageBytes, scales = base + kPairScaleCol + buffer * 24;
-          const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
-          const uint64_t ds = smem_desc_scales(at + kPairCodes);
-          if (elect_one()) {
+          auto products = [&](int s, uint32_t buf, int word, bool first) {
+            const uint32_t at = ring + s * kPairCodes, scales = base + kPairScaleCol + buf * 24;
+            const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + kChannels * kKBytes);
+            const uint64_t ds = smem_desc_scales(scale_ring + group * kGroupBytes + word * kWordBytes);
             // channels: two words of K; tokens: two words of the first 128, of the others
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-              tmem_copy_scales_pair(scales + 4 * w, ds + w * (512 >> 4));
-              tmem_copy_scales_pair(scales + 8 + 8 * w, ds + ((1024 + 512 * w) >> 4));
-              if (columns > 128) tmem_copy_scales_pair(scales + 12 + 8 * w, ds + ((2048 + 512 * w) >> 4));
+              tmem_copy_scales_pair(scales + 4 * w, ds + ((w * kWordBytes) >> 4));
+              tmem_copy_scales_pair(scales + 8 + 8 * w, ds + ((kSectionBytes + w * kWordBytes) >> 4));
+              if (columns > 128) tmem_copy_scales_pair(scales + 12 + 8 * w, ds + ((2 * kSectionBytes + w * kWordBytes) >> 4));
             }
 #pragma unroll
             for (int k = 0; k < kKBytes / 32; ++k)
               umma_mxf4_pair(d, da + 2 * k, db + 2 * k, idesc[k % 2], scales + k / 2 * 4, scales + 8 + k / 2 * 8,
-                             b > 0 || k > 0);
-            tc_commit_pair(empty + 8 * stage);
-            if (b == blocks - 1) tc_commit_pair(tfull + 8 * acc);
+                             !first || k > 0);
+            tc_commit_pair(empty + 8 * s);
+          };
+          const uint32_t next_buffer = buffer + 1 < kPairBuffers ? buffer + 1 : 0;
+          if (elect_one()) {
+            products(stage, buffer, b % kGroupStages * 2, b == 0);
+            if (two) products(next, next_buffer, b % kGroupStages * 2 + 2, false);
+            if (group_ends) tc_commit_pair(sempty + 8 * group);
+            if (last) tc_commit_pair(tfull + 8 * acc);
           }
           __syncwarp();
-          if (++buffer == kPairBuffers) buffer = 0;
-          if (++stage == S) stage = 0, phase ^= 1;
-          if (b == 0 && t + pairs < tiles) next_rows = walk.at(t + pairs).rows;  // (while these products run)
+          buffer = !two ? next_buffer : next_buffer + 1 < kPairBuffers ? next_buffer + 1 : 0;
+          stage = two ? after : next;
+          phase = two ? after_phase : next_phase;
+          if (group_ends && ++group == kGroups) group = 0;
         }
         if ((acc ^= 1) == 0) acc_phase ^= 1;
       }
@@ -511,7 +567,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
       const PairTile w = walk.at(t);
       const int n0 = w.n0 + rank * kChannels + q * 32, n = n0 + lane;
       const float add = n < P.N && P.bias ? P.bias[int64_t(w.g) * P.N + n] : 0.0f;
-      if (!__all_sync(0xffffffffu, wait_bar(P, tfull + 8 * acc, acc_phase))) break;
+      if (!warp_wait(P, tfull + 8 * acc, acc_phase)) break;
       tc_fence_after();
       const int chunks = (w.rows + 31) / 32;
       const uint32_t sums = tmem + (uint32_t(q) << 21) + acc * kPairTokens;
@@ -542,47 +598,56 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
       if ((acc ^= 1) == 0) acc_phase ^= 1;
     }
   } else if (warp < 10 + kScaleWarps) {
-    // Scales of both operands, as many stages ahead as the ring holds: the copies arrive on their stage's barrier by
+    // Scales of both operands, as many groups ahead as there is room for: the copies arrive on their group's barrier by
     // themselves.
-    const int thread = int(threadIdx.x) - 320;
-    int stage = 0;
+    const int w4 = warp - 10;
+    int group = 0, used = 0;
     uint32_t phase = 0;
     bool ok = true;
     for (int t = pair; ok && t < total; t += pairs) {
       const PairTile w = walk.at(t);
-      const int n0 = w.n0 + rank * kChannels, columns = (w.rows + 31) / 32 * 32;
-      const Scales<kChannels, 32 * kScaleWarps> channels(P.scale_b, int64_t(w.g) * P.scale_stride + int64_t(n0) * P.ldsb, P.ldsb,
-                                                         P.N - n0, kChannels, thread);
-      const Scales<kPairTokens, 32 * kScaleWarps> tokens(P.scale_a, int64_t(w.m0) * P.ldsa, P.ldsa, P.M - w.m0, columns, thread);
-      for (int b = 0; b < blocks; ++b) {
-        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * stage, phase ^ 1)))) break;
-        const uint32_t at = ring + stage * kPairStageBytes + kPairCodes;
-        channels.fetch(at, b * kScaleBytes, P.kscales);
-        tokens.fetch(at + 1024, b * kScaleBytes, P.kscales);
-        cp_async_arrive(scaled + 8 * stage);
-        if (++stage == S) stage = 0, phase ^= 1;
+      const int n0 = w.n0 + rank * kChannels, tokens = min(P.M - w.m0, (w.rows + 31) / 32 * 32);
+      const uint8_t* const row = P.scale_a + int64_t(w.m0) * P.ldsa;
+      const Section b0(P.scale_b + int64_t(w.g) * P.scale_stride + int64_t(n0) * P.ldsb, P.ldsb, P.N - n0, w4, lane),
+          a0(row, P.ldsa, min(tokens, 128), w4, lane), a1(row + 128 * P.ldsa, P.ldsa, tokens - 128, w4, lane);
+      for (int at = 0; at < P.kscales; at += kGroupStages * kScaleBytes) {
+        if (!(ok = warp_wait(P, sempty + 8 * group, phase ^ 1))) break;
+        const uint32_t to = scale_ring + group * kGroupBytes;
+        b0.fetch(to, at, P.kscales, P.scale_b, w4, lane);
+        a0.fetch(to + kSectionBytes, at, P.kscales, P.scale_a, w4, lane);
+        if (tokens > 128) a1.fetch(to + 2 * kSectionBytes, at, P.kscales, P.scale_a, w4, lane);
+        cp_async_arrive(scaled + 8 * group);
+        used = 1;
+        if (++group == kGroups) group = 0, phase ^= 1;
       }
     }
     cp_async_wait_all();
+    // the last arrival that says that a group has been used has come
+    if (ok && used) wait_bar(P, sempty + 8 * (group > 0 ? group - 1 : kGroups - 1), group > 0 ? phase : phase ^ 1);
   } else {
     // The messenger tells rank 0, whose warp has both CTAs' scales copied to TMEM, that this CTA's of a stage are there and
     // that the buffer for them is free: the products that read it, five blocks ago, are done.  The fence makes the words,
     // written by ordinary copies, visible to the tensor core, which reads them in this CTA; by a thread that has copies of
     // its own under way it would wait for them.  So would an arrival that releases to the cluster: 225 us instead of 134
     // (8192 x 8192 x 3584).
-    int stage = 0, before = 0;  // before: blocks so far, kPairBuffers at most
-    uint32_t phase = 0;
+    // It also says how wide a tile is, so that rank 0's issuing warp need not walk.
+    int stage = 0, group = 0, turn = 0, before = 0;  // before: blocks so far, kPairBuffers at most
+    uint32_t phase = 0, group_phase = 0;
     bool ok = true;
-    for (int t = pair; ok && t < total; t += pairs) {
+    for (int t = pair; ok && t < total; t += pairs, ++turn) {
+      if (lane == 0) tile_columns[turn % 8] = (walk.at(t).rows + 31) / 32 * 32;
       for (int b = 0; b < blocks; ++b) {
-        if (!(ok = __all_sync(0xffffffffu, wait_bar(P, scaled + 8 * stage, phase)))) break;
+        if (b % kGroupStages == 0) {
+          if (!(ok = warp_wait(P, scaled + 8 * group, group_phase))) break;
+          if (++group == kGroups) group = 0, group_phase ^= 1;
+          fence_async_smem();
+        }
         if (before == kPairBuffers) {
           const int s = stage >= kPairBuffers ? stage - kPairBuffers : stage + S - kPairBuffers;
-          if (!(ok = __all_sync(0xffffffffu, wait_bar(P, empty + 8 * s, stage >= kPairBuffers ? phase : phase ^ 1)))) break;
+          if (!(ok = warp_wait(P, empty + 8 * s, stage >= kPairBuffers ? phase : phase ^ 1))) break;
         } else {
           ++before;
         }
-        fence_async_smem();
         if (lane == 0) mbar_arrive_there(map_to_cta(full + 8 * stage, 0));
         __syncwarp();
         if (++stage == S) stage = 0, phase ^= 1;
