@@ -19,100 +19,127 @@ struct Params {
   uint8_t* q;      // codes, two a byte
   uint8_t* scale;  // scale bytes
   int64_t rows, ldx, ldq, lds;
-  int cols, row_threads;
+  int cols;
 };
-
-// Eight elements of a row of `cols`, zeros behind its end.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int left, float (&f)[8]) {
-  if (VEC && left >= 8) {
-    constexpr int V = 16 / sizeof(T);
-#pragma unroll
-    for (int i = 0; i < 8 / V; ++i) {
-      float g[V];
-      unpack<T, V>(reinterpret_cast<const Piece<T, V>*>(p)[i], g);
-#pragma unroll
-      for (int e = 0; e < V; ++e) f[i * V + e] = g[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = e < left ? Elem<T>::up(p[e]) : 0.0f;
-  }
-}
 
 // Two values as codes, the first in the low half: to the nearest, ties to the even code, the largest where above it.
 __device__ __forceinline__ uint32_t codes2(float a, float b) {
   return uint32_t(__nv_cvt_float2_to_fp4x2(make_float2(a, b), __NV_E2M1, cudaRoundNearest));
 }
 
-// Four lanes have a block: its largest magnitude's exponent, two less, is the scale's (6 = 1.5 * 2^2 is the largest
-// code).  The product with the inverse power of two is exact as far as the rounding to a code can see.
-template <typename T, int P, bool VEC>
+// Sixteen elements of a row, as they lie in memory where they are whole and aligned, zeros behind the row's end.
+template <typename T, bool WHOLE>
+struct Half {
+  static constexpr int V = 16 / sizeof(T), N = 16 / V;
+  Piece<T, V> v[N];
+  __device__ __forceinline__ void load(const T* p, int left) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (WHOLE) {
+        v[i] = left > i * V ? reinterpret_cast<const Piece<T, V>*>(p)[i] : Piece<T, V>{};
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[i].e[e] = i * V + e < left ? p[i * V + e] : Elem<T>::down(0.0f);
+      }
+    }
+  }
+  __device__ __forceinline__ uint32_t top() const {  // fp32 bits of the largest magnitude (infinity or above: not finite)
+    if constexpr (sizeof(T) == 2) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        uint32_t w[4];
+        memcpy(w, &v[i], 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __vmaxu2(m, w[j] & 0x7fff7fffu);
+      }
+      const uint16_t h = uint16_t(max(m & 0xffffu, m >> 16));
+      T t;
+      memcpy(&t, &h, 2);
+      return __float_as_uint(Elem<T>::up(t));
+    } else {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) m = max(m, __float_as_uint(v[i].e[e]) & 0x7fffffffu);
+      return m;
+    }
+  }
+  __device__ __forceinline__ uint2 codes(float up) const {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float f[V];
+      unpack<T, V>(v[i], f);
+#pragma unroll
+      for (int e = 0; e < V; e += 2) w[(i * V + e) / 8] |= codes2(f[e] * up, f[e + 1] * up) << (4 * ((i * V + e) % 8));
+    }
+    return make_uint2(w[0], w[1]);
+  }
+};
+
+// Two lanes have a block: its largest magnitude's exponent, two less, is the scale's (6 = 1.5 * 2^2 is the largest code).
+// The product with the inverse power of two is exact as far as the rounding to a code can see.
+template <typename T, int P, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
-  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
+  const int lane = int(threadIdx.x), width = int(blockDim.x);
+  const int64_t row = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
   const bool there = row < a.rows;
   const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
   uint8_t* const q = a.q + row * a.ldq;
   uint8_t* const scale = a.scale + row * a.lds;
-  const int step = 8 * P * a.row_threads, cols = there ? a.cols : 0;
+  const int step = 16 * P * width, cols = there ? a.cols : 0;
   // (whole warps go through the loop together: they vote on the blocks' scales)
   for (int64_t base = int64_t(blockIdx.y) * step; base < a.cols; base += int64_t(gridDim.y) * step) {
     const int c0 = int(base);
-    float f[P][8];
+    Half<T, WHOLE> h[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = c0 + 8 * (i * a.row_threads + lane);
-      load8<T, VEC>(x + at, max(cols - at, 0), f[i]);
+      const int at = c0 + 16 * (i * width + lane);
+      h[i].load(x + at, cols - at);
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = c0 + 8 * (i * a.row_threads + lane);
-      uint32_t top = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7fffffffu);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2)) >> 23;
+      const int at = c0 + 16 * (i * width + lane);
+      uint32_t top = h[i].top();
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1)) >> 23;
       if (at >= cols) continue;
       const bool fine = top < 255;
       const uint32_t byte = fine ? (top > 2 ? top - 2 : 0) : 255;
-      const float up = __uint_as_float((254 - byte) << 23);
-      uint32_t w = 0;
-      if (fine) {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) w |= codes2(f[i][e] * up, f[i][e + 1] * up) << (4 * e);
-      }
+      uint2 w = h[i].codes(__uint_as_float((254 - byte) << 23));
+      if (!fine) w = make_uint2(0, 0);
       if (at % kBlock == 0) scale[at / kBlock] = uint8_t(byte);
-      if (VEC && at + 8 <= a.cols) {
-        *reinterpret_cast<uint32_t*>(q + at / 2) = w;
+      if (WHOLE && at + 16 <= cols) {
+        *reinterpret_cast<uint2*>(q + at / 2) = w;
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2)
-          if (at + e < a.cols) q[(at + e) / 2] = uint8_t(w >> (4 * e));
+        for (int e = 0; e < 16; e += 2)
+          if (at + e < cols) q[(at + e) / 2] = uint8_t((e < 8 ? w.x : w.y) >> (4 * (e % 8)));
       }
     }
   }
 }
 
-template <typename T, int P, bool VEC>
+template <typename T, int P, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) {
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
-  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
+  const int lane = int(threadIdx.x), width = int(blockDim.x);
+  const int64_t row = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
   if (row >= a.rows) return;
   T* const x = static_cast<T*>(a.x) + row * a.ldx;
   const uint8_t* const q = a.q + row * a.ldq;
   const uint8_t* const scale = a.scale + row * a.lds;
-  const int step = 8 * P * a.row_threads;
+  const int step = 8 * P * width;
   for (int64_t base = int64_t(blockIdx.y) * step; base < a.cols; base += int64_t(gridDim.y) * step) {
     const int c0 = int(base);
     uint32_t w[P], byte[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = c0 + 8 * (i * a.row_threads + lane);
+      const int at = c0 + 8 * (i * width + lane);
       w[i] = byte[i] = 0;
       if (at < a.cols) {
         byte[i] = scale[at / kBlock];
-        if (VEC && at + 8 <= a.cols) {
+        if constexpr (WHOLE) {
           w[i] = *reinterpret_cast<const uint32_t*>(q + at / 2);
         } else {
 #pragma unroll
@@ -123,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) 
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = c0 + 8 * (i * a.row_threads + lane);
+      const int at = c0 + 8 * (i * width + lane);
       if (at >= a.cols) continue;
       // 2^(byte-127); 2^-127 is half of the least normal number, 255 stands for NaN
       const float s = __uint_as_float(byte[i] == 255 ? 0x7fffffffu : byte[i] ? byte[i] << 23 : 0x00400000u);
@@ -135,7 +162,7 @@ __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) 
         f[e] = d.x * s;
         f[e + 1] = d.y * s;
       }
-      if (VEC && at + 8 <= a.cols) {
+      if constexpr (WHOLE) {
         constexpr int V = 16 / sizeof(T);
 #pragma unroll
         for (int j = 0; j < 8 / V; ++j) {
@@ -153,26 +180,40 @@ __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) 
   }
 }
 
-template <typename T, int P>
-int run_by(Params a, bool back, bool vec, cudaStream_t stream) {
-  const int64_t groups = (int64_t(a.cols) + 7) / 8;
-  // whole warps of a row's threads where a row has that much
-  a.row_threads = int(std::min<int64_t>(kThreads, (groups + P * 32 - 1) / (P * 32) * 32));
-  while (a.row_threads > 4 && a.row_threads / 2 * P >= groups) a.row_threads /= 2;
-  const int per_cta = kThreads / a.row_threads;
-  const int64_t chunks = (groups + P * a.row_threads - 1) / (P * a.row_threads);
-  const dim3 grid(unsigned((a.rows + per_cta - 1) / per_cta), unsigned(std::min<int64_t>(chunks, 65535)));
-  auto kernel = back ? (vec ? dequant_mxf4_kernel<T, P, true> : dequant_mxf4_kernel<T, P, false>)
-                     : (vec ? quant_mxf4_kernel<T, P, true> : quant_mxf4_kernel<T, P, false>);
-  kernel<<<grid, per_cta * a.row_threads, 0, stream>>>(a);
-  return launched(cudaSuccess);
+// Threads of a row and rows of a CTA: whole warps of a row's threads where a row has that many pieces.
+template <int P>
+dim3 shape(int64_t pieces, int least) {
+  int width = int(std::min<int64_t>(kThreads, (pieces + P * 32 - 1) / (P * 32) * 32));
+  while (width > least && width / 2 * P >= pieces) width /= 2;
+  return dim3(unsigned(width), unsigned(kThreads / width));
+}
+dim3 grid_of(const Params& a, const dim3& block, int64_t per_chunk) {
+  const int64_t chunks = (a.cols + per_chunk - 1) / per_chunk;
+  return dim3(unsigned((a.rows + block.y - 1) / block.y), unsigned(std::min<int64_t>(chunks, 65535)));
 }
 
 template <typename T>
 int run(const Params& a, bool back, cudaStream_t stream) {
-  const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.q, a.ldq, 1, 4);
-  // little work: one group a thread, for the latency
-  return a.rows * int64_t(a.cols) < (1 << 20) ? run_by<T, 1>(a, back, vec, stream) : run_by<T, 4>(a, back, vec, stream);
+  // little work: one piece a thread, for the latency
+  const bool little = a.rows * int64_t(a.cols) < (1 << 20), aligned = aligned_rows(a.x, a.ldx, sizeof(T));
+  if (back) {
+    // groups of eight elements, all whole and on 16 bytes' (codes: 4 bytes') boundaries
+    const bool whole = a.cols % 8 == 0 && aligned && aligned_rows(a.q, a.ldq, 1, 4);
+    const int64_t groups = (int64_t(a.cols) + 7) / 8;
+    const dim3 block = little ? shape<1>(groups, 4) : shape<4>(groups, 4);
+    auto kernel = little ? (whole ? dequant_mxf4_kernel<T, 1, true> : dequant_mxf4_kernel<T, 1, false>)
+                         : (whole ? dequant_mxf4_kernel<T, 4, true> : dequant_mxf4_kernel<T, 4, false>);
+    kernel<<<grid_of(a, block, int64_t(little ? 8 : 32) * block.x), block, 0, stream>>>(a);
+  } else {
+    // pieces of sixteen elements, made of whole words of 16 bytes; codes on 8 bytes' boundaries
+    const bool whole = a.cols % (16 / int(sizeof(T))) == 0 && aligned && aligned_rows(a.q, a.ldq, 1, 8);
+    const int64_t halves = (int64_t(a.cols) + 15) / 16;
+    const dim3 block = little ? shape<1>(halves, 2) : shape<2>(halves, 2);
+    auto kernel = little ? (whole ? quant_mxf4_kernel<T, 1, true> : quant_mxf4_kernel<T, 1, false>)
+                         : (whole ? quant_mxf4_kernel<T, 2, true> : quant_mxf4_kernel<T, 2, false>);
+    kernel<<<grid_of(a, block, int64_t(little ? 16 : 32) * block.x), block, 0, stream>>>(a);
+  }
+  return launched(cudaSuccess);
 }
 
 int convert(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* q, int64_t ldq,

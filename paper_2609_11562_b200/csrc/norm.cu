@@ -5,6 +5,7 @@
 #include <cstring>
 
 #include "ops_common.cuh"
+#include "sm100.cuh"
 
 namespace entwine {
 namespace {
@@ -173,72 +174,77 @@ struct DropParams {
   const void* residual;
   void* out;
   int64_t rows, ldx, ldr, ldo;
-  int cols, row_threads;
+  int cols;
   Dropout d;
 };
 
 constexpr int kDropThreads = 256;
 
-// P groups of eight elements a thread; a CTA takes as many rows as fit.
+// P groups of eight elements a thread; a CTA (threads of a row x rows) goes from rows to rows.  16384 x 4096 bf16: XXDROP.
+// The generator takes 18 us of that (its wide multiplications issue at a quarter of the rate), so everything else has to be
+// short: set-up is paid once a thread, and whole groups have no element-wise alternative beside them.
 template <typename T, int P, bool VEC>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams a) {
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
-  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
-  if (row >= a.rows) return;
+  const int lane = int(threadIdx.x), width = int(blockDim.x);
   const Stream rng(a.d.rng);
-  const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
-  const T* const r = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
-  T* const out = static_cast<T*>(a.out) + row * a.ldo;
-  const uint32_t number = a.d.row0 + uint32_t(row);
-  const int full = a.cols / kGroup, step = P * a.row_threads;
-  for (int g0 = int(blockIdx.y) * step + lane; g0 < full; g0 += int(gridDim.y) * step) {
-    Raw<T> v[P], res[P];
+  const int full = a.cols / kGroup, step = P * width;
+  const int64_t stride = int64_t(gridDim.x) * blockDim.y;
+  for (int64_t row = int64_t(blockIdx.x) * blockDim.y + threadIdx.y; row < a.rows; row += stride) {
+    const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* const r = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
+    T* const out = static_cast<T*>(a.out) + row * a.ldo;
+    const uint32_t number = a.d.row0 + uint32_t(row);
+    for (int g0 = int(blockIdx.y) * step + lane; g0 < full; g0 += int(gridDim.y) * step) {
+      Raw<T> v[P], res[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int g = g0 + i * a.row_threads;
-      if (g < full) {
-        v[i].template load<VEC>(x + int64_t(g) * kGroup);
-        if (r) res[i].template load<VEC>(r + int64_t(g) * kGroup);
-      }
-    }
-    uint32_t c[P][4];
-    rng.words<P>(uint32_t(g0), uint32_t(a.row_threads), number, c);
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int g = g0 + i * a.row_threads;
-      if (g < full) {
-        float f[8];
-        v[i].get(f);
-        drop8(c[i], a.d, f);
-        if (r) {
-          float h[8];
-          res[i].get(h);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] += h[e];
+      for (int i = 0; i < P; ++i) {
+        const int g = g0 + i * width;
+        if (g < full) {
+          v[i].template load<VEC>(x + int64_t(g) * kGroup);
+          if (r) res[i].template load<VEC>(r + int64_t(g) * kGroup);
         }
-        store8<T, VEC>(out + int64_t(g) * kGroup, f);
+      }
+      uint32_t c[P][4];
+      rng.words<P>(uint32_t(g0), uint32_t(width), number, c);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const int g = g0 + i * width;
+        if (g < full) {
+          float f[8];
+          v[i].get(f);
+          drop8(c[i], a.d, f);
+          if (r) {
+            float h[8];
+            res[i].get(h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] += h[e];
+          }
+          store8<T, VEC>(out + int64_t(g) * kGroup, f);
+        }
       }
     }
-  }
-  const int col = full * kGroup + lane;
-  if (blockIdx.y == 0 && lane < kGroup && col < a.cols) {
-    float f = drop1(rng, a.d, number, uint32_t(col), Elem<T>::up(x[col]));
-    if (r) f += Elem<T>::up(r[col]);
-    out[col] = Elem<T>::down(f);
+    const int col = full * kGroup + lane;
+    if (blockIdx.y == 0 && lane < kGroup && col < a.cols) {
+      float f = drop1(rng, a.d, number, uint32_t(col), Elem<T>::up(x[col]));
+      if (r) f += Elem<T>::up(r[col]);
+      out[col] = Elem<T>::down(f);
+    }
   }
 }
 
 template <typename T, int P>
-int run_dropout_by(DropParams a, bool vec, cudaStream_t stream) {
+int run_dropout_by(const DropParams& a, bool vec, cudaStream_t stream) {
   const int64_t full = std::max(1, a.cols / kGroup);
   // whole warps of a row's threads where a row has that much
-  a.row_threads = int(std::min<int64_t>(kDropThreads, (full + 31) / 32 * 32 < 32 * P ? 32 : (full + P * 32 - 1) / (P * 32) * 32));
-  while (a.row_threads > 8 && a.row_threads / 2 * P >= full) a.row_threads /= 2;
-  const int per_cta = kDropThreads / a.row_threads;
-  const int64_t chunks = (full + P * a.row_threads - 1) / (P * a.row_threads);
-  const dim3 grid(unsigned((a.rows + per_cta - 1) / per_cta), unsigned(std::min<int64_t>(chunks, 65535)));
+  int width = int(std::min<int64_t>(kDropThreads, (full + P * 32 - 1) / (P * 32) * 32));
+  while (width > 8 && width / 2 * P >= full) width /= 2;
+  const int high = kDropThreads / width;
+  const int64_t chunks = std::min<int64_t>((full + P * width - 1) / (P * width), 1024), bands = (a.rows + high - 1) / high;
+  // a few rows for every thread where there are many
+  const int64_t most = std::max<int64_t>(1, int64_t(sm_count()) * 32 / chunks);
+  const dim3 grid(unsigned(std::min(bands, most)), unsigned(chunks));
   auto kernel = vec ? dropout_kernel<T, P, true> : dropout_kernel<T, P, false>;
-  kernel<<<grid, per_cta * a.row_threads, 0, stream>>>(a);
+  kernel<<<grid, dim3(width, high), 0, stream>>>(a);
   return launched(cudaSuccess);
 }
 
@@ -263,32 +269,33 @@ struct NormParams {
   float* mean;
   float* rstd;
   int64_t rows, ldx, ldr, ldh, ldo;
-  int cols, row_threads, wide;
+  int cols, wide;
   float eps;
   Dropout d;
 };
 
-// Sum over the threads of a row (row_threads of them, whole warps, from warp first_warp on).
+// Sum over the threads of a row: whole warps, threadIdx.x of them, from the CTA's warp first_warp on.
 __device__ __forceinline__ float row_sum(float v, float* part, int first_warp, int warps) {
   v = warp_sum(v);
   if (warps == 1) return v;
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) part[first_warp + threadIdx.x / 32] = v;
   __syncthreads();
-  v = 0.0f;
-  for (int w = 0; w < warps; ++w) v += part[first_warp + w];
-  return v;
+  return warp_sum(lane < warps ? part[first_warp + lane] : 0.0f);
 }
 
-// A row in registers: up to P groups a thread and one element of the last, incomplete group.  The mean first, then the
-// mean of the squared distances from it: no difference of large sums.
-template <typename T, int P, bool VEC, bool DROP>
+// A row in registers: P groups a thread, all of them whole and there (FULL), or up to P and one element of the last,
+// incomplete group.  The mean first, then the mean of the squared distances from it: no difference of large sums.  A CTA is
+// threads of a row x rows.
+template <typename T, int P, bool VEC, bool FULL, bool DROP>
 __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const NormParams a) {
   __shared__ float part[2][32];
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) - slot * a.row_threads;
-  const int64_t row = int64_t(blockIdx.x) * (blockDim.x / a.row_threads) + slot;
+  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x);
+  const int64_t row = int64_t(blockIdx.x) * blockDim.y + slot;
   const bool there = row < a.rows;
-  const int full = there ? a.cols / kGroup : 0, tail = full * kGroup + lane;
-  const bool has_tail = there && lane < kGroup && tail < a.cols;
+  const int full = !there ? 0 : FULL ? P * width : a.cols / kGroup, tail = full * kGroup + lane;
+  const bool has_tail = !FULL && there && lane < kGroup && tail < a.cols;
+  auto whole = [&](int i) { return FULL ? there : i * width + lane < full; };
   const uint32_t number = a.d.row0 + uint32_t(row);
   const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
   const T* const res = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
@@ -297,8 +304,8 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
   float last = 0.0f, sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const int g = i * a.row_threads + lane;
-    if (g < full) v[i].template load<VEC>(x + g * kGroup);
+    const int g = i * width + lane;
+    if (whole(i)) v[i].template load<VEC>(x + g * kGroup);
     else v[i].zero();
   }
   if (has_tail) last = Elem<T>::up(x[tail]);
@@ -307,16 +314,16 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
     if (res) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        const int g = i * a.row_threads + lane;
-        if (g < full) r[i].template load<VEC>(res + g * kGroup);
+        const int g = i * width + lane;
+        if (whole(i)) r[i].template load<VEC>(res + g * kGroup);
       }
     }
     uint32_t c[P][4];
     const Stream rng(DROP ? a.d.rng : nullptr);
-    if constexpr (DROP) rng.words<P>(uint32_t(lane), uint32_t(a.row_threads), number, c);
+    if constexpr (DROP) rng.words<P>(uint32_t(lane), uint32_t(width), number, c);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      if (i * a.row_threads + lane < full) {
+      if (whole(i)) {
         float f[8];
         v[i].get(f);
         if constexpr (DROP) drop8(c[i], a.d, f);
@@ -337,19 +344,19 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
   float h[P][8];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (hidden && i * a.row_threads + lane < full) v[i].template store<VEC>(hidden + (i * a.row_threads + lane) * kGroup);
+    if (hidden && whole(i)) v[i].template store<VEC>(hidden + (i * width + lane) * kGroup);
     v[i].get(h[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += h[i][e];
   }
   if (hidden && has_tail) hidden[tail] = Elem<T>::down(last);
   sum += last;
-  const int first_warp = slot * (a.row_threads / 32), warps = a.row_threads / 32;
+  const int warps = width / 32, first_warp = slot * warps;
   const float mean = row_sum(sum, part[0], first_warp, warps) / float(a.cols);
   float square = 0.0f;
 #pragma unroll
   for (int i = 0; i < P; ++i)
-    if (i * a.row_threads + lane < full) {
+    if (whole(i)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         h[i][e] -= mean;
@@ -370,8 +377,8 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
   T* const out = static_cast<T*>(a.out) + row * a.ldo;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const int g = i * a.row_threads + lane;
-    if (g < full) {
+    const int g = i * width + lane;
+    if (whole(i)) {
       float w[8], b[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       weight.template load<VEC>(g * kGroup, w);
       if (a.bias) bias.template load<VEC>(g * kGroup, b);
@@ -426,32 +433,37 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_rows_kernel(const Norm
 }
 
 template <typename T, bool DROP>
-auto pick_norm(int each, bool vec) {
-  if (!vec) return each == 1 ? norm_rows_kernel<T, 1, false, DROP> : each == 2 ? norm_rows_kernel<T, 2, false, DROP> : norm_rows_kernel<T, 4, false, DROP>;
-  return each == 1 ? norm_rows_kernel<T, 1, true, DROP> : each == 2 ? norm_rows_kernel<T, 2, true, DROP> : norm_rows_kernel<T, 4, true, DROP>;
+auto pick_norm(int each, bool vec, bool full) {
+  if (!vec) return norm_rows_kernel<T, 2, false, false, DROP>;
+  if (!full) return each == 4 ? norm_rows_kernel<T, 4, true, false, DROP> : norm_rows_kernel<T, 2, true, false, DROP>;
+  return each == 4   ? norm_rows_kernel<T, 4, true, true, DROP>
+         : each == 2 ? norm_rows_kernel<T, 2, true, true, DROP>
+                     : norm_rows_kernel<T, 1, true, true, DROP>;
 }
 
 template <typename T>
-int run_norm(NormParams a, cudaStream_t stream) {
+int run_norm(const NormParams& a, cudaStream_t stream) {
   auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
   const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.out, a.ldo, sizeof(T)) &&
                    (!a.residual || aligned_rows(a.residual, a.ldr, sizeof(T))) &&
                    (!a.hidden || aligned_rows(a.hidden, a.ldh, sizeof(T))) && aligned(a.weight) &&
                    (!a.bias || aligned(a.bias));
-  const int64_t groups = std::max(1, a.cols / kGroup);
-  if (groups > 4 * 512) {
+  const int groups = std::max(1, a.cols / kGroup);
+  if (groups > 2048) {
     norm_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
     return launched(cudaSuccess);
   }
-  // few rows: many threads with little each, for the latency
+  // Groups a thread: few rows, many threads with little each, for the latency; else four, or what divides a row evenly.
+  auto fits = [&](int p) { return vec && a.cols % kGroup == 0 && groups % (32 * p) == 0 && groups / p <= (p == 4 ? 512 : 1024); };
   const int most = a.rows < 512 ? 1 : a.rows < 2048 ? 2 : 4;
-  const int each = groups <= most * 512 ? most : groups <= 1024 ? 2 : 4;
-  const int64_t warps = (groups + each * 32 - 1) / (each * 32);
-  a.row_threads = int(warps * 32);
-  const int per_cta = std::max(1, 128 / a.row_threads), threads = per_cta * a.row_threads;
-  const unsigned grid = unsigned((a.rows + per_cta - 1) / per_cta);
-  auto kernel = a.d.rng ? pick_norm<T, true>(each, vec) : pick_norm<T, false>(each, vec);
-  kernel<<<grid, threads, 0, stream>>>(a);
+  int each = most;
+  while (each > 1 && !fits(each)) each /= 2;
+  const bool full = fits(each);
+  if (!full) each = vec && (most == 4 || groups > 1024) ? 4 : 2;
+  const int width = (groups + each * 32 - 1) / (each * 32) * 32, high = std::max(1, 128 / width);
+  const unsigned grid = unsigned((a.rows + high - 1) / high);
+  auto kernel = a.d.rng ? pick_norm<T, true>(each, vec, full) : pick_norm<T, false>(each, vec, full);
+  kernel<<<grid, dim3(width, high), 0, stream>>>(a);
   return launched(cudaSuccess);
 }
 
@@ -469,7 +481,7 @@ struct GradParams {
   void* dresidual;
   float* work;  // [parts][2][cols]: each part's sums over its rows, of the weight's gradient and the bias's
   int64_t rows, ldo, ldh, lddh, lddx, lddr;
-  int cols, row_threads, wide;
+  int cols, wide;
   Dropout d;
 };
 
@@ -482,6 +494,7 @@ struct GradPlan {
 
 constexpr int kGradGroups = 2;           // groups of eight columns a thread
 constexpr int kGradThreads = 512;        // at most
+constexpr int kGradHalf = 320;           // at most, where two CTAs share an SM
 constexpr int kStripRows = 64;           // rows of a part where the columns are summed by themselves
 
 GradPlan grad_plan(int64_t rows, int64_t cols) {
@@ -496,38 +509,41 @@ GradPlan grad_plan(int64_t rows, int64_t cols) {
   }
   g.row_threads = int((groups + kGradGroups * 32 - 1) / (kGradGroups * 32)) * 32;
   g.per_cta = std::max(1, 256 / g.row_threads);
-  const int resident = std::max(1, 512 / (g.row_threads * g.per_cta));
+  const int resident = g.row_threads <= kGradHalf ? 2 : 1;
   g.ctas = int(std::min<int64_t>((rows + g.per_cta - 1) / g.per_cta, int64_t(resident) * 148));
   g.ctas = std::max(1, g.ctas);
   return g;
 }
 
-// Two sums over the threads of a row.  `part` is one of two buffers in turn: one barrier a row.
+// Two sums over the threads of a row, of 16 warps at most: the halves of a warp take one each.  `part` is one of two buffers
+// in turn: one barrier a row.
 __device__ __forceinline__ float2 row_sum2(float2 v, float2* part, int first_warp, int warps) {
-  v.x = warp_sum(v.x);
-  v.y = warp_sum(v.y);
-  if (warps == 1) return v;
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = make_float2(0.0f, 0.0f);
-  for (int w = 0; w < warps; ++w) {
-    v.x += part[first_warp + w].x;
-    v.y += part[first_warp + w].y;
+  const int lane = threadIdx.x & 31;
+  const bool upper = lane & 16;
+  float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (warps > 1) {
+    if ((lane & 15) == 0) reinterpret_cast<float*>(part)[2 * (first_warp + threadIdx.x / 32) + (lane >> 4)] = s;
+    __syncthreads();
+    s = (lane & 15) < warps ? reinterpret_cast<const float*>(part)[2 * (first_warp + (lane & 15)) + (lane >> 4)] : 0.0f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   }
-  return v;
+  const float other = __shfl_xor_sync(0xffffffffu, s, 16);
+  return upper ? make_float2(other, s) : make_float2(s, other);
 }
 
 // With g = dout weight and n = (hidden - mean) rstd: dh = rstd (g - mean(g) - n mean(g n)) + dhidden.  A thread keeps its
-// columns from row to row, and with them their sums of dout n and dout.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const GradParams a) {
+// columns from row to row, and with them their sums of dout n and dout.  This form is for rows that start anywhere.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) norm_grad_anywhere_kernel(const GradParams a) {
   constexpr int P = kGradGroups;
   __shared__ float2 part[2][32];
-  const int slot = int(threadIdx.x) / a.row_threads, lane = int(threadIdx.x) % a.row_threads;
-  const int per_cta = int(blockDim.x) / a.row_threads;
+  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x), per_cta = int(blockDim.y);
   const int full = a.cols / kGroup, tail = full * kGroup + lane;
   const bool has_tail = lane < kGroup && tail < a.cols;
-  const int first_warp = slot * (a.row_threads / 32), warps = a.row_threads / 32;
+  const int warps = width / 32, first_warp = slot * warps;
   const Weights<T> weight{a.weight, a.wide != 0};
   const Stream rng(a.d.rng);
   const float per_col = 1.0f / float(a.cols);
@@ -543,18 +559,18 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const GradParam
     const float mean = there ? a.mean[row] : 0.0f, rstd = there ? a.rstd[row] : 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = i * a.row_threads + lane;
+      const int at = i * width + lane;
       if (there && at < full) {
-        load8<T, VEC>(dout + at * kGroup, g[i]);
-        load8<T, VEC>(hidden + at * kGroup, n[i]);
+        load8<T, false>(dout + at * kGroup, g[i]);
+        load8<T, false>(hidden + at * kGroup, n[i]);
       }
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = i * a.row_threads + lane;
+      const int at = i * width + lane;
       if (there && at < full) {
         float w[8];
-        weight.template load<VEC>(at * kGroup, w);
+        weight.template load<false>(at * kGroup, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           n[i][e] = (n[i][e] - mean) * rstd;
@@ -585,19 +601,19 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const GradParam
     const uint32_t number = a.d.row0 + uint32_t(row);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = i * a.row_threads + lane;
+      const int at = i * width + lane;
       if (at < full) {
         float f[8] = {};
-        if (dhidden) load8<T, VEC>(dhidden + at * kGroup, f);
+        if (dhidden) load8<T, false>(dhidden + at * kGroup, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, g[i][e] - s.x - n[i][e] * s.y, f[e]);
-        if (dresidual) store8<T, VEC>(dresidual + at * kGroup, f);
+        if (dresidual) store8<T, false>(dresidual + at * kGroup, f);
         if (a.d.rng) {
           uint32_t c[1][4];
           rng.words<1>(uint32_t(at), 0, number, c);
           drop8(c[0], a.d, f);
         }
-        store8<T, VEC>(dx + at * kGroup, f);
+        store8<T, false>(dx + at * kGroup, f);
       }
     }
     if (has_tail) {
@@ -610,7 +626,7 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const GradParam
   float* const sums = a.work + (int64_t(blockIdx.x) * per_cta + slot) * 2 * a.cols;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const int at = i * a.row_threads + lane;
+    const int at = i * width + lane;
     if (at < full) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -623,6 +639,168 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(const GradParam
     sums[tail] = dw_tail;
     sums[int64_t(a.cols) + tail] = db_tail;
   }
+}
+
+// The same for rows on 16-byte boundaries (FULL: whose groups are all whole and there).  Every thread copies its own pieces
+// of dout, hidden and dhidden ahead, into places of shared memory that no other thread looks at: D rows are under way or in
+// work, and the only barrier of a row is that of its two sums.  What the second half of a row needs is read again instead of
+// held in registers, the weights too: 96 registers have to do where two CTAs share an SM.
+template <typename T, int D, int THREADS, bool FULL>
+__global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_grad_kernel(const GradParams a) {
+  constexpr int P = kGradGroups, N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float2 part[2][32];
+  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x), per_cta = int(blockDim.y);
+  const int full = FULL ? P * width : a.cols / kGroup, tail = full * kGroup + lane;
+  const bool has_tail = !FULL && lane < kGroup && tail < a.cols;
+  const int warps = width / 32, first_warp = slot * warps;
+  const Weights<T> weight{a.weight, a.wide != 0};
+  const Stream rng(a.d.rng);
+  const float per_col = 1.0f / float(a.cols);
+  const int64_t stride = int64_t(gridDim.x) * per_cta;
+  int64_t row = int64_t(blockIdx.x) * per_cta + slot, ahead = row;
+  const T *dout = static_cast<const T*>(a.dout) + row * a.ldo + lane * kGroup,
+          *hidden = static_cast<const T*>(a.hidden) + row * a.ldh + lane * kGroup,
+          *dhidden = a.dhidden ? static_cast<const T*>(a.dhidden) + row * a.lddh + lane * kGroup : nullptr;
+  uint4* const mine = reinterpret_cast<uint4*>(ring) + slot * width + lane;
+  auto whole = [&](int i) { return FULL || i * width + lane < full; };
+  // the next row of this thread's to place d
+  auto fetch = [&](int d) {
+    if (ahead < a.rows) {
+      const uint32_t to = smem_u32(mine + d * kRow);
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        if (whole(i)) {
+#pragma unroll
+          for (int piece = 0; piece < N; ++piece) {
+            const int at = i * width * kGroup + piece * V;
+            cp_async16(to + ((0 * P + i) * N + piece) * THREADS * 16, dout + at);
+            cp_async16(to + ((1 * P + i) * N + piece) * THREADS * 16, hidden + at);
+            if (a.dhidden) cp_async16(to + ((2 * P + i) * N + piece) * THREADS * 16, dhidden + at);
+          }
+        }
+    }
+    cp_async_commit();
+    ahead += stride;
+    dout += stride * a.ldo;
+    hidden += stride * a.ldh;
+    if (a.dhidden) dhidden += stride * a.lddh;
+  };
+  auto get = [&](const uint4* from, int what, int i, float (&f)[8]) {
+    Raw<T> r;
+#pragma unroll
+    for (int piece = 0; piece < N; ++piece) {
+      const uint4 w = from[((what * P + i) * N + piece) * THREADS];
+      memcpy(&r.v[piece], &w, 16);
+    }
+    r.get(f);
+  };
+  float dw[P][8] = {}, db[P][8] = {}, dw_tail = 0.0f, db_tail = 0.0f;
+  int turn = 0, d = 0;
+#pragma unroll
+  for (int i = 0; i < D - 1; ++i) fetch(i);
+  float mean = 0.0f, rstd = 0.0f, next_mean = row < a.rows ? a.mean[row] : 0.0f, next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
+  for (int64_t row0 = int64_t(blockIdx.x) * per_cta; row0 < a.rows; row0 += stride, row += stride, turn ^= 1) {
+    const bool there = row < a.rows;
+    fetch(d + D - 1 < D ? d + D - 1 : d - 1);
+    mean = next_mean;
+    rstd = next_rstd;
+    if (row + stride < a.rows) {
+      next_mean = a.mean[row + stride];
+      next_rstd = a.rstd[row + stride];
+    }
+    cp_async_wait<D - 1>();
+    const uint4* const from = mine + d * kRow;
+    float2 s = make_float2(0.0f, 0.0f);
+    float g_tail = 0.0f, n_tail = 0.0f;
+    if (there) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        if (whole(i)) {
+          float g[8], h[8], w[8];
+          weight.template load<true>((i * width + lane) * kGroup, w);
+          get(from, 0, i, g);
+          get(from, 1, i, h);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float n = (h[e] - mean) * rstd;
+            dw[i][e] = fmaf(g[e], n, dw[i][e]);
+            db[i][e] += g[e];
+            g[e] *= w[e];
+            s.x += g[e];
+            s.y = fmaf(g[e], n, s.y);
+          }
+        }
+      }
+      if (has_tail) {
+        g_tail = Elem<T>::up(static_cast<const T*>(a.dout)[row * a.ldo + tail]);
+        n_tail = (Elem<T>::up(static_cast<const T*>(a.hidden)[row * a.ldh + tail]) - mean) * rstd;
+        dw_tail = fmaf(g_tail, n_tail, dw_tail);
+        db_tail += g_tail;
+        g_tail *= weight.one(tail);
+        s.x += g_tail;
+        s.y = fmaf(g_tail, n_tail, s.y);
+      }
+    }
+    s = row_sum2(s, part[turn], first_warp, warps);
+    s.x *= per_col;
+    s.y *= per_col;
+    if (there) {
+      T* const dresidual = a.dresidual ? static_cast<T*>(a.dresidual) + row * a.lddr : nullptr;
+      T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
+      const uint32_t number = a.d.row0 + uint32_t(row);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        if (whole(i)) {
+          const int g0 = i * width + lane;
+          float g[8], h[8], w[8], f[8] = {};
+          weight.template load<true>(g0 * kGroup, w);
+          get(from, 0, i, g);
+          get(from, 1, i, h);
+          if (a.dhidden) get(from, 2, i, f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, fmaf(g[e], w[e], -s.x) - (h[e] - mean) * rstd * s.y, f[e]);
+          if (dresidual) store8<T, true>(dresidual + g0 * kGroup, f);
+          if (a.d.rng) {
+            uint32_t c[1][4];
+            rng.words<1>(uint32_t(g0), 0, number, c);
+            drop8(c[0], a.d, f);
+          }
+          store8<T, true>(dx + g0 * kGroup, f);
+        }
+      }
+      if (has_tail) {
+        float f = fmaf(rstd, g_tail - s.x - n_tail * s.y,
+                       a.dhidden ? Elem<T>::up(static_cast<const T*>(a.dhidden)[row * a.lddh + tail]) : 0.0f);
+        if (dresidual) dresidual[tail] = Elem<T>::down(f);
+        if (a.d.rng) f = drop1(rng, a.d, number, uint32_t(tail), f);
+        dx[tail] = Elem<T>::down(f);
+      }
+    }
+    if (++d == D) d = 0;
+  }
+  cp_async_wait<0>();
+  float* const sums = a.work + (int64_t(blockIdx.x) * per_cta + slot) * 2 * a.cols;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (whole(i)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sums[(i * width + lane) * kGroup + e] = dw[i][e];
+        sums[int64_t(a.cols) + (i * width + lane) * kGroup + e] = db[i][e];
+      }
+    }
+  }
+  if (has_tail) {
+    sums[tail] = dw_tail;
+    sums[int64_t(a.cols) + tail] = db_tail;
+  }
+}
+
+template <typename T, int THREADS>
+auto pick_grad(int depth, bool full) {
+  if (depth == 3) return full ? norm_grad_kernel<T, 3, THREADS, true> : norm_grad_kernel<T, 3, THREADS, false>;
+  return full ? norm_grad_kernel<T, 2, THREADS, true> : norm_grad_kernel<T, 2, THREADS, false>;
 }
 
 // Rows too long for that: dx by a CTA that reads a row twice, ...
@@ -672,7 +850,7 @@ __global__ void __launch_bounds__(128) norm_grad_columns_kernel(const GradParams
   a.work[int64_t(part) * 2 * a.cols + a.cols + c] = db;
 }
 
-constexpr int kSumRows = 16;
+constexpr int kSumRows = 32;
 
 // The parts' sums added up, in their order: 32 columns a CTA.
 __global__ void __launch_bounds__(32 * kSumRows) norm_sum_kernel(const float* work, int64_t parts, int cols, float* dweight,
@@ -682,8 +860,10 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_sum_kernel(const float* wo
   const int64_t c = int64_t(blockIdx.x) * 32 + lane;
   const float* const in = work + int64_t(blockIdx.y) * cols + c;
   float v = 0.0f;
-  if (c < cols)
+  if (c < cols) {
+#pragma unroll 4
     for (int64_t i = y; i < parts; i += kSumRows) v += in[i * 2 * cols];
+  }
   sums[y][lane] = v;
   __syncthreads();
   if (y == 0 && c < cols) {
@@ -693,16 +873,27 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_sum_kernel(const float* wo
 }
 
 template <typename T>
-int run_grad(GradParams a, float* dweight, float* dbias, cudaStream_t stream) {
+int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t stream) {
   const GradPlan plan = grad_plan(a.rows, a.cols);
-  a.row_threads = plan.row_threads;
   auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
   if (plan.in_registers) {
     const bool vec = aligned_rows(a.dout, a.ldo, sizeof(T)) && aligned_rows(a.hidden, a.ldh, sizeof(T)) &&
                      aligned_rows(a.dx, a.lddx, sizeof(T)) && (!a.dhidden || aligned_rows(a.dhidden, a.lddh, sizeof(T))) &&
                      (!a.dresidual || aligned_rows(a.dresidual, a.lddr, sizeof(T))) && aligned(a.weight);
-    auto kernel = vec ? norm_grad_kernel<T, true> : norm_grad_kernel<T, false>;
-    kernel<<<unsigned(plan.ctas), plan.row_threads * plan.per_cta, 0, stream>>>(a);
+    const dim3 threads(plan.row_threads, plan.per_cta);
+    if (vec) {
+      // three rows where they fit (with two CTAs to an SM, or alone), else two
+      const bool half = plan.row_threads * plan.per_cta <= kGradHalf;
+      const bool full = a.cols == plan.row_threads * kGradGroups * kGroup;
+      const int row_bytes = (half ? kGradHalf : kGradThreads) * 3 * kGradGroups * kGroup * int(sizeof(T));
+      const int depth = row_bytes * 3 <= (half ? 112 : 224) * 1024 ? 3 : 2;
+      auto kernel = half ? pick_grad<T, kGradHalf>(depth, full) : pick_grad<T, kGradThreads>(depth, full);
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, row_bytes * depth);
+      if (e != cudaSuccess) return launched(e);
+      kernel<<<unsigned(plan.ctas), threads, row_bytes * depth, stream>>>(a);
+    } else {
+      norm_grad_anywhere_kernel<T><<<unsigned(plan.ctas), threads, 0, stream>>>(a);
+    }
   } else {
     if (a.rows > 0) norm_grad_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
     const dim3 grid(unsigned((int64_t(a.cols) + 127) / 128), unsigned(plan.ctas));
