@@ -20,6 +20,7 @@ struct Params {
   uint8_t* scale;  // scale bytes
   int64_t rows, ldx, ldq, lds;
   int cols;
+  int q_wide;      // rows of codes start on 8-byte boundaries (4, on the way back)
 };
 
 // Two values as codes, the first in the low half: to the nearest, ties to the even code, the largest where above it.
@@ -27,20 +28,27 @@ __device__ __forceinline__ uint32_t codes2(float a, float b) {
   return uint32_t(__nv_cvt_float2_to_fp4x2(make_float2(a, b), __NV_E2M1, cudaRoundNearest));
 }
 
-// Sixteen elements of a row, as they lie in memory where they are whole and aligned, zeros behind the row's end.
+// Sixteen elements of a row, zeros behind the row's end: as they lie in memory where they are whole and aligned, else put
+// together from the aligned words around them, which are read inside the matrix only.
 template <typename T, bool WHOLE>
 struct Half {
   static constexpr int V = 16 / sizeof(T), N = 16 / V;
   Piece<T, V> v[N];
-  __device__ __forceinline__ void load(const T* p, int left) {
+  __device__ __forceinline__ void load(const T* p, int left, const Span& inside) {
+    if constexpr (WHOLE) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if constexpr (WHOLE) {
-        v[i] = left > i * V ? reinterpret_cast<const Piece<T, V>*>(p)[i] : Piece<T, V>{};
-      } else {
+      for (int i = 0; i < N; ++i) v[i] = left > i * V ? reinterpret_cast<const Piece<T, V>*>(p)[i] : Piece<T, V>{};
+    } else if (left >= 16 && !Anywhere<T>::alone(p, inside) && !Anywhere<T>::alone(p + (N - 1) * V, inside)) {
+      Anywhere<T> w[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i].fetch(p + i * V, true);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = w[i].get();
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) v[i].e[e] = i * V + e < left ? p[i * V + e] : Elem<T>::down(0.0f);
-      }
     }
   }
   __device__ __forceinline__ uint32_t top() const {  // fp32 bits of the largest magnitude (infinity or above: not finite)
@@ -90,6 +98,7 @@ __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
   uint8_t* const q = a.q + row * a.ldq;
   uint8_t* const scale = a.scale + row * a.lds;
   const int step = 16 * P * width, cols = there ? a.cols : 0;
+  const Span inside = span_of(static_cast<const T*>(a.x), a.rows, a.cols, a.ldx);
   // (whole warps go through the loop together: they vote on the blocks' scales)
   for (int64_t base = int64_t(blockIdx.y) * step; base < a.cols; base += int64_t(gridDim.y) * step) {
     const int c0 = int(base);
@@ -97,7 +106,7 @@ __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int at = c0 + 16 * (i * width + lane);
-      h[i].load(x + at, cols - at);
+      h[i].load(x + at, cols - at, inside);
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -110,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
       uint2 w = h[i].codes(__uint_as_float((254 - byte) << 23));
       if (!fine) w = make_uint2(0, 0);
       if (at % kBlock == 0) scale[at / kBlock] = uint8_t(byte);
-      if (WHOLE && at + 16 <= cols) {
+      if ((WHOLE || a.q_wide) && at + 16 <= cols) {
         *reinterpret_cast<uint2*>(q + at / 2) = w;
       } else {
 #pragma unroll
@@ -121,7 +130,17 @@ __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
   }
 }
 
-template <typename T, int P, bool WHOLE>
+// 2^(byte-127); 2^-127 is half of the least normal number, 255 stands for NaN.
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+  return __uint_as_float(byte == 255 ? 0x7fffffffu : byte ? byte << 23 : 0x00400000u);
+}
+__device__ __forceinline__ float2 values2(uint32_t codes) {
+  const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2(__nv_fp4x2_storage_t(codes), __NV_E2M1);
+  return __half22float2(__half2(h));
+}
+
+// Groups of eight values, all of them whole and aligned.
+template <typename T, int P>
 __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) {
   const int lane = int(threadIdx.x), width = int(blockDim.x);
   const int64_t row = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
@@ -139,7 +158,51 @@ __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) 
       w[i] = byte[i] = 0;
       if (at < a.cols) {
         byte[i] = scale[at / kBlock];
-        if constexpr (WHOLE) {
+        w[i] = *reinterpret_cast<const uint32_t*>(q + at / 2);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int at = c0 + 8 * (i * width + lane);
+      if (at >= a.cols) continue;
+      const float s = scale_of(byte[i]);
+      constexpr int V = 16 / sizeof(T);
+#pragma unroll
+      for (int j = 0; j < 8 / V; ++j) {
+        float g[V];
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const float2 d = values2((w[i] >> (4 * (j * V + e))) & 0xff);
+          g[e] = d.x * s;
+          g[e + 1] = d.y * s;
+        }
+        reinterpret_cast<Piece<T, V>*>(x + at)[j] = pack<T, V>(g);
+      }
+    }
+  }
+}
+
+// Rows that start anywhere: a warp has 256 columns at a time, and a lane stores eight of them 32 apart, so that its stores
+// lie beside its neighbours'.  Codes and scale of a column come from the lane that has read those of its group of eight.
+template <typename T, int P>
+__global__ void __launch_bounds__(kThreads) dequant_mxf4_anywhere_kernel(const Params a) {
+  const int lane = int(threadIdx.x), width = int(blockDim.x);
+  const int64_t row = int64_t(blockIdx.x) * blockDim.y + threadIdx.y;
+  if (row >= a.rows) return;
+  T* const x = static_cast<T*>(a.x) + row * a.ldx;
+  const uint8_t* const q = a.q + row * a.ldq;
+  const uint8_t* const scale = a.scale + row * a.lds;
+  const int step = 8 * P * width;
+  for (int64_t base = int64_t(blockIdx.y) * step; base < a.cols; base += int64_t(gridDim.y) * step) {
+    const int c0 = int(base);
+    uint32_t w[P], byte[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int at = c0 + 8 * (i * width + lane);
+      w[i] = byte[i] = 0;
+      if (at < a.cols) {
+        byte[i] = scale[at / kBlock];
+        if (a.q_wide && at + 8 <= a.cols) {
           w[i] = *reinterpret_cast<const uint32_t*>(q + at / 2);
         } else {
 #pragma unroll
@@ -150,31 +213,14 @@ __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) 
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = c0 + 8 * (i * width + lane);
-      if (at >= a.cols) continue;
-      // 2^(byte-127); 2^-127 is half of the least normal number, 255 stands for NaN
-      const float s = __uint_as_float(byte[i] == 255 ? 0x7fffffffu : byte[i] ? byte[i] << 23 : 0x00400000u);
-      float f[8];
+      const int first = c0 + 8 * (i * width + (lane & ~31)) + (lane & 31);
+      const float s = scale_of(byte[i]);
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2(__nv_fp4x2_storage_t((w[i] >> (4 * e)) & 0xff), __NV_E2M1);
-        const float2 d = __half22float2(__half2(h));
-        f[e] = d.x * s;
-        f[e + 1] = d.y * s;
-      }
-      if constexpr (WHOLE) {
-        constexpr int V = 16 / sizeof(T);
-#pragma unroll
-        for (int j = 0; j < 8 / V; ++j) {
-          float g[V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) g[e] = f[j * V + e];
-          reinterpret_cast<Piece<T, V>*>(x + at)[j] = pack<T, V>(g);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (at + e < a.cols) x[at + e] = Elem<T>::down(f[e]);
+      for (int e = 0; e < 8; ++e) {
+        const int from = 4 * e + (lane & 31) / 8;
+        const uint32_t code = __shfl_sync(0xffffffffu, w[i], from) >> (4 * (lane & 7)) & 15;
+        const float v = values2(code).x * __shfl_sync(0xffffffffu, s, from);
+        if (first + 32 * e < a.cols) x[first + 32 * e] = Elem<T>::down(v);
       }
     }
   }
@@ -193,20 +239,23 @@ dim3 grid_of(const Params& a, const dim3& block, int64_t per_chunk) {
 }
 
 template <typename T>
-int run(const Params& a, bool back, cudaStream_t stream) {
+int run(Params a, bool back, cudaStream_t stream) {
   // little work: one piece a thread, for the latency
   const bool little = a.rows * int64_t(a.cols) < (1 << 20), aligned = aligned_rows(a.x, a.ldx, sizeof(T));
   if (back) {
     // groups of eight elements, all whole and on 16 bytes' (codes: 4 bytes') boundaries
     const bool whole = a.cols % 8 == 0 && aligned && aligned_rows(a.q, a.ldq, 1, 4);
     const int64_t groups = (int64_t(a.cols) + 7) / 8;
-    const dim3 block = little ? shape<1>(groups, 4) : shape<4>(groups, 4);
-    auto kernel = little ? (whole ? dequant_mxf4_kernel<T, 1, true> : dequant_mxf4_kernel<T, 1, false>)
-                         : (whole ? dequant_mxf4_kernel<T, 4, true> : dequant_mxf4_kernel<T, 4, false>);
+    const int least = whole ? 4 : 32;  // (else by whole warps)
+    const dim3 block = little ? shape<1>(groups, least) : shape<4>(groups, least);
+    a.q_wide = aligned_rows(a.q, a.ldq, 1, 4);
+    auto kernel = little ? (whole ? dequant_mxf4_kernel<T, 1> : dequant_mxf4_anywhere_kernel<T, 1>)
+                         : (whole ? dequant_mxf4_kernel<T, 4> : dequant_mxf4_anywhere_kernel<T, 4>);
     kernel<<<grid_of(a, block, int64_t(little ? 8 : 32) * block.x), block, 0, stream>>>(a);
   } else {
     // pieces of sixteen elements, made of whole words of 16 bytes; codes on 8 bytes' boundaries
-    const bool whole = a.cols % (16 / int(sizeof(T))) == 0 && aligned && aligned_rows(a.q, a.ldq, 1, 8);
+    a.q_wide = aligned_rows(a.q, a.ldq, 1, 8);
+    const bool whole = a.cols % (16 / int(sizeof(T))) == 0 && aligned && a.q_wide;
     const int64_t halves = (int64_t(a.cols) + 15) / 16;
     const dim3 block = little ? shape<1>(halves, 2) : shape<2>(halves, 2);
     auto kernel = little ? (whole ? quant_mxf4_kernel<T, 1, true> : quant_mxf4_kernel<T, 1, false>)

@@ -91,25 +91,13 @@ template <typename T>
 struct Raw {
   static constexpr int V = 16 / sizeof(T), N = 8 / V;
   Piece<T, V> v[N];
-  template <bool VEC>
   __device__ __forceinline__ void load(const T* p) {
-    if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = reinterpret_cast<const Piece<T, V>*>(p)[i];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e / V].e[e % V] = p[e];
-    }
+    for (int i = 0; i < N; ++i) v[i] = reinterpret_cast<const Piece<T, V>*>(p)[i];
   }
-  template <bool VEC>
   __device__ __forceinline__ void store(T* p) const {
-    if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) reinterpret_cast<Piece<T, V>*>(p)[i] = v[i];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = v[e / V].e[e % V];
-    }
+    for (int i = 0; i < N; ++i) reinterpret_cast<Piece<T, V>*>(p)[i] = v[i];
   }
   __device__ __forceinline__ void get(float (&f)[8]) const {
 #pragma unroll
@@ -134,17 +122,50 @@ struct Raw {
     for (int i = 0; i < N; ++i) v[i] = Piece<T, V>{};
   }
 };
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
   Raw<T> r;
-  r.template load<VEC>(p);
+  r.load(p);
   r.get(f);
 }
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
   Raw<T> r;
   r.set(f);
-  r.template store<VEC>(p);
+  r.store(p);
+}
+
+// Rows that start anywhere go element by element, and so that a warp's accesses lie side by side: it has 256 columns at a
+// time, a lane eight of them 32 apart.  (Eight neighbouring ones a lane touch as many lines with each access as all eight
+// accesses need together.)  `left` columns of the row lie at and behind the lane's first.
+template <typename T>
+__device__ __forceinline__ void load_apart(const T* p, int left, float (&f)[8]) {
+  T v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 32 * e < left ? p[32 * e] : Elem<T>::down(0.0f);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = Elem<T>::up(v[e]);
+}
+template <typename T>
+__device__ __forceinline__ void store_apart(T* p, int left, const float (&f)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (32 * e < left) p[32 * e] = Elem<T>::down(f[e]);
+}
+// The first column of a row's thread in its i-th turn.
+__device__ __forceinline__ int first_apart(int i, int width, int lane) {
+  return (i * width + (lane & ~31)) * kGroup + (lane & 31);
+}
+// Its eight columns lie in eight groups of the warp's 32, of which every lane has called the generator for one.
+__device__ __forceinline__ void drop_apart(const uint32_t (&c)[4], const Dropout& d, int lane, float (&f)[8]) {
+  uint32_t mine = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) mine |= uint32_t(kept(c, e, d.t16)) << e;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t group = __shfl_sync(0xffffffffu, mine, 4 * e + (lane & 31) / 8);
+    f[e] = group >> (lane & 7) & 1 ? f[e] * d.scale : 0.0f;
+  }
 }
 template <typename T>
 __device__ __forceinline__ float rounded(float f) {
@@ -156,10 +177,13 @@ template <typename T>
 struct Weights {
   const void* at;
   bool wide;
-  template <bool VEC>
   __device__ __forceinline__ void load(int col, float (&f)[8]) const {
-    if (wide) load8<float, VEC>(static_cast<const float*>(at) + col, f);
-    else load8<T, VEC>(static_cast<const T*>(at) + col, f);
+    if (wide) load8(static_cast<const float*>(at) + col, f);
+    else load8(static_cast<const T*>(at) + col, f);
+  }
+  __device__ __forceinline__ void apart(int col, int left, float (&f)[8]) const {
+    if (wide) load_apart(static_cast<const float*>(at) + col, left, f);
+    else load_apart(static_cast<const T*>(at) + col, left, f);
   }
   __device__ __forceinline__ float one(int col) const {
     return wide ? static_cast<const float*>(at)[col] : Elem<T>::up(static_cast<const T*>(at)[col]);
@@ -183,7 +207,7 @@ constexpr int kDropThreads = 256;
 // P groups of eight elements a thread; a CTA (threads of a row x rows) goes from rows to rows.  16384 x 4096 bf16: XXDROP.
 // The generator takes 18 us of that (its wide multiplications issue at a quarter of the rate), so everything else has to be
 // short: set-up is paid once a thread, and whole groups have no element-wise alternative beside them.
-template <typename T, int P, bool VEC>
+template <typename T, int P>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams a) {
   const int lane = int(threadIdx.x), width = int(blockDim.x);
   const Stream rng(a.d.rng);
@@ -200,8 +224,8 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams 
       for (int i = 0; i < P; ++i) {
         const int g = g0 + i * width;
         if (g < full) {
-          v[i].template load<VEC>(x + int64_t(g) * kGroup);
-          if (r) res[i].template load<VEC>(r + int64_t(g) * kGroup);
+          v[i].load(x + int64_t(g) * kGroup);
+          if (r) res[i].load(r + int64_t(g) * kGroup);
         }
       }
       uint32_t c[P][4];
@@ -219,7 +243,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams 
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] += h[e];
           }
-          store8<T, VEC>(out + int64_t(g) * kGroup, f);
+          store8(out + int64_t(g) * kGroup, f);
         }
       }
     }
@@ -232,18 +256,52 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropParams 
   }
 }
 
+// The same for rows that start anywhere.
+template <typename T, int P>
+__global__ void __launch_bounds__(kDropThreads) dropout_anywhere_kernel(const DropParams a) {
+  const int lane = int(threadIdx.x), width = int(blockDim.x), step = P * width * kGroup;
+  const Stream rng(a.d.rng);
+  const int64_t stride = int64_t(gridDim.x) * blockDim.y;
+  for (int64_t row = int64_t(blockIdx.x) * blockDim.y + threadIdx.y; row < a.rows; row += stride) {
+    const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* const r = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
+    T* const out = static_cast<T*>(a.out) + row * a.ldo;
+    for (int64_t base = int64_t(blockIdx.y) * step; base < a.cols; base += int64_t(gridDim.y) * step) {
+      float f[P][8], res[P][8];
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const int64_t c = base + first_apart(i, width, lane);
+        const int left = int(a.cols - c);
+        load_apart(x + c, left, f[i]);
+        if (r) load_apart(r + c, left, res[i]);
+      }
+      uint32_t w[P][4];
+      rng.words<P>(uint32_t(base / kGroup) + uint32_t(lane), uint32_t(width), a.d.row0 + uint32_t(row), w);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const int64_t c = base + first_apart(i, width, lane);
+        drop_apart(w[i], a.d, lane, f[i]);
+        if (r) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[i][e] += res[i][e];
+        }
+        store_apart(out + c, int(a.cols - c), f[i]);
+      }
+    }
+  }
+}
+
 template <typename T, int P>
 int run_dropout_by(const DropParams& a, bool vec, cudaStream_t stream) {
-  const int64_t full = std::max(1, a.cols / kGroup);
-  // whole warps of a row's threads where a row has that much
-  int width = int(std::min<int64_t>(kDropThreads, (full + P * 32 - 1) / (P * 32) * 32));
-  while (width > 8 && width / 2 * P >= full) width /= 2;
-  const int high = kDropThreads / width;
-  const int64_t chunks = std::min<int64_t>((full + P * width - 1) / (P * width), 1024), bands = (a.rows + high - 1) / high;
+  const int64_t groups = (int64_t(a.cols) + kGroup - 1) / kGroup, chunks = (groups + P * kDropThreads - 1) / (P * kDropThreads);
+  // whole warps of a row's threads, as many as share its groups evenly; fewer where a short row has fewer groups
+  int width = int((groups + P * chunks * 32 - 1) / (P * chunks * 32) * 32);
+  while (vec && width > 8 && width / 2 * P >= groups) width /= 2;
+  const int high = std::max(1, kDropThreads / width);
   // a few rows for every thread where there are many
-  const int64_t most = std::max<int64_t>(1, int64_t(sm_count()) * 32 / chunks);
-  const dim3 grid(unsigned(std::min(bands, most)), unsigned(chunks));
-  auto kernel = vec ? dropout_kernel<T, P, true> : dropout_kernel<T, P, false>;
+  const int64_t bands = (a.rows + high - 1) / high, y = std::min<int64_t>(chunks, 1024);
+  const dim3 grid(unsigned(std::min(bands, std::max<int64_t>(1, int64_t(sm_count()) * 32 / y))), unsigned(y));
+  auto kernel = vec ? dropout_kernel<T, P> : dropout_anywhere_kernel<T, P>;
   kernel<<<grid, dim3(width, high), 0, stream>>>(a);
   return launched(cudaSuccess);
 }
@@ -287,7 +345,7 @@ __device__ __forceinline__ float row_sum(float v, float* part, int first_warp, i
 // A row in registers: P groups a thread, all of them whole and there (FULL), or up to P and one element of the last,
 // incomplete group.  The mean first, then the mean of the squared distances from it: no difference of large sums.  A CTA is
 // threads of a row x rows.
-template <typename T, int P, bool VEC, bool FULL, bool DROP>
+template <typename T, int P, bool FULL, bool DROP>
 __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const NormParams a) {
   __shared__ float part[2][32];
   const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x);
@@ -305,7 +363,7 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const int g = i * width + lane;
-    if (whole(i)) v[i].template load<VEC>(x + g * kGroup);
+    if (whole(i)) v[i].load(x + g * kGroup);
     else v[i].zero();
   }
   if (has_tail) last = Elem<T>::up(x[tail]);
@@ -315,7 +373,7 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const int g = i * width + lane;
-        if (whole(i)) r[i].template load<VEC>(res + g * kGroup);
+        if (whole(i)) r[i].load(res + g * kGroup);
       }
     }
     uint32_t c[P][4];
@@ -344,7 +402,7 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
   float h[P][8];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (hidden && whole(i)) v[i].template store<VEC>(hidden + (i * width + lane) * kGroup);
+    if (hidden && whole(i)) v[i].store(hidden + (i * width + lane) * kGroup);
     v[i].get(h[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += h[i][e];
@@ -380,11 +438,11 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
     const int g = i * width + lane;
     if (whole(i)) {
       float w[8], b[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-      weight.template load<VEC>(g * kGroup, w);
-      if (a.bias) bias.template load<VEC>(g * kGroup, b);
+      weight.load(g * kGroup, w);
+      if (a.bias) bias.load(g * kGroup, b);
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[i][e] = fmaf(h[i][e] * rstd, w[e], b[e]);
-      store8<T, VEC>(out + g * kGroup, h[i]);
+      store8(out + g * kGroup, h[i]);
     }
   }
   if (has_tail) out[tail] = Elem<T>::down(fmaf(last * rstd, weight.one(tail), a.bias ? bias.one(tail) : 0.0f));
@@ -432,13 +490,78 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_rows_kernel(const Norm
   }
 }
 
+// The same for rows that start anywhere.
+template <typename T, int P>
+__global__ void __launch_bounds__(1024) norm_rows_anywhere_kernel(const NormParams a) {
+  __shared__ float part[2][32];
+  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x);
+  const int64_t row = int64_t(blockIdx.x) * blockDim.y + slot;
+  const int cols = row < a.rows ? a.cols : 0;
+  const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+  const T* const res = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
+  T* const hidden = a.hidden ? static_cast<T*>(a.hidden) + row * a.ldh : nullptr;
+  float h[P][8], sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < P; ++i) load_apart(x + first_apart(i, width, lane), cols - first_apart(i, width, lane), h[i]);
+  if (a.d.rng || res) {
+    const Stream rng(a.d.rng);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = first_apart(i, width, lane);
+      float r[8] = {};
+      if (res) load_apart(res + c, cols - c, r);
+      if (a.d.rng) {
+        uint32_t w[1][4];
+        rng.words<1>(uint32_t(i * width + lane), 0, a.d.row0 + uint32_t(row), w);
+        drop_apart(w[0], a.d, lane, h[i]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] = rounded<T>(res ? h[i][e] + r[e] : h[i][e]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int c = first_apart(i, width, lane);
+    if (hidden) store_apart(hidden + c, cols - c, h[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += h[i][e];  // (0 behind the row's end)
+  }
+  const int warps = width / 32, first_warp = slot * warps;
+  const float mean = row_sum(sum, part[0], first_warp, warps) / float(a.cols);
+  float square = 0.0f;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int left = cols - first_apart(i, width, lane);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      h[i][e] -= mean;
+      if (32 * e < left) square = fmaf(h[i][e], h[i][e], square);
+    }
+  }
+  const float rstd = 1.0f / sqrtf(row_sum(square, part[1], first_warp, warps) / float(a.cols) + a.eps);
+  if (cols == 0) return;
+  if (lane == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  const Weights<T> weight{a.weight, a.wide != 0}, bias{a.bias, a.wide != 0};
+  T* const out = static_cast<T*>(a.out) + row * a.ldo;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int c = first_apart(i, width, lane), left = cols - c;
+    float w[8], b[8] = {};
+    weight.apart(c, left, w);
+    if (a.bias) bias.apart(c, left, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[i][e] = fmaf(h[i][e] * rstd, w[e], b[e]);
+    store_apart(out + c, left, h[i]);
+  }
+}
+
 template <typename T, bool DROP>
-auto pick_norm(int each, bool vec, bool full) {
-  if (!vec) return norm_rows_kernel<T, 2, false, false, DROP>;
-  if (!full) return each == 4 ? norm_rows_kernel<T, 4, true, false, DROP> : norm_rows_kernel<T, 2, true, false, DROP>;
-  return each == 4   ? norm_rows_kernel<T, 4, true, true, DROP>
-         : each == 2 ? norm_rows_kernel<T, 2, true, true, DROP>
-                     : norm_rows_kernel<T, 1, true, true, DROP>;
+auto pick_norm(int each, bool full) {
+  if (!full) return each == 4 ? norm_rows_kernel<T, 4, false, DROP> : norm_rows_kernel<T, 2, false, DROP>;
+  return each == 4 ? norm_rows_kernel<T, 4, true, DROP> : each == 2 ? norm_rows_kernel<T, 2, true, DROP> : norm_rows_kernel<T, 1, true, DROP>;
 }
 
 template <typename T>
@@ -448,7 +571,7 @@ int run_norm(const NormParams& a, cudaStream_t stream) {
                    (!a.residual || aligned_rows(a.residual, a.ldr, sizeof(T))) &&
                    (!a.hidden || aligned_rows(a.hidden, a.ldh, sizeof(T))) && aligned(a.weight) &&
                    (!a.bias || aligned(a.bias));
-  const int groups = std::max(1, a.cols / kGroup);
+  const int groups = (a.cols + kGroup - 1) / kGroup;
   if (groups > 2048) {
     norm_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
     return launched(cudaSuccess);
@@ -459,10 +582,11 @@ int run_norm(const NormParams& a, cudaStream_t stream) {
   int each = most;
   while (each > 1 && !fits(each)) each /= 2;
   const bool full = fits(each);
-  if (!full) each = vec && (most == 4 || groups > 1024) ? 4 : 2;
+  if (!full) each = vec && (most == 4 || groups > 1024) ? 4 : vec || most > 1 || groups > 1024 ? 2 : 1;
   const int width = (groups + each * 32 - 1) / (each * 32) * 32, high = std::max(1, 128 / width);
   const unsigned grid = unsigned((a.rows + high - 1) / high);
-  auto kernel = a.d.rng ? pick_norm<T, true>(each, vec, full) : pick_norm<T, false>(each, vec, full);
+  auto kernel = !vec ? (each == 1 ? norm_rows_anywhere_kernel<T, 1> : norm_rows_anywhere_kernel<T, 2>)
+                : a.d.rng ? pick_norm<T, true>(each, full) : pick_norm<T, false>(each, full);
   kernel<<<grid, dim3(width, high), 0, stream>>>(a);
   return launched(cudaSuccess);
 }
@@ -485,32 +609,31 @@ struct GradParams {
   Dropout d;
 };
 
-// How the rows are spread: parts of the sums are CTAs times the rows that each takes at a time.
+// How the rows are spread: every CTA gives a part of the sums.
 struct GradPlan {
-  int row_threads, per_cta, ctas;
+  int each, width, high, ctas;  // groups of eight columns a thread, threads of a row, rows of a CTA at a time
   bool in_registers;
-  int64_t parts() const { return int64_t(ctas) * per_cta; }
 };
 
-constexpr int kGradGroups = 2;           // groups of eight columns a thread
 constexpr int kGradThreads = 512;        // at most
 constexpr int kGradHalf = 320;           // at most, where two CTAs share an SM
 constexpr int kStripRows = 64;           // rows of a part where the columns are summed by themselves
 
 GradPlan grad_plan(int64_t rows, int64_t cols) {
   GradPlan g;
-  const int64_t groups = std::max<int64_t>(1, cols / kGroup);
-  g.in_registers = groups <= kGradGroups * kGradThreads;
+  const int64_t groups = (cols + kGroup - 1) / kGroup;
+  g.in_registers = groups <= 4 * kGradThreads;
   if (!g.in_registers) {
-    g.row_threads = kLongThreads;
-    g.per_cta = 1;
+    g.each = g.high = 1;
+    g.width = kLongThreads;
     g.ctas = int(std::min<int64_t>(256, std::max<int64_t>(1, (rows + kStripRows - 1) / kStripRows)));
     return g;
   }
-  g.row_threads = int((groups + kGradGroups * 32 - 1) / (kGradGroups * 32)) * 32;
-  g.per_cta = std::max(1, 256 / g.row_threads);
-  const int resident = g.row_threads <= kGradHalf ? 2 : 1;
-  g.ctas = int(std::min<int64_t>((rows + g.per_cta - 1) / g.per_cta, int64_t(resident) * 148));
+  g.each = groups <= 2 * kGradThreads ? 2 : 4;
+  g.width = int((groups + g.each * 32 - 1) / (g.each * 32)) * 32;
+  g.high = std::max(1, 256 / g.width);
+  const int resident = g.each == 2 && g.width <= kGradHalf ? 2 : 1;
+  g.ctas = int(std::min<int64_t>((rows + g.high - 1) / g.high, int64_t(resident) * 148));
   g.ctas = std::max(1, g.ctas);
   return g;
 }
@@ -534,131 +657,132 @@ __device__ __forceinline__ float2 row_sum2(float2 v, float2* part, int first_war
   return upper ? make_float2(other, s) : make_float2(s, other);
 }
 
+// A CTA's part of the sums: put(to) writes a thread's own to a [2][cols].  Those of several
+// rows at a time meet in shared memory first.
+template <typename F>
+__device__ __forceinline__ void put_sums(const GradParams& a, float* pool, int slot, int high, const F& put) {
+  float* const part = a.work + int64_t(blockIdx.x) * 2 * a.cols;
+  if (high == 1) {
+    put(part);
+    return;
+  }
+  __syncthreads();  // (what else the pool was for is over)
+  put(pool + slot * 2 * a.cols);
+  __syncthreads();
+  for (int i = int(threadIdx.y * blockDim.x + threadIdx.x); i < 2 * a.cols; i += int(blockDim.x * blockDim.y)) {
+    float v = pool[i];
+    for (int s = 1; s < high; ++s) v += pool[s * 2 * a.cols + i];
+    part[i] = v;
+  }
+}
+
 // With g = dout weight and n = (hidden - mean) rstd: dh = rstd (g - mean(g) - n mean(g n)) + dhidden.  A thread keeps its
-// columns from row to row, and with them their sums of dout n and dout.  This form is for rows that start anywhere.
-template <typename T>
+// columns from row to row, and with them their sums of dout n and dout.  This form is for rows that start anywhere.  With four
+// groups a thread the second half of a row reads it again.
+template <typename T, int P>
 __global__ void __launch_bounds__(kGradThreads) norm_grad_anywhere_kernel(const GradParams a) {
-  constexpr int P = kGradGroups;
+  extern __shared__ float pool[];
   __shared__ float2 part[2][32];
-  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x), per_cta = int(blockDim.y);
-  const int full = a.cols / kGroup, tail = full * kGroup + lane;
-  const bool has_tail = lane < kGroup && tail < a.cols;
+  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x), high = int(blockDim.y);
   const int warps = width / 32, first_warp = slot * warps;
   const Weights<T> weight{a.weight, a.wide != 0};
   const Stream rng(a.d.rng);
   const float per_col = 1.0f / float(a.cols);
-  float dw[P][8] = {}, db[P][8] = {}, dw_tail = 0.0f, db_tail = 0.0f;
+  float dw[P][8] = {}, db[P][8] = {};
   int turn = 0;
-  for (int64_t row0 = int64_t(blockIdx.x) * per_cta; row0 < a.rows; row0 += int64_t(gridDim.x) * per_cta, turn ^= 1) {
+  for (int64_t row0 = int64_t(blockIdx.x) * high; row0 < a.rows; row0 += int64_t(gridDim.x) * high, turn ^= 1) {
     const int64_t row = row0 + slot;
     const bool there = row < a.rows;
+    const int cols = there ? a.cols : 0;
     const T* const dout = static_cast<const T*>(a.dout) + row * a.ldo;
     const T* const hidden = static_cast<const T*>(a.hidden) + row * a.ldh;
-    float g[P][8], n[P][8], g_tail = 0.0f, n_tail = 0.0f;
+    constexpr int KEEP = P <= 2 ? P : 1;
+    float g[KEEP][8], n[KEEP][8];
     float2 s = make_float2(0.0f, 0.0f);
     const float mean = there ? a.mean[row] : 0.0f, rstd = there ? a.rstd[row] : 0.0f;
+    auto load = [&](int i) {
+      const int c = first_apart(i, width, lane);
+      load_apart(dout + c, cols - c, g[i % KEEP]);  // (0 behind the row's end, and so is what is made of it)
+      load_apart(hidden + c, cols - c, n[i % KEEP]);
+    };
+    if constexpr (KEEP == P) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int at = i * width + lane;
-      if (there && at < full) {
-        load8<T, false>(dout + at * kGroup, g[i]);
-        load8<T, false>(hidden + at * kGroup, n[i]);
-      }
+      for (int i = 0; i < P; ++i) load(i);
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = i * width + lane;
-      if (there && at < full) {
-        float w[8];
-        weight.template load<false>(at * kGroup, w);
+      const int c = first_apart(i, width, lane), k = i % KEEP;
+      if constexpr (KEEP < P) load(i);
+      float w[8];
+      weight.apart(c, cols - c, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          n[i][e] = (n[i][e] - mean) * rstd;
-          dw[i][e] = fmaf(g[i][e], n[i][e], dw[i][e]);
-          db[i][e] += g[i][e];
-          g[i][e] *= w[e];
-          s.x += g[i][e];
-          s.y = fmaf(g[i][e], n[i][e], s.y);
-        }
+      for (int e = 0; e < 8; ++e) {
+        n[k][e] = (n[k][e] - mean) * rstd;
+        dw[i][e] = 32 * e < cols - c ? fmaf(g[k][e], n[k][e], dw[i][e]) : dw[i][e];
+        db[i][e] += g[k][e];
+        g[k][e] *= w[e];
+        s.x += g[k][e];
+        s.y = 32 * e < cols - c ? fmaf(g[k][e], n[k][e], s.y) : s.y;
       }
-    }
-    if (has_tail && there) {
-      g_tail = Elem<T>::up(dout[tail]);
-      n_tail = (Elem<T>::up(hidden[tail]) - mean) * rstd;
-      dw_tail = fmaf(g_tail, n_tail, dw_tail);
-      db_tail += g_tail;
-      g_tail *= weight.one(tail);
-      s.x += g_tail;
-      s.y = fmaf(g_tail, n_tail, s.y);
     }
     s = row_sum2(s, part[turn], first_warp, warps);
     s.x *= per_col;
     s.y *= per_col;
     if (!there) continue;
-    const T* const dhidden = a.dhidden ? static_cast<const T*>(a.dhidden) + row * a.lddh : nullptr;
-    T* const dresidual = a.dresidual ? static_cast<T*>(a.dresidual) + row * a.lddr : nullptr;
-    T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
-    const uint32_t number = a.d.row0 + uint32_t(row);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = i * width + lane;
-      if (at < full) {
-        float f[8] = {};
-        if (dhidden) load8<T, false>(dhidden + at * kGroup, f);
+      const int c = first_apart(i, width, lane), k = i % KEEP;
+      if constexpr (KEEP < P) {
+        float w[8];
+        load(i);
+        weight.apart(c, cols - c, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, g[i][e] - s.x - n[i][e] * s.y, f[e]);
-        if (dresidual) store8<T, false>(dresidual + at * kGroup, f);
-        if (a.d.rng) {
-          uint32_t c[1][4];
-          rng.words<1>(uint32_t(at), 0, number, c);
-          drop8(c[0], a.d, f);
+        for (int e = 0; e < 8; ++e) {
+          n[k][e] = (n[k][e] - mean) * rstd;
+          g[k][e] *= w[e];
         }
-        store8<T, false>(dx + at * kGroup, f);
       }
-    }
-    if (has_tail) {
-      float f = fmaf(rstd, g_tail - s.x - n_tail * s.y, dhidden ? Elem<T>::up(dhidden[tail]) : 0.0f);
-      if (dresidual) dresidual[tail] = Elem<T>::down(f);
-      if (a.d.rng) f = drop1(rng, a.d, number, uint32_t(tail), f);
-      dx[tail] = Elem<T>::down(f);
-    }
-  }
-  float* const sums = a.work + (int64_t(blockIdx.x) * per_cta + slot) * 2 * a.cols;
+      float f[8] = {};
+      if (a.dhidden) load_apart(static_cast<const T*>(a.dhidden) + row * a.lddh + c, cols - c, f);
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const int at = i * width + lane;
-    if (at < full) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sums[at * kGroup + e] = dw[i][e];
-        sums[int64_t(a.cols) + at * kGroup + e] = db[i][e];
+      for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, g[k][e] - s.x - n[k][e] * s.y, f[e]);
+      if (a.dresidual) store_apart(static_cast<T*>(a.dresidual) + row * a.lddr + c, cols - c, f);
+      if (a.d.rng) {
+        uint32_t w[1][4];
+        rng.words<1>(uint32_t(i * width + lane), 0, a.d.row0 + uint32_t(row), w);
+        drop_apart(w[0], a.d, lane, f);
       }
+      store_apart(static_cast<T*>(a.dx) + row * a.lddx + c, cols - c, f);
     }
   }
-  if (has_tail) {
-    sums[tail] = dw_tail;
-    sums[int64_t(a.cols) + tail] = db_tail;
-  }
+  put_sums(a, pool, slot, high, [&](float* sums) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = first_apart(i, width, lane);
+      store_apart(sums + c, a.cols - c, dw[i]);
+      store_apart(sums + a.cols + c, a.cols - c, db[i]);
+    }
+  });
 }
 
 // The same for rows on 16-byte boundaries (FULL: whose groups are all whole and there).  Every thread copies its own pieces
 // of dout, hidden and dhidden ahead, into places of shared memory that no other thread looks at: D rows are under way or in
 // work, and the only barrier of a row is that of its two sums.  What the second half of a row needs is read again instead of
 // held in registers, the weights too: 96 registers have to do where two CTAs share an SM.
-template <typename T, int D, int THREADS, bool FULL>
+template <typename T, int P, int D, int THREADS, bool FULL>
 __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_grad_kernel(const GradParams a) {
-  constexpr int P = kGradGroups, N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
+  constexpr int N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float2 part[2][32];
-  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x), per_cta = int(blockDim.y);
+  const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x), high = int(blockDim.y);
   const int full = FULL ? P * width : a.cols / kGroup, tail = full * kGroup + lane;
   const bool has_tail = !FULL && lane < kGroup && tail < a.cols;
   const int warps = width / 32, first_warp = slot * warps;
   const Weights<T> weight{a.weight, a.wide != 0};
   const Stream rng(a.d.rng);
   const float per_col = 1.0f / float(a.cols);
-  const int64_t stride = int64_t(gridDim.x) * per_cta;
-  int64_t row = int64_t(blockIdx.x) * per_cta + slot, ahead = row;
+  const int64_t stride = int64_t(gridDim.x) * high;
+  int64_t row = int64_t(blockIdx.x) * high + slot, ahead = row;
   const T *dout = static_cast<const T*>(a.dout) + row * a.ldo + lane * kGroup,
           *hidden = static_cast<const T*>(a.hidden) + row * a.ldh + lane * kGroup,
           *dhidden = a.dhidden ? static_cast<const T*>(a.dhidden) + row * a.lddh + lane * kGroup : nullptr;
@@ -700,7 +824,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
 #pragma unroll
   for (int i = 0; i < D - 1; ++i) fetch(i);
   float mean = 0.0f, rstd = 0.0f, next_mean = row < a.rows ? a.mean[row] : 0.0f, next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
-  for (int64_t row0 = int64_t(blockIdx.x) * per_cta; row0 < a.rows; row0 += stride, row += stride, turn ^= 1) {
+  for (int64_t row0 = int64_t(blockIdx.x) * high; row0 < a.rows; row0 += stride, row += stride, turn ^= 1) {
     const bool there = row < a.rows;
     fetch(d + D - 1 < D ? d + D - 1 : d - 1);
     mean = next_mean;
@@ -718,7 +842,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
       for (int i = 0; i < P; ++i) {
         if (whole(i)) {
           float g[8], h[8], w[8];
-          weight.template load<true>((i * width + lane) * kGroup, w);
+          weight.load((i * width + lane) * kGroup, w);
           get(from, 0, i, g);
           get(from, 1, i, h);
 #pragma unroll
@@ -754,19 +878,19 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
         if (whole(i)) {
           const int g0 = i * width + lane;
           float g[8], h[8], w[8], f[8] = {};
-          weight.template load<true>(g0 * kGroup, w);
+          weight.load(g0 * kGroup, w);
           get(from, 0, i, g);
           get(from, 1, i, h);
           if (a.dhidden) get(from, 2, i, f);
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, fmaf(g[e], w[e], -s.x) - (h[e] - mean) * rstd * s.y, f[e]);
-          if (dresidual) store8<T, true>(dresidual + g0 * kGroup, f);
+          if (dresidual) store8(dresidual + g0 * kGroup, f);
           if (a.d.rng) {
             uint32_t c[1][4];
             rng.words<1>(uint32_t(g0), 0, number, c);
             drop8(c[0], a.d, f);
           }
-          store8<T, true>(dx + g0 * kGroup, f);
+          store8(dx + g0 * kGroup, f);
         }
       }
       if (has_tail) {
@@ -780,27 +904,31 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
     if (++d == D) d = 0;
   }
   cp_async_wait<0>();
-  float* const sums = a.work + (int64_t(blockIdx.x) * per_cta + slot) * 2 * a.cols;
+  put_sums(a, reinterpret_cast<float*>(ring), slot, high, [&](float* sums) {
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    if (whole(i)) {
+    for (int i = 0; i < P; ++i) {
+      if (whole(i)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sums[(i * width + lane) * kGroup + e] = dw[i][e];
-        sums[int64_t(a.cols) + (i * width + lane) * kGroup + e] = db[i][e];
+        for (int e = 0; e < 8; ++e) {
+          sums[(i * width + lane) * kGroup + e] = dw[i][e];
+          sums[a.cols + (i * width + lane) * kGroup + e] = db[i][e];
+        }
       }
     }
-  }
-  if (has_tail) {
-    sums[tail] = dw_tail;
-    sums[int64_t(a.cols) + tail] = db_tail;
-  }
+    if (has_tail) {
+      sums[tail] = dw_tail;
+      sums[a.cols + tail] = db_tail;
+    }
+  });
 }
 
-template <typename T, int THREADS>
-auto pick_grad(int depth, bool full) {
-  if (depth == 3) return full ? norm_grad_kernel<T, 3, THREADS, true> : norm_grad_kernel<T, 3, THREADS, false>;
-  return full ? norm_grad_kernel<T, 2, THREADS, true> : norm_grad_kernel<T, 2, THREADS, false>;
+// By depth and threads; four groups a thread only where two rows of 512 such threads fit (16-bit types).
+template <typename T, bool FULL>
+auto pick_grad(int each, int depth, bool half) {
+  if constexpr (sizeof(T) == 2)
+    if (each == 4) return norm_grad_kernel<T, 4, 2, kGradThreads, FULL>;
+  if (half) return depth == 3 ? norm_grad_kernel<T, 2, 3, kGradHalf, FULL> : norm_grad_kernel<T, 2, 2, kGradHalf, FULL>;
+  return depth == 3 ? norm_grad_kernel<T, 2, 3, kGradThreads, FULL> : norm_grad_kernel<T, 2, 2, kGradThreads, FULL>;
 }
 
 // Rows too long for that: dx by a CTA that reads a row twice, ...
@@ -850,26 +978,28 @@ __global__ void __launch_bounds__(128) norm_grad_columns_kernel(const GradParams
   a.work[int64_t(part) * 2 * a.cols + a.cols + c] = db;
 }
 
-constexpr int kSumRows = 32;
+constexpr int kSumThreads = 1024;
 
-// The parts' sums added up, in their order: 32 columns a CTA.
-__global__ void __launch_bounds__(32 * kSumRows) norm_sum_kernel(const float* work, int64_t parts, int cols, float* dweight,
-                                                                 float* dbias) {
-  __shared__ float sums[kSumRows][33];
-  const int lane = int(threadIdx.x) % 32, y = int(threadIdx.x) / 32;
-  const int64_t c = int64_t(blockIdx.x) * 32 + lane;
+// The parts' sums added up, in a fixed order: X columns a CTA.
+template <int X>
+__global__ void __launch_bounds__(kSumThreads) norm_sum_kernel(const float* work, int parts, int cols, float* dweight, float* dbias) {
+  constexpr int Y = kSumThreads / X;
+  __shared__ float sums[Y][X + 1];
+  const int x = int(threadIdx.x) % X, y = int(threadIdx.x) / X;
+  const int64_t c = int64_t(blockIdx.x) * X + x;
   const float* const in = work + int64_t(blockIdx.y) * cols + c;
   float v = 0.0f;
   if (c < cols) {
 #pragma unroll 4
-    for (int64_t i = y; i < parts; i += kSumRows) v += in[i * 2 * cols];
+    for (int i = y; i < parts; i += Y) v += in[int64_t(i) * 2 * cols];
   }
-  sums[y][lane] = v;
-  __syncthreads();
-  if (y == 0 && c < cols) {
-    for (int i = 1; i < kSumRows; ++i) v += sums[i][lane];
-    (blockIdx.y == 0 ? dweight : dbias)[c] = v;
+  sums[y][x] = v;
+#pragma unroll
+  for (int half = Y / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (y < half) sums[y][x] += sums[y + half][x];
   }
+  if (y == 0 && c < cols) (blockIdx.y == 0 ? dweight : dbias)[c] = sums[0][x];
 }
 
 template <typename T>
@@ -880,19 +1010,21 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
     const bool vec = aligned_rows(a.dout, a.ldo, sizeof(T)) && aligned_rows(a.hidden, a.ldh, sizeof(T)) &&
                      aligned_rows(a.dx, a.lddx, sizeof(T)) && (!a.dhidden || aligned_rows(a.dhidden, a.lddh, sizeof(T))) &&
                      (!a.dresidual || aligned_rows(a.dresidual, a.lddr, sizeof(T))) && aligned(a.weight);
-    const dim3 threads(plan.row_threads, plan.per_cta);
-    if (vec) {
+    const dim3 threads(plan.width, plan.high);
+    if (vec && (plan.each == 2 || sizeof(T) == 2)) {
       // three rows where they fit (with two CTAs to an SM, or alone), else two
-      const bool half = plan.row_threads * plan.per_cta <= kGradHalf;
-      const bool full = a.cols == plan.row_threads * kGradGroups * kGroup;
-      const int row_bytes = (half ? kGradHalf : kGradThreads) * 3 * kGradGroups * kGroup * int(sizeof(T));
+      const bool half = plan.each == 2 && plan.width * plan.high <= kGradHalf;
+      const bool full = a.cols == plan.width * plan.each * kGroup;
+      const int row_bytes = (half ? kGradHalf : kGradThreads) * 3 * plan.each * kGroup * int(sizeof(T));
       const int depth = row_bytes * 3 <= (half ? 112 : 224) * 1024 ? 3 : 2;
-      auto kernel = half ? pick_grad<T, kGradHalf>(depth, full) : pick_grad<T, kGradThreads>(depth, full);
+      auto kernel = full ? pick_grad<T, true>(plan.each, depth, half) : pick_grad<T, false>(plan.each, depth, half);
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, row_bytes * depth);
       if (e != cudaSuccess) return launched(e);
       kernel<<<unsigned(plan.ctas), threads, row_bytes * depth, stream>>>(a);
     } else {
-      norm_grad_anywhere_kernel<T><<<unsigned(plan.ctas), threads, 0, stream>>>(a);
+      auto kernel = plan.each == 2 ? norm_grad_anywhere_kernel<T, 2> : norm_grad_anywhere_kernel<T, 4>;
+      const int pool = plan.high > 1 ? plan.high * 2 * a.cols * 4 : 0;  // (32 KB at most: 256 threads' 16 columns)
+      kernel<<<unsigned(plan.ctas), threads, pool, stream>>>(a);
     }
   } else {
     if (a.rows > 0) norm_grad_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
@@ -901,8 +1033,11 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
   }
   const int rc = launched(cudaSuccess);
   if (rc != ENTWINE_OK) return rc;
-  const dim3 grid(unsigned((int64_t(a.cols) + 31) / 32), dbias ? 2 : 1);
-  norm_sum_kernel<<<grid, 32 * kSumRows, 0, stream>>>(a.work, plan.parts(), a.cols, dweight, dbias);
+  // (narrow strips where there are few columns: more CTAs, fewer parts for each thread)
+  const int x = a.cols >= 4096 ? 32 : 8;
+  const dim3 grid(unsigned((int64_t(a.cols) + x - 1) / x), dbias ? 2 : 1);
+  auto kernel = x == 32 ? norm_sum_kernel<32> : norm_sum_kernel<8>;
+  kernel<<<grid, kSumThreads, 0, stream>>>(a.work, plan.ctas, a.cols, dweight, dbias);
   return launched(cudaSuccess);
 }
 
@@ -997,7 +1132,7 @@ int entwine_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int
 
 int entwine_layer_norm_bwd_work(int64_t rows, int64_t cols, int64_t* floats) {
   if (!floats || rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols) return ENTWINE_ERR_INVALID;
-  *floats = grad_plan(rows, cols).parts() * 2 * cols;
+  *floats = int64_t(grad_plan(rows, cols).ctas) * 2 * cols;
   return ENTWINE_OK;
 }
 
@@ -1014,7 +1149,7 @@ int entwine_layer_norm_bwd(const void* dout, int dtype, int64_t rows, int64_t co
   if (!make_dropout(p, rng, row0, rows, &a.d)) return ENTWINE_ERR_INVALID;
   const int64_t elem = bytes_of(dtype), w_elem = bytes_of(w_dtype);
   if (bad_pointer(dweight, 4) || (dbias && bad_pointer(dbias, 4)) || bad_pointer(work, 4) ||
-      work_floats < grad_plan(rows, cols).parts() * 2 * cols)
+      work_floats < int64_t(grad_plan(rows, cols).ctas) * 2 * cols)
     return ENTWINE_ERR_INVALID;
   // (without rows the sums are still written)
   if (rows > 0 && (bad_pointer(dout, elem) || bad_pointer(hidden, elem) || bad_pointer(weight, w_elem) ||
