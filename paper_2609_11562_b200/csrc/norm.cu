@@ -172,6 +172,38 @@ __device__ __forceinline__ float rounded(float f) {
   return Elem<T>::up(Elem<T>::down(f));
 }
 
+// Two fp32 values in one register pair, and arithmetic on both at once.
+struct Two {
+  unsigned long long v;
+  Two() = default;
+  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Two add(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two mul(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ void twos(const float (&f)[8], Two (&t)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t[j] = Two(f[2 * j], f[2 * j + 1]);
+}
+__device__ __forceinline__ void ones(const Two (&t)[4], float (&f)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t[j].get(f[2 * j], f[2 * j + 1]);
+}
+
 // Weights: of the rows' type, or fp32.
 template <typename T>
 struct Weights {
@@ -387,9 +419,13 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
         if constexpr (DROP) drop8(c[i], a.d, f);
         if (res) {
           float h[8];
+          Two t[4], u[4];
           r[i].get(h);
+          twos(f, t);
+          twos(h, u);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] += h[e];
+          for (int j = 0; j < 4; ++j) t[j] = add(t[j], u[j]);
+          ones(t, f);
         }
         v[i].set(f);  // rounded, as it is written
       }
@@ -399,28 +435,35 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
       last = rounded<T>(res ? last + Elem<T>::up(res[tail]) : last);
     }
   }
-  float h[P][8];
+  Two h[P][4], all(0.0f);
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     if (hidden && whole(i)) v[i].store(hidden + (i * width + lane) * kGroup);
-    v[i].get(h[i]);
+    float f[8];
+    v[i].get(f);
+    twos(f, h[i]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += h[i][e];
+    for (int j = 0; j < 4; ++j) all = add(all, h[i][j]);
   }
   if (hidden && has_tail) hidden[tail] = Elem<T>::down(last);
-  sum += last;
+  float even, odd;
+  all.get(even, odd);
+  sum = even + odd + last;
   const int warps = width / 32, first_warp = slot * warps;
   const float mean = row_sum(sum, part[0], first_warp, warps) / float(a.cols);
-  float square = 0.0f;
+  const Two minus_mean(-mean);
+  all = Two(0.0f);
 #pragma unroll
   for (int i = 0; i < P; ++i)
     if (whole(i)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        h[i][e] -= mean;
-        square = fmaf(h[i][e], h[i][e], square);
+      for (int j = 0; j < 4; ++j) {
+        h[i][j] = add(h[i][j], minus_mean);
+        all = fma(h[i][j], h[i][j], all);
       }
     }
+  all.get(even, odd);
+  float square = even + odd;
   if (has_tail) {
     last -= mean;
     square = fmaf(last, last, square);
@@ -433,6 +476,7 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
   }
   const Weights<T> weight{a.weight, a.wide != 0}, bias{a.bias, a.wide != 0};
   T* const out = static_cast<T*>(a.out) + row * a.ldo;
+  const Two by_rstd(rstd);
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     const int g = i * width + lane;
@@ -440,9 +484,13 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
       float w[8], b[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       weight.load(g * kGroup, w);
       if (a.bias) bias.load(g * kGroup, b);
+      Two t[4], u[4];
+      twos(w, t);
+      twos(b, u);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[i][e] = fmaf(h[i][e] * rstd, w[e], b[e]);
-      store8(out + g * kGroup, h[i]);
+      for (int j = 0; j < 4; ++j) t[j] = fma(mul(h[i][j], by_rstd), t[j], u[j]);
+      ones(t, w);
+      store8(out + g * kGroup, w);
     }
   }
   if (has_tail) out[tail] = Elem<T>::down(fmaf(last * rstd, weight.one(tail), a.bias ? bias.one(tail) : 0.0f));
@@ -768,10 +816,11 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_anywhere_kernel(const 
 // The same for rows on 16-byte boundaries (FULL: whose groups are all whole and there).  Every thread copies its own pieces
 // of dout, hidden and dhidden ahead, into places of shared memory that no other thread looks at: D rows are under way or in
 // work, and the only barrier of a row is that of its two sums.  What the second half of a row needs is read again instead of
-// held in registers, the weights too: 96 registers have to do where two CTAs share an SM.
+// held in registers, the weights (in fp32) too: 96 registers have to do where two CTAs share an SM.
 template <typename T, int P, int D, int THREADS, bool FULL>
 __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_grad_kernel(const GradParams a) {
   constexpr int N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
+  constexpr bool KEPT = P == 2;  // weights kept in shared memory, fp32, behind the rows
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float2 part[2][32];
   const int slot = int(threadIdx.y), lane = int(threadIdx.x), width = int(blockDim.x), high = int(blockDim.y);
@@ -810,16 +859,46 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
     hidden += stride * a.ldh;
     if (a.dhidden) dhidden += stride * a.lddh;
   };
-  auto get = [&](const uint4* from, int what, int i, float (&f)[8]) {
+  auto get = [&](const uint4* from, int what, int i, Two (&t)[4]) {
     Raw<T> r;
 #pragma unroll
     for (int piece = 0; piece < N; ++piece) {
       const uint4 w = from[((what * P + i) * N + piece) * THREADS];
       memcpy(&r.v[piece], &w, 16);
     }
+    float f[8];
     r.get(f);
+    twos(f, t);
   };
-  float dw[P][8] = {}, db[P][8] = {}, dw_tail = 0.0f, db_tail = 0.0f;
+  uint4* const kept_weights = mine + D * kRow;
+  if constexpr (KEPT) {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (whole(i)) {
+        float w[8];
+        weight.load((i * width + lane) * kGroup, w);
+        uint4 v[2];
+        memcpy(v, w, sizeof(v));
+        kept_weights[2 * i * THREADS] = v[0];
+        kept_weights[(2 * i + 1) * THREADS] = v[1];
+      }
+  }
+  auto get_weight = [&](int i, Two (&t)[4]) {
+    float w[8];
+    if constexpr (KEPT) {
+      const uint4 v[2] = {kept_weights[2 * i * THREADS], kept_weights[(2 * i + 1) * THREADS]};
+      memcpy(w, v, sizeof(v));
+    } else {
+      weight.load((i * width + lane) * kGroup, w);
+    }
+    twos(w, t);
+  };
+  Two dw[P][4], db[P][4];
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dw[i][j] = db[i][j] = Two(0.0f);
+  float dw_tail = 0.0f, db_tail = 0.0f;
   int turn = 0, d = 0;
 #pragma unroll
   for (int i = 0; i < D - 1; ++i) fetch(i);
@@ -835,24 +914,26 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
     }
     cp_async_wait<D - 1>();
     const uint4* const from = mine + d * kRow;
+    const Two minus_mean(-mean), by_rstd(rstd);
+    Two sum(0.0f), dot(0.0f);
     float2 s = make_float2(0.0f, 0.0f);
     float g_tail = 0.0f, n_tail = 0.0f;
     if (there) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         if (whole(i)) {
-          float g[8], h[8], w[8];
-          weight.load((i * width + lane) * kGroup, w);
+          Two g[4], h[4], w[4];
           get(from, 0, i, g);
           get(from, 1, i, h);
+          get_weight(i, w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float n = (h[e] - mean) * rstd;
-            dw[i][e] = fmaf(g[e], n, dw[i][e]);
-            db[i][e] += g[e];
-            g[e] *= w[e];
-            s.x += g[e];
-            s.y = fmaf(g[e], n, s.y);
+          for (int j = 0; j < 4; ++j) {
+            const Two n = mul(add(h[j], minus_mean), by_rstd);
+            dw[i][j] = fma(g[j], n, dw[i][j]);
+            db[i][j] = add(db[i][j], g[j]);
+            const Two gw = mul(g[j], w[j]);
+            sum = add(sum, gw);
+            dot = fma(gw, n, dot);
           }
         }
       }
@@ -866,9 +947,15 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
         s.y = fmaf(g_tail, n_tail, s.y);
       }
     }
+    float even, odd;
+    sum.get(even, odd);
+    s.x += even + odd;
+    dot.get(even, odd);
+    s.y += even + odd;
     s = row_sum2(s, part[turn], first_warp, warps);
     s.x *= per_col;
     s.y *= per_col;
+    const Two minus_sum(-s.x), minus_dot(-s.y);
     if (there) {
       T* const dresidual = a.dresidual ? static_cast<T*>(a.dresidual) + row * a.lddr : nullptr;
       T* const dx = static_cast<T*>(a.dx) + row * a.lddx;
@@ -877,13 +964,20 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
       for (int i = 0; i < P; ++i) {
         if (whole(i)) {
           const int g0 = i * width + lane;
-          float g[8], h[8], w[8], f[8] = {};
-          weight.load(g0 * kGroup, w);
+          Two g[4], h[4], w[4], t[4];
           get(from, 0, i, g);
           get(from, 1, i, h);
-          if (a.dhidden) get(from, 2, i, f);
+          get_weight(i, w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, fmaf(g[e], w[e], -s.x) - (h[e] - mean) * rstd * s.y, f[e]);
+          for (int j = 0; j < 4; ++j) t[j] = Two(0.0f);
+          if (a.dhidden) get(from, 2, i, t);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const Two n = mul(add(h[j], minus_mean), by_rstd);
+            t[j] = fma(by_rstd, fma(n, minus_dot, fma(g[j], w[j], minus_sum)), t[j]);
+          }
+          float f[8];
+          ones(t, f);
           if (dresidual) store8(dresidual + g0 * kGroup, f);
           if (a.d.rng) {
             uint32_t c[1][4];
@@ -908,11 +1002,13 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       if (whole(i)) {
+        float f[8];
+        ones(dw[i], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sums[(i * width + lane) * kGroup + e] = dw[i][e];
-          sums[a.cols + (i * width + lane) * kGroup + e] = db[i][e];
-        }
+        for (int e = 0; e < 8; ++e) sums[(i * width + lane) * kGroup + e] = f[e];
+        ones(db[i], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[a.cols + (i * width + lane) * kGroup + e] = f[e];
       }
     }
     if (has_tail) {
@@ -978,7 +1074,7 @@ __global__ void __launch_bounds__(128) norm_grad_columns_kernel(const GradParams
   a.work[int64_t(part) * 2 * a.cols + a.cols + c] = db;
 }
 
-constexpr int kSumThreads = 1024;
+constexpr int kSumThreads = 512;
 
 // The parts' sums added up, in a fixed order: X columns a CTA.
 template <int X>
@@ -990,7 +1086,7 @@ __global__ void __launch_bounds__(kSumThreads) norm_sum_kernel(const float* work
   const float* const in = work + int64_t(blockIdx.y) * cols + c;
   float v = 0.0f;
   if (c < cols) {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = y; i < parts; i += Y) v += in[int64_t(i) * 2 * cols];
   }
   sums[y][x] = v;
@@ -1016,11 +1112,12 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
       const bool half = plan.each == 2 && plan.width * plan.high <= kGradHalf;
       const bool full = a.cols == plan.width * plan.each * kGroup;
       const int row_bytes = (half ? kGradHalf : kGradThreads) * 3 * plan.each * kGroup * int(sizeof(T));
-      const int depth = row_bytes * 3 <= (half ? 112 : 224) * 1024 ? 3 : 2;
+      const int kept = plan.each == 2 ? (half ? kGradHalf : kGradThreads) * plan.each * kGroup * 4 : 0;
+      const int depth = row_bytes * 3 + kept <= (half ? 112 : 224) * 1024 ? 3 : 2, bytes = row_bytes * depth + kept;
       auto kernel = full ? pick_grad<T, true>(plan.each, depth, half) : pick_grad<T, false>(plan.each, depth, half);
-      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, row_bytes * depth);
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
       if (e != cudaSuccess) return launched(e);
-      kernel<<<unsigned(plan.ctas), threads, row_bytes * depth, stream>>>(a);
+      kernel<<<unsigned(plan.ctas), threads, bytes, stream>>>(a);
     } else {
       auto kernel = plan.each == 2 ? norm_grad_anywhere_kernel<T, 2> : norm_grad_anywhere_kernel<T, 4>;
       const int pool = plan.high > 1 ? plan.high * 2 * a.cols * 4 : 0;  // (32 KB at most: 256 threads' 16 columns)
