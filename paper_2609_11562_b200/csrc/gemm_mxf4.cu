@@ -67,6 +67,20 @@ __device__ __forceinline__ bool wait_bar(const Params& P, uint32_t bar, uint32_t
   wait_failed();
   return false;
 }
+// The same for a warp that has time: it sleeps between its looks, which leaves the barriers to the warps that have not.
+__device__ __forceinline__ bool idle_wait(const Params& P, uint32_t bar, uint32_t parity, int ns) {
+  unsigned long long t0 = 0;
+  while (!__all_sync(0xffffffffu, mbar_test(bar, parity))) {
+    const unsigned long long now = globaltimer_ns();
+    if (t0 == 0) t0 = now;
+    if (__any_sync(0xffffffffu, now - t0 > P.wait_ns)) {
+      wait_failed();
+      return false;
+    }
+    __nanosleep(ns);
+  }
+  return true;
+}
 // The same by a whole warp.
 __device__ __forceinline__ bool warp_wait(const Params& P, uint32_t bar, uint32_t parity) {
   return __all_sync(0xffffffffu, wait_bar(P, bar, parity));
@@ -307,8 +321,10 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
 // half of the tokens' codes and all of their scales).  Two accumulators in TMEM, 2 x 192 of its 512 columns, so that the
 // epilogue of a tile runs beside the products of the next, and five buffers of scales of 24 columns.  (224 tokens leave
 // room for two: the way from products that are done to the next but one's scales is then longer than the products between.)
-constexpr int kScaleWarps = 4;
-constexpr int kPairThreads = 32 * (2 + 8 + kScaleWarps + 1);  // TMA, MMA, eight epilogue warps, scale warps, their messenger
+// TMA warp, MMA warp, epilogue warps by groups of four, scale warps, their messenger.  (Eight epilogue warps: 59 us instead of
+// 53 for 32 experts' 15.6k rows of 4096 x 1024, where the epilogue is what a tile waits for; 16 have too few registers.)
+constexpr int kEpilogueGroups = 3, kScaleWarps = 4;
+constexpr int kFirstScaleWarp = 2 + 4 * kEpilogueGroups, kPairThreads = 32 * (kFirstScaleWarp + kScaleWarps + 1);
 constexpr int kPairTokens = 192;
 constexpr int kPairCodes = (kChannels + kPairTokens / 2) * kKBytes;  // bytes of a stage
 constexpr int kPairStages = 6;
@@ -323,68 +339,21 @@ constexpr int kPairScaleCol = 2 * kPairTokens;
 constexpr int kPairBuffers = 5;
 static_assert(kPairScaleCol + 24 * kPairBuffers <= 512 && kPairBuffers < kPairStages, "TMEM, and barriers that tell a buffer's last use");
 
-// 32 channels (lanes) x 32 tokens (registers) to C: neighbouring lanes exchange halves until each has four consecutive
-// channels of one token, and eight lanes store a token's 64 or 128 bytes.  (Staging the chunk in shared memory costs twice
-// the shared-memory cycles and two barriers.)  `rows` tokens and `left` channels lie inside C.  All exchanges come before
-// the first store, and whole chunks are stored without a look at their borders: with a branch between them each group of
-// four tokens waited for the one before.
+// 32 channels (lanes) x 32 tokens (registers) to C, token by token: 64 or 128 bytes side by side with each store.  (Lanes
+// that first exchange halves until each has four or eight neighbouring channels store a chunk with 8 or 4 instructions
+// instead of 32: no faster, and 20 % slower with 8.)  `rows` tokens and `left` channels lie inside C.
 template <typename Out>
-__device__ __forceinline__ void store_chunk(const float (&f)[32], Out* out, int64_t ldc, int rows, int left, int step, int lane) {
-  const bool one = lane & 1, two = lane & 2;
-  const int col = lane & ~3;
-  Piece<Out, 4> v[8];  // [i]: token 4 i + lane % 4, channels col to col + 3
+__device__ __forceinline__ void store_chunk(const uint32_t (&v)[32], float add, Out* out, int64_t ldc, int rows, int left,
+                                            int lane) {
+  if (lane >= left) return;
+  out += lane;
+  if (rows >= 32) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int j = 4 * i;
-    if constexpr (sizeof(Out) == 2) {
-      uint32_t w[2];  // per pair of tokens: two channels of one
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float g[2] = {f[j + 2 * h], f[j + 2 * h + 1]};
-        const Piece<Out, 2> p = pack<Out, 2>(g);
-        uint32_t mine;
-        memcpy(&mine, &p, 4);
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
-        w[h] = __byte_perm(mine, other, one ? 0x3276 : 0x5410);
-      }
-      const uint32_t other = __shfl_xor_sync(0xffffffffu, two ? w[0] : w[1], 2);
-      const uint32_t o[2] = {two ? other : w[0], two ? w[1] : other};
-      memcpy(&v[i], o, 8);
-    } else {
-      float w[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float a = f[j + 2 * h], b = f[j + 2 * h + 1];
-        const float other = __shfl_xor_sync(0xffffffffu, one ? a : b, 1);
-        w[2 * h] = one ? other : a;
-        w[2 * h + 1] = one ? b : other;
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float other = __shfl_xor_sync(0xffffffffu, two ? w[e] : w[2 + e], 2);
-        v[i].e[e] = two ? other : w[e];
-        v[i].e[2 + e] = two ? w[2 + e] : other;
-      }
-    }
-  }
-  out += int64_t(lane & 3) * ldc + col;
-  const bool wide = step >= int(4 * sizeof(Out));
-  if (wide && rows >= 32 && left >= 32) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) *reinterpret_cast<Piece<Out, 4>*>(out + 4 * i * ldc) = v[i];
+    for (int j = 0; j < 32; ++j) out[j * ldc] = Elem<Out>::down(__uint_as_float(v[j]) + add);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (4 * i + (lane & 3) >= rows) continue;
-      Out* const at = out + 4 * i * ldc;
-      if (wide && col + 4 <= left) {
-        *reinterpret_cast<Piece<Out, 4>*>(at) = v[i];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (col + e < left) at[e] = v[i].e[e];
-      }
-    }
+    for (int j = 0; j < 32; ++j)
+      if (j < rows) out[j * ldc] = Elem<Out>::down(__uint_as_float(v[j]) + add);
   }
 }
 
@@ -439,7 +408,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(tfull + 8 * a, 1);
-      mbar_init(tempty + 8 * a, 16);
+      mbar_init(tempty + 8 * a, 2 * 4 * kEpilogueGroups);
     }
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -556,18 +525,18 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
       __syncwarp();
       wait_bar(P, drain, 0);
     }
-  } else if (warp < 10) {
+  } else if (warp < kFirstScaleWarp) {
     // Epilogue: a warp owns 32 channels (its lane quarter of the accumulator), a lane one of them; groups of four warps
     // take turns at the 32-token chunks of a tile, a chunk's sums read while the chunk before is worked on.
     const int q = warp & 3, group = (warp - 2) / 4;
-    constexpr int kTurns = (kPairTokens / 32 + 1) / 2;  // chunks of a tile that a group takes, at most
+    constexpr int kTurns = (kPairTokens / 32 + kEpilogueGroups - 1) / kEpilogueGroups;  // chunks of a tile that a group takes, at most
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int t = pair; t < total; t += pairs) {
       const PairTile w = walk.at(t);
       const int n0 = w.n0 + rank * kChannels + q * 32, n = n0 + lane;
       const float add = n < P.N && P.bias ? P.bias[int64_t(w.g) * P.N + n] : 0.0f;
-      if (!warp_wait(P, tfull + 8 * acc, acc_phase)) break;
+      if (!idle_wait(P, tfull + 8 * acc, acc_phase, 100)) break;
       tc_fence_after();
       const int chunks = (w.rows + 31) / 32;
       const uint32_t sums = tmem + (uint32_t(q) << 21) + acc * kPairTokens;
@@ -583,24 +552,22 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
       else release();
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {
-        const int c = group + 2 * i;
+        const int c = group + kEpilogueGroups * i, next = c + kEpilogueGroups;
         if (c < chunks) {
           tmem_ld_wait(v[i % 2]);
-          if (c + 2 < chunks) tmem_ld32(sums + (c + 2) * 32, v[(i + 1) % 2]);
+          if (next < chunks) tmem_ld32(sums + next * 32, v[(i + 1) % 2]);
           else release();
-          float f[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[i % 2][j]) + add;
-          store_chunk<Out>(f, static_cast<Out*>(P.c) + int64_t(w.m0 + c * 32) * P.ldc + n0, P.ldc, w.rows - c * 32, P.N - n0,
-                           P.c_step, lane);
+          store_chunk<Out>(v[i % 2], add, static_cast<Out*>(P.c) + int64_t(w.m0 + c * 32) * P.ldc + n0, P.ldc, w.rows - c * 32,
+                           P.N - n0, lane);
+          __syncwarp();
         }
       }
       if ((acc ^= 1) == 0) acc_phase ^= 1;
     }
-  } else if (warp < 10 + kScaleWarps) {
+  } else if (warp < kFirstScaleWarp + kScaleWarps) {
     // Scales of both operands, as many groups ahead as there is room for: the copies arrive on their group's barrier by
     // themselves.
-    const int w4 = warp - 10;
+    const int w4 = warp - kFirstScaleWarp;
     int group = 0, used = 0;
     uint32_t phase = 0;
     bool ok = true;

@@ -343,7 +343,7 @@ int run_dropout(const DropParams& a, cudaStream_t stream) {
   const bool vec = aligned_rows(a.x, a.ldx, sizeof(T)) && aligned_rows(a.out, a.ldo, sizeof(T)) &&
                    (!a.residual || aligned_rows(a.residual, a.ldr, sizeof(T)));
   // little work: one group a thread, for the latency
-  return a.rows * int64_t(a.cols) < (1 << 20) ? run_dropout_by<T, 1>(a, vec, stream) : run_dropout_by<T, 2>(a, vec, stream);
+  return a.rows * int64_t(a.cols) < (1 << 20) ? run_dropout_by<T, 1>(a, vec, stream) : run_dropout_by<T, 4>(a, vec, stream);
 }
 
 // ------------------------------------------------------------------------------------------
