@@ -654,16 +654,16 @@ int run_pairs(const Maps& maps, Params P, cudaStream_t stream) {
 // The height of the pair tiles.  Four instructions of a tile h tokens high move 32 KB + 128 h bytes through an SM's
 // shared memory (operands written by TMA, read by the tensor core, half of the tokens by either CTA), 256 + h cycles;
 // the products themselves take 2 h.  So a tile costs 256 + h, and the rows of one matrix are cut so that the waves of
-// the pairs cost least together.
-int pair_rows(const Params& P) {
-  if (P.G > 1) return kPairTokens;
+// the pairs cost least together.  Of experts, a tile holds four times the average's rows (twice: 35 us instead of 33 for 64 experts of 16 rows, whose larger ones are then two tiles).
+int pair_rows(const Params& P, int rows) {
+  if (P.G > 1) return std::min(kPairTokens, (4 * rows + 31) / 32 * 32);
   const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels, pairs = sm_count() / 2;
   int best = kPairTokens;
   int64_t least = 0;
-  for (int rows = kPairTokens; rows >= 96; rows -= 32) {
-    const int64_t token_tiles = (P.M + rows - 1) / rows, waves = (token_tiles * channel_tiles + pairs - 1) / pairs;
-    const int64_t cost = waves * (rows + 256);
-    if (least == 0 || cost < least) least = cost, best = rows;
+  for (int high = kPairTokens; high >= 32; high -= 32) {
+    const int64_t token_tiles = (P.M + high - 1) / high, waves = (token_tiles * channel_tiles + pairs - 1) / pairs;
+    const int64_t cost = waves * (high + 256);
+    if (least == 0 || cost < least) least = cost, best = high;
   }
   return best;
 }
@@ -722,11 +722,17 @@ template <typename Out>
 int run_as(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t expert_stride, const Params& P,
            cudaStream_t stream) {
   const int rows = (P.M + P.G - 1) / P.G;  // of an average expert
-  const int64_t pair_tiles = int64_t(std::min(P.G, P.M)) * ((P.N + kPairChannels - 1) / kPairChannels);
+  const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels;
+  const int64_t pair_tiles = int64_t(std::min(P.G, P.M)) * ((rows + kPairTokens - 1) / kPairTokens) * channel_tiles;
   Maps maps;
-  if (rows > 128 ? (rows + 127) / 128 * pair_tiles >= sm_count() / 4 : pair_tiles >= sm_count()) {
+  // Pairs for more than 64 tokens and for experts where there are 16 tiles for them, for fewer tokens where nearly every
+  // pair gets one; else narrow tiles, which share K between CTAs.  In us, pairs and narrow tiles: 32, 64 and 128 tokens
+  // through 8192 x 3584 9.8 10.0 10.3 and 8.7 9.8 12.5; 64 through 16384 x 8192 18.0 and 20.0; 300 through 1024 x 4096 (8
+  // tiles) 10.1 and 8.8; 600 through 1024 x 1024 (16) 7.0 and 9.3; 64 experts of 4096 x 1024 with 1, 4 and 16 rows 23.5 28.3
+  // 32.7 and 31.2 41.4 68.2.
+  if (pair_tiles >= (rows > 64 || P.G > 1 ? 16 : 64)) {
     Params Q = P;
-    Q.tile_rows = pair_rows(P);
+    Q.tile_rows = pair_rows(P, rows);
     if (!make_maps(&maps, A, lda, B, ldb, expert_stride, Q, Q.tile_rows / 2)) return ENTWINE_ERR_CUDA;
     return run_pairs<Out>(maps, Q, stream);
   }
