@@ -498,43 +498,68 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
 
 constexpr int kLongThreads = 512;
 
-// One element of a row: residual + dropout(x), as it is written.
-template <typename T>
-__device__ __forceinline__ float hidden_at(const NormParams& a, const Stream& rng, int64_t row, int col) {
-  float f = Elem<T>::up(static_cast<const T*>(a.x)[row * a.ldx + col]);
-  if (a.d.rng) f = drop1(rng, a.d, a.d.row0 + uint32_t(row), uint32_t(col), f);
-  if (a.residual) f += Elem<T>::up(static_cast<const T*>(a.residual)[row * a.ldr + col]);
-  return rounded<T>(f);
-}
-
-// Rows too long for registers: a CTA reads one three times, element by element.
+// Rows too long for registers: a CTA goes through one three times.  What it normalises it reads again from hidden, or
+// computes again where that is not kept.
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) norm_long_rows_kernel(const NormParams a) {
   __shared__ float part[2][32];
+  const int lane = int(threadIdx.x);
   const int64_t row = blockIdx.x;
   const Stream rng(a.d.rng);
-  float sum = 0.0f;
-  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
-    const float h = hidden_at<T>(a, rng, row, int(c));
-    if (a.hidden) static_cast<T*>(a.hidden)[row * a.ldh + c] = Elem<T>::down(h);
-    sum += h;
+  const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+  const T* const res = a.residual ? static_cast<const T*>(a.residual) + row * a.ldr : nullptr;
+  T* const hidden = a.hidden ? static_cast<T*>(a.hidden) + row * a.ldh : nullptr;
+  T* const out = static_cast<T*>(a.out) + row * a.ldo;
+  constexpr int64_t kStep = int64_t(kLongThreads) * kGroup;
+  auto values = [&](int64_t base, int64_t c, int left, float (&f)[8]) {
+    load_apart(x + c, left, f);
+    if (a.d.rng) {
+      uint32_t w[1][4];
+      rng.words<1>(uint32_t(base / kGroup) + uint32_t(lane), 0, a.d.row0 + uint32_t(row), w);
+      drop_apart(w[0], a.d, lane, f);
+    }
+    float r[8] = {};
+    if (res) load_apart(res + c, left, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = rounded<T>(res ? f[e] + r[e] : f[e]);
+  };
+  float f[8], sum = 0.0f;
+  for (int64_t base = 0; base < a.cols; base += kStep) {
+    const int64_t c = base + first_apart(0, kLongThreads, lane);
+    const int left = int(a.cols - c);
+    values(base, c, left, f);
+    if (hidden) store_apart(hidden + c, left, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += f[e];  // (0 behind the row's end)
   }
   const float mean = row_sum(sum, part[0], 0, kLongThreads / 32) / float(a.cols);
   sum = 0.0f;
-  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
-    const float d = hidden_at<T>(a, rng, row, int(c)) - mean;
-    sum = fmaf(d, d, sum);
+  for (int64_t base = 0; base < a.cols; base += kStep) {
+    const int64_t c = base + first_apart(0, kLongThreads, lane);
+    const int left = int(a.cols - c);
+    if (hidden) load_apart(hidden + c, left, f);
+    else values(base, c, left, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (32 * e < left) sum = fmaf(f[e] - mean, f[e] - mean, sum);
   }
   const float rstd = 1.0f / sqrtf(row_sum(sum, part[1], 0, kLongThreads / 32) / float(a.cols) + a.eps);
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
   }
   const Weights<T> weight{a.weight, a.wide != 0}, bias{a.bias, a.wide != 0};
-  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
-    const float h = hidden_at<T>(a, rng, row, int(c));
-    static_cast<T*>(a.out)[row * a.ldo + c] =
-        Elem<T>::down(fmaf((h - mean) * rstd, weight.one(int(c)), a.bias ? bias.one(int(c)) : 0.0f));
+  for (int64_t base = 0; base < a.cols; base += kStep) {
+    const int64_t c = base + first_apart(0, kLongThreads, lane);
+    const int left = int(a.cols - c);
+    if (hidden) load_apart(hidden + c, left, f);
+    else values(base, c, left, f);
+    float w[8], b[8] = {};
+    weight.apart(int(c), left, w);
+    if (a.bias) bias.apart(int(c), left, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = fmaf((f[e] - mean) * rstd, w[e], b[e]);
+    store_apart(out + c, left, f);
   }
 }
 
@@ -1032,28 +1057,57 @@ auto pick_grad(int each, int depth, bool half) {
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) norm_grad_long_rows_kernel(const GradParams a) {
   __shared__ float2 part[32];
+  const int lane = int(threadIdx.x);
   const int64_t row = blockIdx.x;
   const T* const dout = static_cast<const T*>(a.dout) + row * a.ldo;
   const T* const hidden = static_cast<const T*>(a.hidden) + row * a.ldh;
   const Weights<T> weight{a.weight, a.wide != 0};
   const Stream rng(a.d.rng);
   const float mean = a.mean[row], rstd = a.rstd[row];
+  constexpr int64_t kStep = int64_t(kLongThreads) * kGroup;
+  // g = dout weight and n of a turn's columns; behind the row's end g is 0
+  auto load = [&](int64_t c, int left, float (&g)[8], float (&n)[8]) {
+    float w[8];
+    load_apart(dout + c, left, g);
+    load_apart(hidden + c, left, n);
+    weight.apart(int(c), left, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      g[e] *= w[e];
+      n[e] = (n[e] - mean) * rstd;
+    }
+  };
+  float g[8], n[8];
   float2 s = make_float2(0.0f, 0.0f);
-  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
-    const float g = Elem<T>::up(dout[c]) * weight.one(int(c)), n = (Elem<T>::up(hidden[c]) - mean) * rstd;
-    s.x += g;
-    s.y = fmaf(g, n, s.y);
+  for (int64_t base = 0; base < a.cols; base += kStep) {
+    const int64_t c = base + first_apart(0, kLongThreads, lane);
+    const int left = int(a.cols - c);
+    load(c, left, g, n);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (32 * e < left) {
+        s.x += g[e];
+        s.y = fmaf(g[e], n[e], s.y);
+      }
   }
   s = row_sum2(s, part, 0, kLongThreads / 32);
   s.x /= float(a.cols);
   s.y /= float(a.cols);
-  for (int64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
-    const float g = Elem<T>::up(dout[c]) * weight.one(int(c)), n = (Elem<T>::up(hidden[c]) - mean) * rstd;
-    float f = a.dhidden ? Elem<T>::up(static_cast<const T*>(a.dhidden)[row * a.lddh + c]) : 0.0f;
-    f = fmaf(rstd, g - s.x - n * s.y, f);
-    if (a.dresidual) static_cast<T*>(a.dresidual)[row * a.lddr + c] = Elem<T>::down(f);
-    if (a.d.rng) f = drop1(rng, a.d, a.d.row0 + uint32_t(row), uint32_t(c), f);
-    static_cast<T*>(a.dx)[row * a.lddx + c] = Elem<T>::down(f);
+  for (int64_t base = 0; base < a.cols; base += kStep) {
+    const int64_t c = base + first_apart(0, kLongThreads, lane);
+    const int left = int(a.cols - c);
+    float f[8] = {};
+    load(c, left, g, n);
+    if (a.dhidden) load_apart(static_cast<const T*>(a.dhidden) + row * a.lddh + c, left, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = fmaf(rstd, g[e] - s.x - n[e] * s.y, f[e]);
+    if (a.dresidual) store_apart(static_cast<T*>(a.dresidual) + row * a.lddr + c, left, f);
+    if (a.d.rng) {
+      uint32_t w[1][4];
+      rng.words<1>(uint32_t(base / kGroup) + uint32_t(lane), 0, a.d.row0 + uint32_t(row), w);
+      drop_apart(w[0], a.d, lane, f);
+    }
+    store_apart(static_cast<T*>(a.dx) + row * a.lddx + c, left, f);
   }
 }
 
@@ -1103,7 +1157,9 @@ template <typename T>
 int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t stream) {
   const GradPlan plan = grad_plan(a.rows, a.cols);
   auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-  if (plan.in_registers) {
+  if (a.rows == 0) {
+    // (no parts: the sums are 0)
+  } else if (plan.in_registers) {
     const bool vec = aligned_rows(a.dout, a.ldo, sizeof(T)) && aligned_rows(a.hidden, a.ldh, sizeof(T)) &&
                      aligned_rows(a.dx, a.lddx, sizeof(T)) && (!a.dhidden || aligned_rows(a.dhidden, a.lddh, sizeof(T))) &&
                      (!a.dresidual || aligned_rows(a.dresidual, a.lddr, sizeof(T))) && aligned(a.weight);
@@ -1131,7 +1187,7 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
       kernel<<<unsigned(plan.ctas), threads, pool, stream>>>(a);
     }
   } else {
-    if (a.rows > 0) norm_grad_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
+    norm_grad_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
     const dim3 grid(unsigned((int64_t(a.cols) + 127) / 128), unsigned(plan.ctas));
     norm_grad_columns_kernel<T><<<grid, 128, 0, stream>>>(a, plan.ctas);
   }
@@ -1141,7 +1197,7 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
   const int x = a.cols >= 4096 ? 32 : 8;
   const dim3 grid(unsigned((int64_t(a.cols) + x - 1) / x), dbias ? 2 : 1);
   auto kernel = x == 32 ? norm_sum_kernel<32> : norm_sum_kernel<8>;
-  kernel<<<grid, kSumThreads, 0, stream>>>(a.work, plan.ctas, a.cols, dweight, dbias);
+  kernel<<<grid, kSumThreads, 0, stream>>>(a.work, a.rows > 0 ? plan.ctas : 0, a.cols, dweight, dbias);
   return launched(cudaSuccess);
 }
 
