@@ -65,14 +65,40 @@ struct Stream {
     }
   }
 };
+// Two fp32 values in one register pair, and arithmetic on both at once.
+struct Two {
+  unsigned long long v;
+  Two() = default;
+  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Two add(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two mul(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
 // Number e of a group's eight is at least t: its word, the number shifted to the top, is at least t * 65536.
 __device__ __forceinline__ bool kept(const uint32_t (&c)[4], int e, uint32_t t16) {
   return (e & 1 ? c[e / 2] : c[e / 2] << 16) >= t16;
 }
-// residual + dropout: a dropped element is 0 whatever it held.
+// A dropped element is 0 whatever it held.
 __device__ __forceinline__ void drop8(const uint32_t (&c)[4], const Dropout& d, float (&f)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = kept(c, e, d.t16) ? f[e] * d.scale : 0.0f;
+  for (int j = 0; j < 4; ++j) {
+    const float a = kept(c, 2 * j, d.t16) ? f[2 * j] : 0.0f, b = kept(c, 2 * j + 1, d.t16) ? f[2 * j + 1] : 0.0f;
+    mul(Two(a, b), Two(d.scale)).get(f[2 * j], f[2 * j + 1]);
+  }
 }
 __device__ __forceinline__ float drop1(const Stream& s, const Dropout& d, uint32_t row, uint32_t col, float f) {
   uint32_t c[1][4];
@@ -172,29 +198,6 @@ __device__ __forceinline__ float rounded(float f) {
   return Elem<T>::up(Elem<T>::down(f));
 }
 
-// Two fp32 values in one register pair, and arithmetic on both at once.
-struct Two {
-  unsigned long long v;
-  Two() = default;
-  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-  __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
-  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-};
-__device__ __forceinline__ Two add(Two a, Two b) {
-  Two r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Two mul(Two a, Two b) {
-  Two r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
-  Two r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
 __device__ __forceinline__ void twos(const float (&f)[8], Two (&t)[4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) t[j] = Two(f[2 * j], f[2 * j + 1]);
@@ -236,7 +239,7 @@ struct DropParams {
 
 constexpr int kDropThreads = 256;
 
-// P groups of eight elements a thread; a CTA (threads of a row x rows) goes from rows to rows.  16384 x 4096 bf16: XXDROP.
+// P groups of eight elements a thread; a CTA (threads of a row x rows) goes from rows to rows.  16384 x 4096 bf16: 55 us.
 // The generator takes 18 us of that (its wide multiplications issue at a quarter of the rate), so everything else has to be
 // short: set-up is paid once a thread, and whole groups have no element-wise alternative beside them.
 template <typename T, int P>
