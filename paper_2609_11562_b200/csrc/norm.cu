@@ -1047,13 +1047,18 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_gr
   });
 }
 
-// By depth and threads; four groups a thread only where two rows of 512 such threads fit (16-bit types).
+// By threads (256, 320 or 512) and depth; four groups a thread only where two rows of 512 such threads fit (16-bit types).
+template <typename T, int THREADS, bool FULL>
+auto pick_depth(int depth) {
+  return depth == 3 ? norm_grad_kernel<T, 2, 3, THREADS, FULL> : norm_grad_kernel<T, 2, 2, THREADS, FULL>;
+}
 template <typename T, bool FULL>
-auto pick_grad(int each, int depth, bool half) {
+auto pick_grad(int each, int depth, int threads) {
   if constexpr (sizeof(T) == 2)
     if (each == 4) return norm_grad_kernel<T, 4, 2, kGradThreads, FULL>;
-  if (half) return depth == 3 ? norm_grad_kernel<T, 2, 3, kGradHalf, FULL> : norm_grad_kernel<T, 2, 2, kGradHalf, FULL>;
-  return depth == 3 ? norm_grad_kernel<T, 2, 3, kGradThreads, FULL> : norm_grad_kernel<T, 2, 2, kGradThreads, FULL>;
+  return threads == 256         ? pick_depth<T, 256, FULL>(depth)
+         : threads == kGradHalf ? pick_depth<T, kGradHalf, FULL>(depth)
+                                : pick_depth<T, kGradThreads, FULL>(depth);
 }
 
 // Rows too long for that: dx by a CTA that reads a row twice, ...
@@ -1169,12 +1174,12 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
     const dim3 threads(plan.width, plan.high);
     if (vec && (plan.each == 2 || sizeof(T) == 2)) {
       // three rows where they fit (with two CTAs to an SM, or alone), else two
-      const bool half = plan.each == 2 && plan.width * plan.high <= kGradHalf;
+      const int count = plan.width * plan.high;
+      const int places = plan.each == 4 || count > kGradHalf ? kGradThreads : count > 256 ? kGradHalf : 256;
       const bool full = a.cols == plan.width * plan.each * kGroup;
-      const int row_bytes = (half ? kGradHalf : kGradThreads) * 3 * plan.each * kGroup * int(sizeof(T));
-      const int kept = plan.each == 2 ? (half ? kGradHalf : kGradThreads) * plan.each * kGroup * 4 : 0;
-      const int depth = row_bytes * 3 + kept <= (half ? 112 : 224) * 1024 ? 3 : 2, bytes = row_bytes * depth + kept;
-      auto kernel = full ? pick_grad<T, true>(plan.each, depth, half) : pick_grad<T, false>(plan.each, depth, half);
+      const int row_bytes = places * 3 * plan.each * kGroup * int(sizeof(T)), kept = plan.each == 2 ? places * plan.each * kGroup * 4 : 0;
+      const int depth = row_bytes * 3 + kept <= (places <= kGradHalf ? 112 : 224) * 1024 ? 3 : 2, bytes = row_bytes * depth + kept;
+      auto kernel = full ? pick_grad<T, true>(plan.each, depth, places) : pick_grad<T, false>(plan.each, depth, places);
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
       if (e != cudaSuccess) return launched(e);
       kernel<<<unsigned(plan.ctas), threads, bytes, stream>>>(a);
