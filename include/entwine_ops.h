@@ -7,14 +7,15 @@
  * void* (NULL = the default stream), and device pointers belong to the current device.
  *
  * These calls have no plan: each is complete in itself, keeps nothing from one call for the next, and needs no
- * workspace (but entwine_layer_norm_bwd, whose caller brings it).  Any of them may be captured into a CUDA graph (its first call too), and calls on different streams
- * may overlap as far as their buffers allow.  Outputs must not overlap inputs or each other.  The same inputs give the
+ * workspace (but entwine_layer_norm_bwd, whose caller brings it).  Any of them may be captured into a CUDA graph (its
+ * first call too), and calls on different streams may overlap as far as their buffers allow.  Outputs must not overlap inputs or each other.  The same inputs give the
  * same bits on every call.
  *
  * Matrices are row-major; ld* is the distance between two rows in elements, at least the row's length.  Element
  * pointers need the alignment of their element only, except where a function says more; rows that start on
  * 16-byte boundaries are the fastest (K or H need not fill them).  Contiguous rows of an odd number of 16-bit elements
- * cost the dispatch a tenth more, the return, its gradients and the quantiser about twice as much.
+ * cost the dispatch a tenth more, dropout a third more, the return, its gradients, the quantisers, layer norm and its
+ * gradients about twice as much.
  */
 #ifndef ENTWINE_OPS_H_
 #define ENTWINE_OPS_H_

@@ -135,7 +135,8 @@ struct Scales {
 
 // One tile of 128 channels x TOKENS tokens per cluster of one to eight CTAs, which share the length K: each sums its
 // blocks of K, then the partial sums meet through distributed shared memory, added in the order of the CTAs, each CTA
-// finishing its share of the tokens.  So a decoding step reads the weights with all SMs.
+// finishing its share of the tokens.  So a decoding step reads the weights with all SMs.  16 tokens through 8192 x 3584 take
+// 8.1 us, the weight's 15.6 MB at 2.4 TB/s: start, the latency of the three or four blocks that a CTA has, and the exchange.
 template <int TOKENS, typename Out>
 __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_constant__ Maps maps,
                                                              const __grid_constant__ Params P) {
@@ -321,6 +322,8 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
 // half of the tokens' codes and all of their scales).  Two accumulators in TMEM, 2 x 192 of its 512 columns, so that the
 // epilogue of a tile runs beside the products of the next, and five buffers of scales of 24 columns.  (224 tokens leave
 // room for two: the way from products that are done to the next but one's scales is then longer than the products between.)
+// 8192 x 8192 x 3584 takes 108 to 117 us, up to 4.4 PFLOP/s: 600 to 670 cycles a block of K, of which the products are 384 and
+// the issuing warp's own instructions 330, at a clock that the power limit holds at 1.5 to 1.6 GHz.
 // TMA warp, MMA warp, epilogue warps by groups of four, scale warps, their messenger.  (Eight epilogue warps: 59 us instead of
 // 53 for 32 experts' 15.6k rows of 4096 x 1024, where the epilogue is what a tile waits for; 16 have too few registers.)
 constexpr int kEpilogueGroups = 3, kScaleWarps = 4;
@@ -337,7 +340,8 @@ constexpr int kGroupBytes = 3 * kSectionBytes;                                  
 constexpr int kPairSmem = kPairStages * kPairCodes + kGroups * kGroupBytes + 1024;
 constexpr int kPairScaleCol = 2 * kPairTokens;
 constexpr int kPairBuffers = 5;
-static_assert(kPairScaleCol + 24 * kPairBuffers <= 512 && kPairBuffers < kPairStages, "TMEM, and barriers that tell a buffer's last use");
+static_assert(kPairScaleCol + 24 * kPairBuffers <= 512 && kPairBuffers < kPairStages,
+              "TMEM, and barriers that tell a buffer's last use");
 
 // 32 channels (lanes) x 32 tokens (registers) to C, token by token: 64 or 128 bytes side by side with each store.  (Lanes
 // that first exchange halves until each has four or eight neighbouring channels store a chunk with 8 or 4 instructions
@@ -369,7 +373,8 @@ struct Section {
     count = max(0, min(8, (rows - r + 3) / 4));
   }
   // The group's words, from byte `at` of the rows on; zeros (a scale that nothing is multiplied with) for what is not there.
-  __device__ __forceinline__ void fetch(uint32_t smem, int at, int row_bytes, const uint8_t* somewhere, int warp, int lane) const {
+  __device__ __forceinline__ void fetch(uint32_t smem, int at, int row_bytes, const uint8_t* somewhere, int warp,
+                                        int lane) const {
     const int left = row_bytes - at - lane % 8 * 4, n = left > 0 ? count : 0;
     const uint32_t to = smem + lane % 8 * kWordBytes + warp * 16 + lane / 8 * 4;
     const uint8_t* p = from + at;
@@ -473,13 +478,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
         if (!(ok = warp_wait(P, tempty + 8 * acc, acc_phase ^ 1))) break;
         const uint32_t d = base + acc * kPairTokens;
         int columns = 0;
-        // two blocks at a time: what a turn costs beside the products is paid half as often (one: 671 cycles a block of
-        // 8192 x 8192 x 3584, of which the products are 384)
+        // two blocks at a time: what a turn costs beside the products is paid half as often
         for (int b = 0; b < blocks; b += 2) {
           const bool two = b + 1 < blocks, last = b + 2 >= blocks, group_ends = last || b % kGroupStages == kGroupStages - 2;
           const int next = stage + 1 < S ? stage + 1 : 0, after = next + 1 < S ? next + 1 : 0;
           const uint32_t next_phase = stage + 1 < S ? phase : phase ^ 1, after_phase = next + 1 < S ? next_phase : next_phase ^ 1;
-          ok = (there[0] || wait_bar(P, full + 8 * stage, phase)) && (!two || there[1] || wait_bar(P, full + 8 * next, next_phase));
+          ok = (there[0] || wait_bar(P, full + 8 * stage, phase)) &&
+               (!two || there[1] || wait_bar(P, full + 8 * next, next_phase));
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
           if (b == 0) columns = int(uniform(uint32_t(tile_columns[turn % 8])));
           const uint32_t idesc[2] = {instr_desc_mxf4(columns, kPairChannels, 0), instr_desc_mxf4(columns, kPairChannels, 1)};
@@ -529,7 +534,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
     // Epilogue: a warp owns 32 channels (its lane quarter of the accumulator), a lane one of them; groups of four warps
     // take turns at the 32-token chunks of a tile, a chunk's sums read while the chunk before is worked on.
     const int q = warp & 3, group = (warp - 2) / 4;
-    constexpr int kTurns = (kPairTokens / 32 + kEpilogueGroups - 1) / kEpilogueGroups;  // chunks of a tile that a group takes, at most
+    // chunks of a tile that a group takes, at most
+    constexpr int kTurns = (kPairTokens / 32 + kEpilogueGroups - 1) / kEpilogueGroups;
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int t = pair; t < total; t += pairs) {
@@ -595,8 +601,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
     // The messenger tells rank 0, whose warp has both CTAs' scales copied to TMEM, that this CTA's of a stage are there and
     // that the buffer for them is free: the products that read it, five blocks ago, are done.  The fence makes the words,
     // written by ordinary copies, visible to the tensor core, which reads them in this CTA; by a thread that has copies of
-    // its own under way it would wait for them.  So would an arrival that releases to the cluster: 225 us instead of 134
-    // (8192 x 8192 x 3584).
+    // its own under way it would wait for them (416 us instead of 288 for 8192 x 8192 x 3584).  So would an arrival that releases
+    // to the cluster (225 instead of 134).
     // It also says how wide a tile is, so that rank 0's issuing warp need not walk.
     int stage = 0, group = 0, turn = 0, before = 0;  // before: blocks so far, kPairBuffers at most
     uint32_t phase = 0, group_phase = 0;
@@ -654,7 +660,8 @@ int run_pairs(const Maps& maps, Params P, cudaStream_t stream) {
 // The height of the pair tiles.  Four instructions of a tile h tokens high move 32 KB + 128 h bytes through an SM's
 // shared memory (operands written by TMA, read by the tensor core, half of the tokens by either CTA), 256 + h cycles;
 // the products themselves take 2 h.  So a tile costs 256 + h, and the rows of one matrix are cut so that the waves of
-// the pairs cost least together.  Of experts, a tile holds four times the average's rows (twice: 35 us instead of 33 for 64 experts of 16 rows, whose larger ones are then two tiles).
+// the pairs cost least together.  Of experts, a tile holds four times the average's rows (twice: 35 us instead of 33 for 64
+// experts of 16 rows, whose larger ones are then two tiles).
 int pair_rows(const Params& P, int rows) {
   if (P.G > 1) return std::min(kPairTokens, (4 * rows + 31) / 32 * 32);
   const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels, pairs = sm_count() / 2;

@@ -88,7 +88,9 @@ struct Half {
 };
 
 // Two lanes have a block: its largest magnitude's exponent, two less, is the scale's (6 = 1.5 * 2^2 is the largest code).
-// The product with the inverse power of two is exact as far as the rounding to a code can see.
+// The product with the inverse power of two is exact as far as the rounding to a code can see.  Bound by its instructions,
+// 92 for eight elements, beside the read of x: 4096 x 5120 bf16 take 14.4 us cold, 53 MB, 63 % of the issue slots (four lanes
+// a block, of which each worked the scale out: 27 us).
 template <typename T, int P, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) quant_mxf4_kernel(const Params a) {
   const int lane = int(threadIdx.x), width = int(blockDim.x);
@@ -139,7 +141,8 @@ __device__ __forceinline__ float2 values2(uint32_t codes) {
   return __half22float2(__half2(h));
 }
 
-// Groups of eight values, all of them whole and aligned.
+// Groups of eight values, all of them whole and aligned: 16-byte stores side by side.  4096 x 5120 bf16 take 11.4 us cold, 77 %
+// of the issue slots.
 template <typename T, int P>
 __global__ void __launch_bounds__(kThreads) dequant_mxf4_kernel(const Params a) {
   const int lane = int(threadIdx.x), width = int(blockDim.x);

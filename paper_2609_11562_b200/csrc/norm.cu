@@ -21,7 +21,7 @@ constexpr int64_t kMaxRows = 2147483647;
 // bijection of a 128-bit counter under a 64-bit key.  The counter is (column / 8, row, offset), the key the seed; its
 // four words are eight 16-bit numbers, one for each column.  16 bits decide whether an element is kept with probability
 // 1 - t / 65536 exactly, and what is kept is multiplied with 65536 / (65536 - t): the expectation is exact, p itself is
-// taken to the nearest 2^-16.  With 32 bits an element the generator, 50 instructions a call, would be the bound instead
+// taken to the nearest 2^-16.  With 32 bits an element the generator, 40 instructions a call, would be the bound instead
 // of the memory.
 struct Dropout {
   const int64_t* rng;  // {seed, offset}
@@ -379,7 +379,10 @@ __device__ __forceinline__ float row_sum(float v, float* part, int first_warp, i
 
 // A row in registers: P groups a thread, all of them whole and there (FULL), or up to P and one element of the last,
 // incomplete group.  The mean first, then the mean of the squared distances from it: no difference of large sums.  A CTA is
-// threads of a row x rows.
+// threads of a row x rows.  8192 x 5120 bf16 with dropout and residual take 74 us, 4.5 TB/s, 55 % of the issue slots with 25
+// warps an SM: bound by the latency of a row's chain (loads, two sums) against the registers that hold rows, and by its
+// instructions, 282 for eight columns.  More groups a thread are better (two: 83 us, one: 106): fewer threads meet at a row's
+// sums; two fp32 operations an instruction, 75 us before.
 template <typename T, int P, bool FULL, bool DROP>
 __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const NormParams a) {
   __shared__ float part[2][32];
@@ -637,8 +640,12 @@ __global__ void __launch_bounds__(1024) norm_rows_anywhere_kernel(const NormPara
 template <typename T, bool DROP>
 auto pick_norm(int each, bool full) {
   if (!full)
-    return each == 4 ? norm_rows_kernel<T, 4, false, DROP> : each == 2 ? norm_rows_kernel<T, 2, false, DROP> : norm_rows_kernel<T, 1, false, DROP>;
-  return each == 4 ? norm_rows_kernel<T, 4, true, DROP> : each == 2 ? norm_rows_kernel<T, 2, true, DROP> : norm_rows_kernel<T, 1, true, DROP>;
+    return each == 4   ? norm_rows_kernel<T, 4, false, DROP>
+           : each == 2 ? norm_rows_kernel<T, 2, false, DROP>
+                       : norm_rows_kernel<T, 1, false, DROP>;
+  return each == 4   ? norm_rows_kernel<T, 4, true, DROP>
+         : each == 2 ? norm_rows_kernel<T, 2, true, DROP>
+                     : norm_rows_kernel<T, 1, true, DROP>;
 }
 
 template <typename T>
@@ -853,7 +860,9 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradWide ? 2 : 1) norm_gr
 // The same for rows on 16-byte boundaries (FULL: whose groups are all whole and there).  Every thread copies its own pieces
 // of dout, hidden and dhidden ahead, into places of shared memory that no other thread looks at: D rows are under way or in
 // work, and the only barrier of a row is that of its two sums.  What the second half of a row needs is read again instead of
-// held in registers, the weights (in fp32) too: 96 registers have to do where two CTAs share an SM.
+// held in registers, the weights (in fp32) too: 96 registers have to do where two CTAs share an SM.  8192 x 5120 bf16 with
+// dropout and the residual stream's gradient take 102 us with the sums' launch (5), 4.1 TB/s, half of the issue slots; loads in
+// order instead of copies ahead 236 us, one fp32 operation an instruction and weights from global memory 120.
 template <typename T, int P, int D, int THREADS, bool FULL>
 __global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_grad_kernel(const GradParams a) {
   constexpr int N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
@@ -1149,7 +1158,8 @@ constexpr int kSumThreads = 512;
 
 // The parts' sums added up, in a fixed order: X columns a CTA.
 template <int X>
-__global__ void __launch_bounds__(kSumThreads) norm_sum_kernel(const float* work, int parts, int cols, float* dweight, float* dbias) {
+__global__ void __launch_bounds__(kSumThreads) norm_sum_kernel(const float* work, int parts, int cols, float* dweight,
+                                                               float* dbias) {
   constexpr int Y = kSumThreads / X;
   __shared__ float sums[Y][X + 1];
   const int x = int(threadIdx.x) % X, y = int(threadIdx.x) / X;
@@ -1185,8 +1195,10 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
       const int count = plan.width * plan.high;
       const int places = plan.each == 4 || count > kGradHalf ? kGradThreads : count > 256 ? kGradHalf : 256;
       const bool full = a.cols == plan.width * plan.each * kGroup;
-      const int row_bytes = places * 3 * plan.each * kGroup * int(sizeof(T)), kept = plan.each == 2 ? places * plan.each * kGroup * 4 : 0;
-      const int depth = row_bytes * 3 + kept <= (places <= kGradHalf ? 112 : 224) * 1024 ? 3 : 2, bytes = row_bytes * depth + kept;
+      const int row_bytes = places * 3 * plan.each * kGroup * int(sizeof(T));
+      const int kept = plan.each == 2 ? places * plan.each * kGroup * 4 : 0;  // weights
+      const int depth = row_bytes * 3 + kept <= (places <= kGradHalf ? 112 : 224) * 1024 ? 3 : 2;
+      const int bytes = row_bytes * depth + kept;
       auto kernel = full ? pick_grad<T, true>(plan.each, depth, places) : pick_grad<T, false>(plan.each, depth, places);
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
       if (e != cudaSuccess) return launched(e);
