@@ -103,3 +103,6 @@ def test_both_products_failures_are_counted_together(withheld):
     E.gemm_i8(i, one, i, one, out)
     withheld.off()
     assert before < after_one < E.ops_failed_waits()
+    with pytest.raises(E.EntwineError):  # (this thread is told once, so that later queries start anew)
+        E.ops_status()
+    E.ops_status()
