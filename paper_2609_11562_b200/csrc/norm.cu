@@ -754,6 +754,7 @@ __device__ __forceinline__ float2 row_sum2(float2 v, float2* part, int first_war
 template <typename F>
 __device__ __forceinline__ void put_sums(const GradParams& a, float* pool, int slot, int high, const F& put) {
   float* const part = a.work + int64_t(blockIdx.x) * 2 * a.cols;
+  grid_let_next_start();  // (the launch that adds the parts; it waits for them)
   if (high == 1) {
     put(part);
     return;
@@ -1166,6 +1167,7 @@ __global__ void __launch_bounds__(kSumThreads) norm_sum_kernel(const float* work
   const int64_t c = int64_t(blockIdx.x) * X + x;
   const float* const in = work + int64_t(blockIdx.y) * cols + c;
   float v = 0.0f;
+  grid_wait();
   if (c < cols) {
 #pragma unroll 8
     for (int i = y; i < parts; i += Y) v += in[int64_t(i) * 2 * cols];
@@ -1225,8 +1227,17 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
   const int x = a.cols >= 4096 ? 32 : 8;
   const dim3 grid(unsigned((int64_t(a.cols) + x - 1) / x), dbias ? 2 : 1);
   auto kernel = x == 32 ? norm_sum_kernel<32> : norm_sum_kernel<8>;
-  kernel<<<grid, kSumThreads, 0, stream>>>(a.work, a.rows > 0 ? plan.ctas : 0, a.cols, dweight, dbias);
-  return launched(cudaSuccess);
+  // It may start while the parts' launch ends, and waits for it: 777 x 1021 fp32 in 12.1 us instead of 12.9.
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kSumThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = a.rows > 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return launched(cudaLaunchKernelEx(&cfg, kernel, static_cast<const float*>(a.work), a.rows > 0 ? plan.ctas : 0, a.cols, dweight, dbias));
 }
 
 bool floating(int dtype) { return dtype == ENTWINE_BF16 || dtype == ENTWINE_FP16 || dtype == ENTWINE_FP32; }
