@@ -12,6 +12,7 @@
 #include "gemm_tiles.cuh"
 #include "ops_common.cuh"
 #include "sm100.cuh"
+#include "tile_rows.h"
 
 namespace entwine {
 namespace {
@@ -660,10 +661,9 @@ int run_pairs(const Maps& maps, Params P, cudaStream_t stream) {
 // The height of the pair tiles.  Four instructions of a tile h tokens high move 32 KB + 128 h bytes through an SM's
 // shared memory (operands written by TMA, read by the tensor core, half of the tokens by either CTA), 256 + h cycles;
 // the products themselves take 2 h.  So a tile costs 256 + h, and the rows of one matrix are cut so that the waves of
-// the pairs cost least together.  Of experts, a tile holds four times the average's rows (twice: 35 us instead of 33 for 64
-// experts of 16 rows, whose larger ones are then two tiles).
+// the pairs cost least together.  Of experts: expert_tile_rows().
 int pair_rows(const Params& P, int rows) {
-  if (P.G > 1) return std::min(kPairTokens, (4 * rows + 31) / 32 * 32);
+  if (P.G > 1) return expert_tile_rows(rows, kPairTokens);
   const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels, pairs = sm_count() / 2;
   int best = kPairTokens;
   int64_t least = 0;
