@@ -368,13 +368,14 @@ struct NormParams {
 };
 
 // Sum over the threads of a row: whole warps, threadIdx.x of them, from the CTA's warp first_warp on.
-__device__ __forceinline__ float row_sum(float v, float* part, int first_warp, int warps) {
+template <typename F>
+__device__ __forceinline__ F row_sum(F v, F* part, int first_warp, int warps) {
   v = warp_sum(v);
   if (warps == 1) return v;
   const int lane = threadIdx.x & 31;
   if (lane == 0) part[first_warp + threadIdx.x / 32] = v;
   __syncthreads();
-  return warp_sum(lane < warps ? part[first_warp + lane] : 0.0f);
+  return warp_sum(lane < warps ? part[first_warp + lane] : F(0));
 }
 
 // A row in registers: P groups a thread, all of them whole and there (FULL), or up to P and one element of the last,
@@ -505,10 +506,11 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 1024) norm_rows_kernel(const No
 constexpr int kLongThreads = 512;
 
 // Rows too long for registers: a CTA goes through one three times.  What it normalises it reads again from hidden, or
-// computes again where that is not kept.
+// computes again where that is not kept.  A thread adds up the eight values of a turn in fp32, the turns in 64 bits: in
+// fp32, which rounds equal values to the same side again and again, the mean of 2^24 of them was off by 2.6e-4 of it.
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) norm_long_rows_kernel(const NormParams a) {
-  __shared__ float part[2][32];
+  __shared__ double part[2][32];
   const int lane = int(threadIdx.x);
   const int64_t row = blockIdx.x;
   const Stream rng(a.d.rng);
@@ -529,27 +531,32 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_rows_kernel(const Norm
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = rounded<T>(res ? f[e] + r[e] : f[e]);
   };
-  float f[8], sum = 0.0f;
+  float f[8];
+  double sum = 0.0;
   for (int64_t base = 0; base < a.cols; base += kStep) {
     const int64_t c = base + first_apart(0, kLongThreads, lane);
     const int left = int(a.cols - c);
     values(base, c, left, f);
     if (hidden) store_apart(hidden + c, left, f);
+    float turn = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += f[e];  // (0 behind the row's end)
+    for (int e = 0; e < 8; ++e) turn += f[e];  // (0 behind the row's end)
+    sum += turn;
   }
-  const float mean = row_sum(sum, part[0], 0, kLongThreads / 32) / float(a.cols);
-  sum = 0.0f;
+  const float mean = float(row_sum(sum, part[0], 0, kLongThreads / 32) / a.cols);
+  sum = 0.0;
   for (int64_t base = 0; base < a.cols; base += kStep) {
     const int64_t c = base + first_apart(0, kLongThreads, lane);
     const int left = int(a.cols - c);
     if (hidden) load_apart(hidden + c, left, f);
     else values(base, c, left, f);
+    float turn = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (32 * e < left) sum = fmaf(f[e] - mean, f[e] - mean, sum);
+      if (32 * e < left) turn = fmaf(f[e] - mean, f[e] - mean, turn);
+    sum += turn;
   }
-  const float rstd = 1.0f / sqrtf(row_sum(sum, part[1], 0, kLongThreads / 32) / float(a.cols) + a.eps);
+  const float rstd = 1.0f / sqrtf(float(row_sum(sum, part[1], 0, kLongThreads / 32) / a.cols) + a.eps);
   if (lane == 0) {
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
@@ -1079,10 +1086,10 @@ auto pick_grad(int each, int depth, int threads) {
                                 : pick_depth<T, kGradThreads, FULL>(depth);
 }
 
-// Rows too long for that: dx by a CTA that reads a row twice, ...
+// Rows too long for that: dx by a CTA that reads a row twice (its two sums as in norm_long_rows_kernel), ...
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) norm_grad_long_rows_kernel(const GradParams a) {
-  __shared__ float2 part[32];
+  __shared__ double part[2][32];
   const int lane = int(threadIdx.x);
   const int64_t row = blockIdx.x;
   const T* const dout = static_cast<const T*>(a.dout) + row * a.ldo;
@@ -1104,21 +1111,23 @@ __global__ void __launch_bounds__(kLongThreads) norm_grad_long_rows_kernel(const
     }
   };
   float g[8], n[8];
-  float2 s = make_float2(0.0f, 0.0f);
+  double sum = 0.0, dot = 0.0;
   for (int64_t base = 0; base < a.cols; base += kStep) {
     const int64_t c = base + first_apart(0, kLongThreads, lane);
     const int left = int(a.cols - c);
     load(c, left, g, n);
+    float2 turn = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (32 * e < left) {
-        s.x += g[e];
-        s.y = fmaf(g[e], n[e], s.y);
+        turn.x += g[e];
+        turn.y = fmaf(g[e], n[e], turn.y);
       }
+    sum += turn.x;
+    dot += turn.y;
   }
-  s = row_sum2(s, part, 0, kLongThreads / 32);
-  s.x /= float(a.cols);
-  s.y /= float(a.cols);
+  const float2 s = make_float2(float(row_sum(sum, part[0], 0, kLongThreads / 32) / a.cols),
+                               float(row_sum(dot, part[1], 0, kLongThreads / 32) / a.cols));
   for (int64_t base = 0; base < a.cols; base += kStep) {
     const int64_t c = base + first_apart(0, kLongThreads, lane);
     const int left = int(a.cols - c);
