@@ -707,16 +707,24 @@ struct GradParams {
   Dropout d;
 };
 
-// How the rows are spread: every CTA gives a part of the sums.
+// How the rows are spread: every CTA gives a part of the sums.  `ctas` is the most of them that any type and alignment of
+// these extents launches; the workspace has room for so many.
 struct GradPlan {
   int each, width, high, ctas;  // groups of eight columns a thread, threads of a row, rows of a CTA at a time
   bool in_registers;
 };
 
 constexpr int kGradThreads = 512;        // at most
-constexpr int kGradHalf = 320;           // at most, where two CTAs and their rows share an SM
+constexpr int kGradHalf = 320;           // at most, where two CTAs and their rows of 16-bit elements share an SM
+constexpr int kGradHalfWide = 256;       // at most, where two and their rows of fp32 do
 constexpr int kGradWide = 352;           // at most, where two CTAs without rows in shared memory do
+constexpr int kGradSms = 148;             // (the extents alone say how large the workspace is)
 constexpr int kStripRows = 64;           // rows of a part where the columns are summed by themselves
+// Two CTAs of the kernel that copies rows ahead share an SM.
+template <typename T>
+constexpr bool two_copy(int threads) {
+  return threads <= (sizeof(T) == 2 ? kGradHalf : kGradHalfWide);
+}
 
 GradPlan grad_plan(int64_t rows, int64_t cols) {
   GradPlan g;
@@ -732,7 +740,7 @@ GradPlan grad_plan(int64_t rows, int64_t cols) {
   g.width = int((groups + g.each * 32 - 1) / (g.each * 32)) * 32;
   g.high = std::max(1, 256 / g.width);
   const int resident = g.each == 2 && g.width <= kGradWide ? 2 : 1;
-  g.ctas = int(std::min<int64_t>((rows + g.high - 1) / g.high, int64_t(resident) * 148));
+  g.ctas = int(std::min<int64_t>((rows + g.high - 1) / g.high, int64_t(resident) * kGradSms));
   g.ctas = std::max(1, g.ctas);
   return g;
 }
@@ -872,7 +880,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradWide ? 2 : 1) norm_gr
 // dropout and the residual stream's gradient take 102 us with the sums' launch (5), 4.1 TB/s, half of the issue slots; loads in
 // order instead of copies ahead 236 us, one fp32 operation an instruction and weights from global memory 120.
 template <typename T, int P, int D, int THREADS, bool FULL>
-__global__ void __launch_bounds__(THREADS, THREADS <= kGradHalf ? 2 : 1) norm_grad_kernel(const GradParams a) {
+__global__ void __launch_bounds__(THREADS, two_copy<T>(THREADS) ? 2 : 1) norm_grad_kernel(const GradParams a) {
   constexpr int N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
   constexpr bool KEPT = P == 2;  // weights kept in shared memory, fp32, behind the rows
   extern __shared__ __align__(16) uint8_t ring[];
@@ -1193,9 +1201,9 @@ __global__ void __launch_bounds__(kSumThreads) norm_sum_kernel(const float* work
 template <typename T>
 int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t stream) {
   const GradPlan plan = grad_plan(a.rows, a.cols);
+  int parts = a.rows > 0 ? plan.ctas : 0;  // (of no rows the sums are 0)
   auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
   if (a.rows == 0) {
-    // (no parts: the sums are 0)
   } else if (plan.in_registers) {
     const bool vec = aligned_rows(a.dout, a.ldo, sizeof(T)) && aligned_rows(a.hidden, a.ldh, sizeof(T)) &&
                      aligned_rows(a.dx, a.lddx, sizeof(T)) && (!a.dhidden || aligned_rows(a.dhidden, a.lddh, sizeof(T))) &&
@@ -1205,6 +1213,9 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
       // three rows where they fit (with two CTAs to an SM, or alone), else two
       const int count = plan.width * plan.high;
       const int places = plan.each == 4 || count > kGradHalf ? kGradThreads : count > 256 ? kGradHalf : 256;
+      // no more CTAs than the GPU holds at once: others would begin when these end (8192 x 5632 bf16 114 us instead of 124,
+      // 4096 x 5120 fp32 116 instead of 120)
+      if (!two_copy<T>(places)) parts = std::min(parts, kGradSms);
       const bool full = a.cols == plan.width * plan.each * kGroup;
       const int row_bytes = places * 3 * plan.each * kGroup * int(sizeof(T));
       const int kept = plan.each == 2 ? places * plan.each * kGroup * 4 : 0;  // weights
@@ -1213,7 +1224,7 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
       auto kernel = full ? pick_grad<T, true>(plan.each, depth, places) : pick_grad<T, false>(plan.each, depth, places);
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
       if (e != cudaSuccess) return launched(e);
-      kernel<<<unsigned(plan.ctas), threads, bytes, stream>>>(a);
+      kernel<<<unsigned(parts), threads, bytes, stream>>>(a);
     } else {
       // (the registers of 256 threads hold what spills with 352, 45 and 54 us for 8192 rows of 1021 bf16; but two CTAs of up to
       // 352 are worth it, 217 us instead of 267 for 8192 rows of 5121)
@@ -1223,12 +1234,12 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
                     : count <= kGradWide ? norm_grad_anywhere_kernel<T, 2, kGradWide>
                                          : norm_grad_anywhere_kernel<T, 2, kGradThreads>;
       const int pool = plan.high > 1 ? plan.high * 2 * a.cols * 4 : 0;  // (32 KB at most: 256 threads' 16 columns)
-      kernel<<<unsigned(plan.ctas), threads, pool, stream>>>(a);
+      kernel<<<unsigned(parts), threads, pool, stream>>>(a);
     }
   } else {
     norm_grad_long_rows_kernel<T><<<unsigned(a.rows), kLongThreads, 0, stream>>>(a);
-    const dim3 grid(unsigned((int64_t(a.cols) + 127) / 128), unsigned(plan.ctas));
-    norm_grad_columns_kernel<T><<<grid, 128, 0, stream>>>(a, plan.ctas);
+    const dim3 grid(unsigned((int64_t(a.cols) + 127) / 128), unsigned(parts));
+    norm_grad_columns_kernel<T><<<grid, 128, 0, stream>>>(a, parts);
   }
   const int rc = launched(cudaSuccess);
   if (rc != ENTWINE_OK) return rc;
@@ -1246,7 +1257,7 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
   attr[0].val.programmaticStreamSerializationAllowed = a.rows > 0;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return launched(cudaLaunchKernelEx(&cfg, kernel, static_cast<const float*>(a.work), a.rows > 0 ? plan.ctas : 0, a.cols, dweight, dbias));
+  return launched(cudaLaunchKernelEx(&cfg, kernel, static_cast<const float*>(a.work), parts, a.cols, dweight, dbias));
 }
 
 bool floating(int dtype) { return dtype == ENTWINE_BF16 || dtype == ENTWINE_FP16 || dtype == ENTWINE_FP32; }
