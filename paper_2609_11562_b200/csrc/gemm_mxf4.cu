@@ -54,13 +54,14 @@ struct Params {
 
 __device__ __noinline__ void wait_failed() { atomicAdd(&g_waits_failed, 1ull); }
 
-// Bounded wait for a phase of a barrier.
+// Bounded wait for a phase of a barrier; CLUSTER: of one that the other CTA arrives at, too.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait_bar(const Params& P, uint32_t bar, uint32_t parity) {
   unsigned long long t0 = 0;
   for (;;) {
 #pragma unroll 1
     for (int i = 0; i < 128; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
+      if (CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
     const unsigned long long now = globaltimer_ns();
     if (t0 == 0) t0 = now;
     if (now - t0 > P.wait_ns) break;
@@ -83,8 +84,9 @@ __device__ __forceinline__ bool idle_wait(const Params& P, uint32_t bar, uint32_
   return true;
 }
 // The same by a whole warp.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(const Params& P, uint32_t bar, uint32_t parity) {
-  return __all_sync(0xffffffffu, wait_bar(P, bar, parity));
+  return __all_sync(0xffffffffu, wait_bar<CLUSTER>(P, bar, parity));
 }
 
 template <int TOKENS>
@@ -390,7 +392,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
                                                                          const __grid_constant__ Params P) {
   constexpr int S = kPairStages;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * S + 2 * kGroups + 5];
+  __shared__ __align__(8) uint64_t bars[2 * S + 3 * kGroups + 5];
   __shared__ uint32_t tmem_slot;
   __shared__ int tile_columns[8];
   __shared__ PairGroups groups;
@@ -398,19 +400,20 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
   const int rank = int(cluster_ctarank());
   const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u;
   const uint32_t full = smem_u32(bars), empty = full + 8 * S, tfull = full + 16 * S, tempty = tfull + 16,
-                 drain = tempty + 16, scaled = drain + 8, sempty = scaled + 8 * kGroups;
+                 drain = tempty + 16, scaled = drain + 8, sempty = scaled + 8 * kGroups, far = sempty + 8 * kGroups;
   const uint32_t scale_ring = ring + S * kPairCodes;
 
   if (threadIdx.x == 0) {
     tma_prefetch_map(&maps.a);
     tma_prefetch_map(&maps.b);
     for (int s = 0; s < S; ++s) {
-      mbar_init(full + 8 * s, 1 + 2);  // the codes, both CTAs' scales
+      mbar_init(full + 8 * s, 1 + 1);  // both CTAs' codes, rank 0's scales
       mbar_init(empty + 8 * s, 1);
     }
     for (int s = 0; s < kGroups; ++s) {
       mbar_init(scaled + 8 * s, 32 * kScaleWarps);
       mbar_init(sempty + 8 * s, 1);
+      mbar_init(far + 8 * s, 1);  // rank 1's scales
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(tfull + 8 * a, 1);
@@ -473,10 +476,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
       const uint32_t base = uniform(tmem);
       const int tiles = int(uniform(uint32_t(total)));
       int stage = 0, acc = 0, turn = 0, group = 0;
-      uint32_t phase = 0, acc_phase = 0, buffer = 0;
+      uint32_t phase = 0, acc_phase = 0, group_phase = 0, buffer = 0;
       bool ok = true, there[2] = {false, false};
       for (int t = pair; ok && t < tiles; t += pairs, ++turn) {
-        if (!(ok = warp_wait(P, tempty + 8 * acc, acc_phase ^ 1))) break;
+        if (!(ok = warp_wait<true>(P, tempty + 8 * acc, acc_phase ^ 1))) break;
         const uint32_t d = base + acc * kPairTokens;
         int columns = 0;
         // two blocks at a time: what a turn costs beside the products is paid half as often
@@ -484,15 +487,16 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
           const bool two = b + 1 < blocks, last = b + 2 >= blocks, group_ends = last || b % kGroupStages == kGroupStages - 2;
           const int next = stage + 1 < S ? stage + 1 : 0, after = next + 1 < S ? next + 1 : 0;
           const uint32_t next_phase = stage + 1 < S ? phase : phase ^ 1, after_phase = next + 1 < S ? next_phase : next_phase ^ 1;
-          ok = (there[0] || wait_bar(P, full + 8 * stage, phase)) &&
-               (!two || there[1] || wait_bar(P, full + 8 * next, next_phase));
+          ok = (there[0] || wait_bar<true>(P, full + 8 * stage, phase)) &&
+               (!two || there[1] || wait_bar<true>(P, full + 8 * next, next_phase)) &&
+               (b % kGroupStages != 0 || wait_bar<true>(P, far + 8 * group, group_phase));
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
           if (b == 0) columns = int(uniform(uint32_t(tile_columns[turn % 8])));
           const uint32_t idesc[2] = {instr_desc_mxf4(columns, kPairChannels, 0), instr_desc_mxf4(columns, kPairChannels, 1)};
           // (a look at the next blocks' barriers takes as long as the issue of these products: both at once)
           const int third = after + 1 < S ? after + 1 : 0;
-          there[0] = mbar_test(full + 8 * (two ? after : next), two ? after_phase : next_phase);
-          there[1] = mbar_test(full + 8 * (two ? third : after), two && after + 1 == S ? after_phase ^ 1 : after_phase);
+          there[0] = mbar_test_cluster(full + 8 * (two ? after : next), two ? after_phase : next_phase);
+          there[1] = mbar_test_cluster(full + 8 * (two ? third : after), two && after + 1 == S ? after_phase ^ 1 : after_phase);
           tc_fence_after();
           auto products = [&](int s, uint32_t buf, int word, bool first) {
             const uint32_t at = ring + s * kPairCodes, scales = base + kPairScaleCol + buf * 24;
@@ -522,7 +526,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
           buffer = !two ? next_buffer : next_buffer + 1 < kPairBuffers ? next_buffer + 1 : 0;
           stage = two ? after : next;
           phase = two ? after_phase : next_phase;
-          if (group_ends && ++group == kGroups) group = 0;
+          if (group_ends && ++group == kGroups) group = 0, group_phase ^= 1;
         }
         if ((acc ^= 1) == 0) acc_phase ^= 1;
       }
@@ -599,32 +603,47 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
     // the last arrival that says that a group has been used has come
     if (ok && used) wait_bar(P, sempty + 8 * (group > 0 ? group - 1 : kGroups - 1), group > 0 ? phase : phase ^ 1);
   } else {
-    // The messenger tells rank 0, whose warp has both CTAs' scales copied to TMEM, that this CTA's of a stage are there and
-    // that the buffer for them is free: the products that read it, five blocks ago, are done.  The fence makes the words,
-    // written by ordinary copies, visible to the tensor core, which reads them in this CTA; by a thread that has copies of
-    // its own under way it would wait for them (416 us instead of 288 for 8192 x 8192 x 3584).  So would an arrival that releases
-    // to the cluster (225 instead of 134).
-    // It also says how wide a tile is, so that rank 0's issuing warp need not walk.
-    int stage = 0, group = 0, turn = 0, before = 0;  // before: blocks so far, kPairBuffers at most
-    uint32_t phase = 0, group_phase = 0;
+    // The messengers tell rank 0's issuing warp, which has both CTAs' scales copied to TMEM, that they are there.  Their fence
+    // makes the words, written by ordinary copies, visible to the tensor core, which reads them in this CTA; by a thread that
+    // has copies of its own under way it would wait for them (416 us instead of 288 for 8192 x 8192 x 3584).  What rank 1's
+    // hands over to the other CTA it releases to the cluster, where it is acquired.  That takes long, so it comes once a group,
+    // as soon as the words are there, ahead of the products (from block to block: 244 us instead of 118).
+    int group = 0;
+    uint32_t group_phase = 0;
     bool ok = true;
-    for (int t = pair; ok && t < total; t += pairs, ++turn) {
-      if (lane == 0) tile_columns[turn % 8] = (walk.at(t).rows + 31) / 32 * 32;
-      for (int b = 0; b < blocks; ++b) {
-        if (b % kGroupStages == 0) {
+    if (rank == 1) {
+      for (int t = pair; ok && t < total; t += pairs) {
+        for (int b = 0; b < blocks; b += kGroupStages) {
           if (!(ok = warp_wait(P, scaled + 8 * group, group_phase))) break;
-          if (++group == kGroups) group = 0, group_phase ^= 1;
           fence_async_smem();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(far + 8 * group, 0));
+          __syncwarp();
+          if (++group == kGroups) group = 0, group_phase ^= 1;
         }
-        if (before == kPairBuffers) {
-          const int s = stage >= kPairBuffers ? stage - kPairBuffers : stage + S - kPairBuffers;
-          if (!(ok = warp_wait(P, empty + 8 * s, stage >= kPairBuffers ? phase : phase ^ 1))) break;
-        } else {
-          ++before;
+      }
+    } else {
+      // Rank 0's says it stage by stage, when the buffer for a stage's scales is free: the products that read it (in both CTAs),
+      // five blocks ago, are done.  It also says how wide a tile is, so that the issuing warp need not walk.
+      int stage = 0, turn = 0, before = 0;  // before: blocks so far, kPairBuffers at most
+      uint32_t phase = 0;
+      for (int t = pair; ok && t < total; t += pairs, ++turn) {
+        if (lane == 0) tile_columns[turn % 8] = (walk.at(t).rows + 31) / 32 * 32;
+        for (int b = 0; b < blocks; ++b) {
+          if (b % kGroupStages == 0) {
+            if (!(ok = warp_wait(P, scaled + 8 * group, group_phase))) break;
+            if (++group == kGroups) group = 0, group_phase ^= 1;
+            fence_async_smem();
+          }
+          if (before == kPairBuffers) {
+            const int s = stage >= kPairBuffers ? stage - kPairBuffers : stage + S - kPairBuffers;
+            if (!(ok = warp_wait(P, empty + 8 * s, stage >= kPairBuffers ? phase : phase ^ 1))) break;
+          } else {
+            ++before;
+          }
+          if (lane == 0) mbar_arrive(full + 8 * stage);
+          __syncwarp();
+          if (++stage == S) stage = 0, phase ^= 1;
         }
-        if (lane == 0) mbar_arrive_there(map_to_cta(full + 8 * stage, 0));
-        __syncwarp();
-        if (++stage == S) stage = 0, phase ^= 1;
       }
     }
   }
