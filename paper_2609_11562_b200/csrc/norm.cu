@@ -720,10 +720,21 @@ constexpr int kGradHalfWide = 256;       // at most, where two and their rows of
 constexpr int kGradWide = 352;           // at most, where two CTAs without rows in shared memory do
 constexpr int kGradSms = 148;             // (the extents alone say how large the workspace is)
 constexpr int kStripRows = 64;           // rows of a part where the columns are summed by themselves
-// Two CTAs of the kernel that copies rows ahead share an SM.
+// Two CTAs of the kernel that copies rows ahead share an SM (registers, and shared memory: 88 and 110 KB of 16-bit elements, 112
+// KB of fp32).
 template <typename T>
 constexpr bool two_copy(int threads) {
   return threads <= (sizeof(T) == 2 ? kGradHalf : kGradHalfWide);
+}
+// Rows that it has under way or in work with `each` groups a thread: as many as the SM's shared memory holds.
+template <typename T>
+__host__ __device__ constexpr int copy_depth(int each) {
+  return sizeof(T) == 2 && each == 2 ? 3 : 2;
+}
+// Its shared memory for `places` threads: those rows' dout, hidden and dhidden; the weights, in fp32, with two groups.
+template <typename T>
+constexpr int copy_bytes(int each, int places) {
+  return places * each * kGroup * (3 * copy_depth<T>(each) * int(sizeof(T)) + (each == 2 ? 4 : 0));
 }
 
 GradPlan grad_plan(int64_t rows, int64_t cols) {
@@ -879,9 +890,9 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kGradWide ? 2 : 1) norm_gr
 // held in registers, the weights (in fp32) too: 96 registers have to do where two CTAs share an SM.  8192 x 5120 bf16 with
 // dropout and the residual stream's gradient take 102 us with the sums' launch (5), 4.1 TB/s, half of the issue slots; loads in
 // order instead of copies ahead 236 us, one fp32 operation an instruction and weights from global memory 120.
-template <typename T, int P, int D, int THREADS, bool FULL>
+template <typename T, int P, int THREADS, bool FULL>
 __global__ void __launch_bounds__(THREADS, two_copy<T>(THREADS) ? 2 : 1) norm_grad_kernel(const GradParams a) {
-  constexpr int N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
+  constexpr int D = copy_depth<T>(P), N = Raw<T>::N, V = Raw<T>::V, kRow = 3 * P * N * THREADS;  // 16-byte places of a row
   constexpr bool KEPT = P == 2;  // weights kept in shared memory, fp32, behind the rows
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float2 part[2][32];
@@ -1080,18 +1091,14 @@ __global__ void __launch_bounds__(THREADS, two_copy<T>(THREADS) ? 2 : 1) norm_gr
   });
 }
 
-// By threads (256, 320 or 512) and depth; four groups a thread only where two rows of 512 such threads fit (16-bit types).
-template <typename T, int THREADS, bool FULL>
-auto pick_depth(int depth) {
-  return depth == 3 ? norm_grad_kernel<T, 2, 3, THREADS, FULL> : norm_grad_kernel<T, 2, 2, THREADS, FULL>;
-}
+// By threads (256, 320 or 512); four groups a thread only where two rows of 512 such threads fit (16-bit types).
 template <typename T, bool FULL>
-auto pick_grad(int each, int depth, int threads) {
+auto pick_grad(int each, int threads) {
   if constexpr (sizeof(T) == 2)
-    if (each == 4) return norm_grad_kernel<T, 4, 2, kGradThreads, FULL>;
-  return threads == 256         ? pick_depth<T, 256, FULL>(depth)
-         : threads == kGradHalf ? pick_depth<T, kGradHalf, FULL>(depth)
-                                : pick_depth<T, kGradThreads, FULL>(depth);
+    if (each == 4) return norm_grad_kernel<T, 4, kGradThreads, FULL>;
+  return threads == 256         ? norm_grad_kernel<T, 2, 256, FULL>
+         : threads == kGradHalf ? norm_grad_kernel<T, 2, kGradHalf, FULL>
+                                : norm_grad_kernel<T, 2, kGradThreads, FULL>;
 }
 
 // Rows too long for that: dx by a CTA that reads a row twice (its two sums as in norm_long_rows_kernel), ...
@@ -1210,18 +1217,14 @@ int run_grad(const GradParams& a, float* dweight, float* dbias, cudaStream_t str
                      (!a.dresidual || aligned_rows(a.dresidual, a.lddr, sizeof(T))) && aligned(a.weight);
     const dim3 threads(plan.width, plan.high);
     if (vec && (plan.each == 2 || sizeof(T) == 2)) {
-      // three rows where they fit (with two CTAs to an SM, or alone), else two
       const int count = plan.width * plan.high;
       const int places = plan.each == 4 || count > kGradHalf ? kGradThreads : count > 256 ? kGradHalf : 256;
       // no more CTAs than the GPU holds at once: others would begin when these end (8192 x 5632 bf16 114 us instead of 124,
       // 4096 x 5120 fp32 116 instead of 120)
       if (!two_copy<T>(places)) parts = std::min(parts, kGradSms);
       const bool full = a.cols == plan.width * plan.each * kGroup;
-      const int row_bytes = places * 3 * plan.each * kGroup * int(sizeof(T));
-      const int kept = plan.each == 2 ? places * plan.each * kGroup * 4 : 0;  // weights
-      const int depth = row_bytes * 3 + kept <= (places <= kGradHalf ? 112 : 224) * 1024 ? 3 : 2;
-      const int bytes = row_bytes * depth + kept;
-      auto kernel = full ? pick_grad<T, true>(plan.each, depth, places) : pick_grad<T, false>(plan.each, depth, places);
+      const int bytes = copy_bytes<T>(plan.each, places);
+      auto kernel = full ? pick_grad<T, true>(plan.each, places) : pick_grad<T, false>(plan.each, places);
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
       if (e != cudaSuccess) return launched(e);
       kernel<<<unsigned(parts), threads, bytes, stream>>>(a);
