@@ -751,12 +751,7 @@ int run_as(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t exper
   const int64_t channel_tiles = (P.N + kPairChannels - 1) / kPairChannels;
   const int64_t pair_tiles = int64_t(std::min(P.G, P.M)) * ((rows + kPairTokens - 1) / kPairTokens) * channel_tiles;
   Maps maps;
-  // Pairs for more than 64 tokens and for experts where there are 16 tiles for them, for fewer tokens where nearly every
-  // pair gets one; else narrow tiles, which share K between CTAs.  In us, pairs and narrow tiles: 32, 64 and 128 tokens
-  // through 8192 x 3584 9.8 10.0 10.3 and 8.7 9.8 12.5; 64 through 16384 x 8192 18.0 and 20.0; 300 through 1024 x 4096 (8
-  // tiles) 10.1 and 8.8; 600 through 1024 x 1024 (16) 7.0 and 9.3; 64 experts of 4096 x 1024 with 1, 4 and 16 rows 23.5 28.3
-  // 32.7 and 31.2 41.4 68.2.
-  if (pair_tiles >= (rows > 64 || P.G > 1 ? 16 : 64)) {
+  if (product_by_pairs(rows, pair_tiles)) {
     Params Q = P;
     Q.tile_rows = pair_rows(P, rows);
     if (!make_maps(&maps, A, lda, B, ldb, expert_stride, Q, Q.tile_rows / 2)) return ENTWINE_ERR_CUDA;

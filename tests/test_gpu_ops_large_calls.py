@@ -153,6 +153,8 @@ def test_product_of_exact_sums(M, N_, K, dtype):
 
 @pytest.mark.parametrize("dtype", FLOATING, ids=_id)
 @pytest.mark.parametrize("counts,N_,K", [((700, 0, 350, 1200, 65, 900, 300, 513), 2048, 1280), ((700, 0, 350, 1200, 65, 900, 300, 513), 2048, 2336),
-                                         ((30, 1, 0, 90, 17, 64, 5, 33) * 4, 2304, 1536), ((16,) * 64, 1536, 1100)])
+                                         ((30, 1, 0, 90, 17, 64, 5, 33) * 4, 2304, 1536), ((16,) * 64, 1536, 1100),
+                                         # few rows and tiles: narrow tiles, K shared by the CTAs of a cluster
+                                         ((16, 0, 9, 40, 3, 16, 20, 1), 512, 4096), ((64, 30, 70, 64), 1000, 3000)])
 def test_grouped_product_of_exact_sums(counts, N_, K, dtype):
     Q._grouped(counts, N_, K, dtype, bias=True, spare=5, first=3)
