@@ -213,11 +213,13 @@ int entwine_dropout(const void* x, int dtype, int64_t rows, int64_t cols, int64_
  *   hidden = residual + dropout(x)   (rounded to dtype; without residual and with p = 0 it is x)
  *   mean = sum_c hidden / cols;  rstd = 1 / sqrt(sum_c (hidden - mean)^2 / cols + eps);
  *   out = (hidden - mean) rstd weight + bias
- * computed in fp32 from the rounded hidden values, as entwine_gemm_rs_norm does.  dropout, p, rng, row0: entwine_dropout.
+ * computed in fp32 from the rounded hidden values, as entwine_gemm_rs_norm does (sums over more than 16384 columns in more bits).
+ * dropout, p, rng, row0: entwine_dropout.
  *   x, residual (or NULL), hidden (NULL: not written), out: [rows, cols] of one dtype
  *   weight, bias (or NULL) [cols], both of w_dtype: dtype or ENTWINE_FP32
  *   mean, rstd [rows] fp32 (NULL: not written), what the gradients need;  eps >= 0
- * A row of equal values has variance 0: with eps = 0 its out is NaN.  rows = 0 does nothing.
+ * A row of equal values has variance 0 but for the rounding of its mean: with eps = 0 its out is NaN, or of the order of
+ * the weight where the mean came out one rounding beside the values.  rows = 0 does nothing.
  *
  * entwine_layer_norm_bwd - its gradients for dout [rows, cols], with n = (hidden - mean) rstd and g = dout weight:
  *   dh = rstd (g - sum_c g / cols - n sum_c (g n) / cols) + dhidden
@@ -227,6 +229,8 @@ int entwine_dropout(const void* x, int dtype, int64_t rows, int64_t cols, int64_
  *   dweight, dbias [cols] fp32, dbias may be NULL; of no rows they are 0
  *   work       work_floats fp32 values, at least what entwine_layer_norm_bwd_work gives for these extents; the partial
  *              sums of dweight and dbias, added in a fixed order.  Calls that may overlap (two streams, two graphs) need one each.
+ * dweight and dbias are fp32 sums, so their error grows with the rows as such sums' does.  fp32 rows of 8193 to 16384 columns
+ * take the time of rows that start anywhere, wherever they start.
  * mean and rstd, p, rng and row0 as in the forward call.  Errors of all three: ENTWINE_ERR_INVALID, ENTWINE_ERR_CUDA.
  */
 int entwine_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* residual,

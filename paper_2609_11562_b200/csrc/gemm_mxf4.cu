@@ -139,7 +139,7 @@ struct Scales {
 // One tile of 128 channels x TOKENS tokens per cluster of one to eight CTAs, which share the length K: each sums its
 // blocks of K, then the partial sums meet through distributed shared memory, added in the order of the CTAs, each CTA
 // finishing its share of the tokens.  So a decoding step reads the weights with all SMs.  16 tokens through 8192 x 3584 take
-// 8.1 us, the weight's 15.6 MB at 2.4 TB/s: start, the latency of the three or four blocks that a CTA has, and the exchange.
+// 8.1 us, the weight's 15.6 MB at 1.9 TB/s: start, the latency of the three or four blocks that a CTA has, and the exchange.
 template <int TOKENS, typename Out>
 __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_constant__ Maps maps,
                                                              const __grid_constant__ Params P) {
@@ -325,10 +325,11 @@ __global__ void __launch_bounds__(kThreads) gemm_mxf4_kernel(const __grid_consta
 // half of the tokens' codes and all of their scales).  Two accumulators in TMEM, 2 x 192 of its 512 columns, so that the
 // epilogue of a tile runs beside the products of the next, and five buffers of scales of 24 columns.  (224 tokens leave
 // room for two: the way from products that are done to the next but one's scales is then longer than the products between.)
-// 8192 x 8192 x 3584 takes 108 to 117 us, up to 4.4 PFLOP/s: 600 to 670 cycles a block of K, of which the products are 384 and
-// the issuing warp's own instructions 330, at a clock that the power limit holds at 1.5 to 1.6 GHz.
-// TMA warp, MMA warp, epilogue warps by groups of four, scale warps, their messenger.  (Eight epilogue warps: 59 us instead of
-// 53 for 32 experts' 15.6k rows of 4096 x 1024, where the epilogue is what a tile waits for; 16 have too few registers.)
+// 8192 x 8192 x 3584 takes 115 to 118 us, 4.2 PFLOP/s: 670 to 680 cycles a block of K, of which the products are 384 and the
+// issuing warp's own instructions 330, at 1.7 GHz; 135 us in a long series, which the power limit holds at 1.44 GHz.
+// TMA warp, MMA warp, epilogue warps by groups of four, scale warps, their messenger.  (Eight epilogue warps: 59 us where
+// twelve took 53, for 32 experts' 15.6k rows of 4096 x 1024, where the epilogue is what a tile waits for; 16 have too few
+// registers.)
 constexpr int kEpilogueGroups = 3, kScaleWarps = 4;
 constexpr int kFirstScaleWarp = 2 + 4 * kEpilogueGroups, kPairThreads = 32 * (kFirstScaleWarp + kScaleWarps + 1);
 constexpr int kPairTokens = 192;
@@ -482,7 +483,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) gemm_mxf4_pair_kernel(const _
         if (!(ok = warp_wait<true>(P, tempty + 8 * acc, acc_phase ^ 1))) break;
         const uint32_t d = base + acc * kPairTokens;
         int columns = 0;
-        // two blocks at a time: what a turn costs beside the products is paid half as often
+        // two blocks at a time: what a turn costs beside the products is paid half as often (one at a time: 128 us instead of 115)
         for (int b = 0; b < blocks; b += 2) {
           const bool two = b + 1 < blocks, last = b + 2 >= blocks, group_ends = last || b % kGroupStages == kGroupStages - 2;
           const int next = stage + 1 < S ? stage + 1 : 0, after = next + 1 < S ? next + 1 : 0;

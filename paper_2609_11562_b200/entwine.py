@@ -400,7 +400,8 @@ def dequant_mxf4(q, scale, x, stream=None):
 def gemm_mxf4(a, scale_a, b, scale_b, out, bias=None, stream=None):
     """out[m, n] = sum_k a[m, k] b[n, k] (+ bias[n]) of the values that codes and scales stand for.  a [M, ceil(K/2)],
     b [N, ceil(K/2)] uint8 with rows on 16-byte boundaries; scale_a [M, ceil(K/32)], scale_b [N, ceil(K/32)] uint8 with rows on
-    4-byte boundaries; bias [N] fp32; out [M, N] bf16, fp16 or fp32."""
+    4-byte boundaries (a contiguous [N, 90] needs a copy with rows of 92); of an odd K the last upper half is zero, as quant_mxf4
+    writes it; bias [N] fp32; out [M, N] bf16, fp16 or fp32."""
     _opcalls.gemm_mxf4(a, scale_a, b, scale_b, out, bias, stream)
 
 
